@@ -345,6 +345,145 @@ int bd_lce_objective(const float* logp, const float* logp_old, const float* logp
                      const float* weight, int N, int kind, float eps, float beta, float* loss, float* dlogp,
                      hipStream_t stream);
 
+/*
+ * Norms of queries and keys for each head with the rotary embedding, in front
+ * of the attention: from the projections' token-major layout into the
+ * attention's head-major one, in one pass.  For every head row x of D values of
+ * token (b, n) at position p = positions[b * pos_stride + n]:
+ *   r = (mean(x^2) + eps)^(-1/2),  y = w x r,
+ *   out[j]       = y[j] cos(p f_j) - y[j + D/2] sin(p f_j)
+ *   out[j + D/2] = y[j + D/2] cos(p f_j) + y[j] sin(p f_j)      (j < D/2)
+ * with w = q_weight for query heads, k_weight for key heads; value heads are
+ * laid out only.
+ *
+ * Q, K, V: projections; head h of token (b, n) starts at element
+ *   b * stride[0] + n * stride[1] + h * stride[2] of its array, `strides` (a
+ *   HOST array of 9) holding those of Q, K and V in turn, each a non-negative
+ *   multiple of 8 (arrays may be views of one fused projection, or broadcast).
+ * Qo, Ko, Vo: [B, Hq, N, D], [B, Hkv, N, D], [B, Hkv, N, D] contiguous: what
+ *   bd_attn_fwd takes with N = 2L (for packed sequences, B = 1 and N = 2T give
+ *   bd_attn_varlen_fwd's [H, 2T, D]; N = S gives the decode calls' blocks).
+ * rope: [n_rope, D] float32, row p the cosines, then the sines of position p
+ *   (bd_rope_table).  positions: DEVICE int32 array, values clamped to
+ *   [0, n_rope); pos_stride 0: the same positions for every b.
+ * dtype: BD_ATTN_BF16, or BD_ATTN_FP32 for float32 rows (in float32 throughout
+ *   here).  wdtype: type of q_weight and k_weight [D], BD_ATTN_FP32 or dtype.
+ * Arithmetic is in float32, each result is rounded once.  D is 64 or 128;
+ * B, N >= 0 (nothing is enqueued for no tokens), B * N <= 2^28, Hq and Hkv up to
+ * 2^14 (Hq need not be a multiple of Hkv), eps >= 0, n_rope >= 1.  Every array
+ * 16-byte aligned, positions 4-byte.  Ownership, stream order and errors are as
+ * for bd_attn_fwd.
+ */
+int bd_qk_norm_rope_fwd(const void* Q, const void* K, const void* V, const int64_t* strides, const void* q_weight,
+                        const void* k_weight, const float* rope, int n_rope, const int32_t* positions,
+                        int64_t pos_stride, int B, int N, int Hq, int Hkv, int D, float eps, int dtype, int wdtype,
+                        void* Qo, void* Ko, void* Vo, hipStream_t stream);
+/*
+ * Its vector-Jacobian product: from dQo, dKo, dVo (contiguous as the outputs)
+ * and the forward's Q and K, the gradients dQ, dK, dV of the projections
+ * (`grad_strides`: 9 host values as above; rows must not overlap, but the three
+ * may be views of one fused gradient), and those of the weights, dq_weight and
+ * dk_weight ([D] of wdtype, summed in float32 over all tokens and heads in a
+ * fixed order: results are bitwise reproducible; zeros for no tokens).
+ * `strides`: 6 host values, those of Q and K.  ws/ws_bytes: at least
+ * bd_qk_norm_rope_workspace_bytes bytes, 16-byte aligned.
+ */
+int bd_qk_norm_rope_bwd(const void* dQo, const void* dKo, const void* dVo, const void* Q, const void* K,
+                        const int64_t* strides, const void* q_weight, const void* k_weight, const float* rope,
+                        int n_rope, const int32_t* positions, int64_t pos_stride, int B, int N, int Hq, int Hkv,
+                        int D, float eps, int dtype, int wdtype, void* dQ, void* dK, void* dV,
+                        const int64_t* grad_strides, void* dq_weight, void* dk_weight, void* ws, size_t ws_bytes,
+                        hipStream_t stream);
+/* Workspace bytes for bd_qk_norm_rope_bwd; 0 for arguments it would reject (and for no tokens). */
+size_t bd_qk_norm_rope_workspace_bytes(int B, int N, int Hq, int Hkv, int D, int dtype);
+/*
+ * bd_qk_norm_rope_fwd for serving (bfloat16 rows): queries to Qo [B, Hq, N, D],
+ * keys and values into the pages of a cache.  slots: DEVICE int32 [B * N], the
+ * row of the pages that token b * N + n goes to, page * page_size + row in the
+ * page (bd_paged_plan); a slot outside [0, num_pages * page_size) writes nothing,
+ * and the slots of a call that write must differ (two tokens in one slot leave
+ * a mixture of both).
+ * Pages: row r of KV head h of page g starts at element
+ *   g * page_stride + h * head_stride + r * row_stride of K_pages and of V_pages
+ *   (multiples of 8; rows must not overlap, K and V may be interleaved), so
+ *   pages may hold their heads or their tokens outermost.  page_size: a power of two from
+ *   16 to 2^15; num_pages >= 1, num_pages * page_size <= 2^31 - 1.
+ */
+int bd_qk_norm_rope_paged(const void* Q, const void* K, const void* V, const int64_t* strides, const void* q_weight,
+                          const void* k_weight, const float* rope, int n_rope, const int32_t* positions,
+                          int64_t pos_stride, const int32_t* slots, int B, int N, int Hq, int Hkv, int D, float eps,
+                          int dtype, int wdtype, void* Qo, void* K_pages, void* V_pages, int num_pages, int page_size,
+                          int64_t page_stride, int64_t head_stride, int64_t row_stride, hipStream_t stream);
+/*
+ * Rows of the rotary table: table[p][j] = cos(p inv_freq[j]) and
+ * table[p][D/2 + j] = sin(p inv_freq[j]) for p < n, j < D/2; inv_freq: DEVICE
+ * float64 [D/2] (angles are formed in float64), table: float32 [n, D].
+ * 1 <= n <= 2^25, D 64 or 128.
+ */
+int bd_rope_table(const double* inv_freq, int n, int D, float* table, hipStream_t stream);
+
+/*
+ * Page tables and slots for the next tokens of B sequences, from lengths that
+ * only the device knows.  Sequence b holds len_b = cache_lens[b] tokens (clamped to its
+ * room max_pages * page_size) in the pages of row b of page_table and gets
+ * new_lens[b] more (clamped to be non-negative).  Every page that these begin
+ * is taken from the free list, in sequence order from entry free_head[0]
+ * (clamped to [0, n_free]) on, and entered in the table.
+ *
+ * page_table: [B] rows of max_pages int32, table_stride elements apart, updated
+ *   in place: only the entries of pages begun by this call are written.
+ * free_pages: int32 [n_free], ids of pages in [0, num_pages) that no table
+ *   holds (not checked: a page twice in it serves two sequences); an id outside
+ *   is entered as -1 and gives its tokens no slot.  free_head: int32 [1].
+ * S >= 1: slots and positions are [B, S], row b those of the (up to S) new
+ *   tokens of sequence b; total is ignored.  S = 0: they are [total], the new
+ *   tokens of all sequences in order; new_lens must sum to at most total.
+ * Results (int32): lens [B], cache_lens[b] + new_lens[b], at most the room; cu
+ *   [B + 1], the sums of the new lengths before each sequence; slots, the row
+ *   page * page_size + position mod page_size of each new token, -1 for rows that hold none and
+ *   for tokens without a page; positions, len_b + i of each new token, 0 in rows
+ *   that hold none; state [2], the free list's new head (at most n_free), and
+ *   the number of new tokens without a slot, 0 if all is well: those past the
+ *   room, in the pages that the free list could not give (entered as -1), behind
+ *   cached tokens whose last page is none, or past total.
+ * B from 1 to 2^16, max_pages >= 1, max_pages * page_size <= 2^30, page_size a
+ * power of two from 16 to 2^15, num_pages * page_size <= 2^31 - 1, B * S and total at most 2^30.
+ * All arrays are on the device, 4-byte aligned; outputs must not overlap
+ * inputs or each other (lens may become the next call's cache_lens, state its
+ * free_head).  Ownership, stream order and errors are as for bd_attn_fwd.
+ */
+int bd_paged_plan(const int32_t* cache_lens, const int32_t* new_lens, int32_t* page_table, int B, int max_pages,
+                  int64_t table_stride, const int32_t* free_pages, int n_free, const int32_t* free_head,
+                  int num_pages, int page_size, int S, int total, int32_t* lens, int32_t* cu, int32_t* slots,
+                  int32_t* positions, int32_t* state, hipStream_t stream);
+
+/*
+ * Decoding over a paged cache: bd_attn_decode_fwd with the cached keys and
+ * values in pages (layout as for bd_qk_norm_rope_paged, page g of sequence b
+ * being page_table[b * table_stride + g]), and K_new, V_new optional: without
+ * them (both NULL) the queries see the cache alone, as when the new token's own
+ * key is already in it.  S is 1 for token-by-token decoding.
+ *
+ * Keys j < cache_lens[b] (clamped to [0, max_pages * page_size]) are read;
+ * nothing else in the pages is.  A table entry outside [0, num_pages) stands for a page without
+ * keys (never written, or dropped): its positions are left out of the softmax.
+ * A row that sees no key gets O = 0 and LSE = -inf.
+ * Values in K, V and Q must be finite.  bfloat16 only; D, S, B, heads, scale,
+ * O [B, Hq, S, D] and LSE [B, Hq, S] as for bd_attn_decode_fwd, max_pages >= 1
+ * and max_pages * page_size <= 2^22; page_size, num_pages as for bd_paged_plan;
+ * page strides are multiples of 8, row_stride at least D and at most 2^20.
+ * ws/ws_bytes: at least bd_attn_paged_decode_workspace_bytes bytes (16-byte
+ * aligned; it need not be initialised).
+ */
+int bd_attn_paged_decode_fwd(const void* Q, const void* K_pages, const void* V_pages, const int32_t* page_table,
+                             const int32_t* cache_lens, const void* K_new, const void* V_new, int B, int S, int Hq,
+                             int Hkv, int D, int num_pages, int page_size, int max_pages, int64_t table_stride,
+                             int64_t page_stride, int64_t head_stride, int64_t row_stride, float scale, int dtype,
+                             void* O, float* LSE, void* ws, size_t ws_bytes, hipStream_t stream);
+/* Workspace bytes for bd_attn_paged_decode_fwd; 0 for arguments it would reject. */
+size_t bd_attn_paged_decode_workspace_bytes(int B, int S, int Hq, int Hkv, int D, int page_size, int max_pages,
+                                            int dtype);
+
 /* Comma-separated names of the kernels bd_attn_fwd (for_bwd = 0) or
  * bd_attn_bwd (for_bwd = 1) launch for `dtype`, in launch order (static). */
 const char* bd_attn_stage_names(int for_bwd, int dtype);

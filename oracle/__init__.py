@@ -1,4 +1,5 @@
-"""Plain fp64 CPU oracle for block-diffusion masked attention and for the
+"""Plain fp64 CPU oracle for block-diffusion masked attention, for the norms
+and rotations in front of it, for decoding over a paged cache, and for the
 token log-probabilities and objectives that consume its output.
 
 TEST INFRASTRUCTURE ONLY.  Only the test suite, the smoke check and the
@@ -25,3 +26,5 @@ from .lce_oracle import (  # noqa: F401
     dipo_objective,
     lm_head_sampled,
 )
+from .rope_oracle import rope_table, norm_rope, norm_rope_backward  # noqa: F401
+from .paged_oracle import paged_decode_forward, paged_plan  # noqa: F401

@@ -12,11 +12,14 @@ earlier blocks; a clean query sees clean keys of its own and earlier blocks.
 """
 from __future__ import annotations
 
+import collections
+import contextlib
 import ctypes
 import functools
 
 import numpy as np
 import torch
+from torch.autograd.function import once_differentiable
 
 from ._lib import LIB_PATH, BdAttnError, lib, status_string  # noqa: F401
 
@@ -33,6 +36,9 @@ __all__ = [
     "bd_attn_varlen_workspace_bytes", "bd_attn_decode_fwd", "bd_attn_decode_workspace_bytes",
     "bd_lce_fwd", "bd_lce_bwd", "bd_lce_workspace_bytes", "bd_lce_logits_bytes", "bd_lce_objective", "LceFunction", "lm_head_logprobs",
     "BD_LCE_CE", "BD_LCE_DIPO",
+    "bd_rope_table", "bd_qk_norm_rope_fwd", "bd_qk_norm_rope_bwd", "bd_qk_norm_rope_workspace_bytes",
+    "QkNormRopeFunction", "QkvNormRopeFunction", "qk_norm_rope", "qkv_norm_rope", "bd_qk_norm_rope_paged",
+    "bd_paged_plan", "PagedPlan", "bd_attn_paged_decode_fwd", "bd_attn_paged_decode_workspace_bytes",
 ]
 
 
@@ -549,3 +555,354 @@ def lm_head_logprobs(h, w, targets, keep_logits=False):
     [0, V): 0).  keep_logits trades N x V float32 of memory for the
     backward's recomputation of the logits."""
     return LceFunction.apply(h, w, targets, keep_logits)
+
+
+# ---------------------------------------------------------------------------
+# Norms of queries and keys with the rotary embedding, in front of the
+# attention: projections [B, N, H, D] (or [N, H, D]) with any strides in,
+# contiguous heads [B, H, N, D] ([H, N, D]) out.
+
+def _launch_context(device: torch.device, stream):
+    """Where a call allocates and launches: on the tensors' device, and on
+    `stream`, whose pool its results and workspace then come from."""
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    if device.type == "cuda" and device.index != torch.cuda.current_device():
+        return torch.cuda.device(device)
+    return contextlib.nullcontext()
+
+
+def _span(strides):
+    return (ctypes.c_int64 * len(strides))(*strides)
+
+
+def _head_rows(name, t, shape, dtype, device):
+    """Element strides (batch, token, head) of rows t [B, N, H, D], D contiguous."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name}: expected device {device}, got {t.device}")
+    if t.stride(-1) != 1 and t.numel() > 0:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    st = [s if n > 1 else 0 for n, s in zip(t.shape[:-1], t.stride()[:-1])]
+    if any(s % 8 for s in st):
+        raise ValueError(f"{name}: strides must be multiples of 8 elements, got {t.stride()}")
+    return st if len(st) == 3 else [0] + st
+
+
+def _rope_args(q, k, v, q_weight, k_weight, rope, positions):
+    """Checked arguments common to the calls: (B, N, Hq, Hkv, D, device, dtype code, input strides, the C
+    call's middle arguments, lead), lead being the leading dimensions ((B,) or ()) of the results."""
+    if q.dim() not in (3, 4) or k.dim() != q.dim():
+        raise ValueError("q [B,N,Hq,D] and k/v [B,N,Hkv,D] (or without B) expected")
+    lead = tuple(q.shape[:-3])
+    B = lead[0] if lead else 1
+    N, Hq, D = q.shape[-3:]
+    Hkv = k.shape[-2]
+    dev, dt = q.device, q.dtype
+    code = _dtype_code(q)
+    strides = _head_rows("q", q, lead + (N, Hq, D), dt, dev) + _head_rows("k", k, lead + (N, Hkv, D), dt, dev)
+    if v is not None:
+        strides += _head_rows("v", v, lead + (N, Hkv, D), dt, dev)
+    wdt = q_weight.dtype
+    if wdt not in (dt, torch.float32):
+        raise TypeError(f"q_weight: expected {dt} or torch.float32, got {wdt}")
+    _check("q_weight", q_weight, (D,), wdt, dev)
+    _check("k_weight", k_weight, (D,), wdt, dev)
+    if rope.dim() != 2:
+        raise ValueError("rope [n, D] expected")
+    _check("rope", rope, (rope.shape[0], D), torch.float32, dev)
+    if positions.dim() == 1:
+        _check("positions", positions, (N,), torch.int32, dev)
+    else:
+        _check("positions", positions, lead + (N,), torch.int32, dev)
+    pos_stride = N if positions.dim() == 2 else 0
+    middle = (_ptr(q_weight), _ptr(k_weight), _ptr(rope), rope.shape[0], _ptr(positions), pos_stride)
+    return B, N, Hq, Hkv, D, dev, code, _dtype_code(q_weight), strides, middle, lead
+
+
+def bd_rope_table(n: int, D: int, theta: float = 1e6, inv_freq=None, device="cuda", out=None, stream=None):
+    """Rotary table of positions 0..n-1: float32 [n, D], the cosines of p f_j, then the sines.
+
+    f_j = theta^(-2j/D), or inv_freq (float64 [D/2] on the device) for scaled
+    frequencies.  Angles are formed in float64."""
+    if out is not None:
+        device = out.device
+    elif inv_freq is not None:
+        device = inv_freq.device
+    device = torch.device(device)
+    if device.type == "cuda" and device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    with _launch_context(device, stream):
+        if inv_freq is None:
+            inv_freq = float(theta) ** (-2.0 * torch.arange(D // 2, dtype=torch.float64, device=device) / D)
+        _check("inv_freq", inv_freq, (D // 2,), torch.float64, device)
+        t = torch.empty((n, D), dtype=torch.float32, device=device) if out is None else out
+        _check("out", t, (n, D), torch.float32, device)
+        st = lib().bd_rope_table(_ptr(inv_freq), n, D, _ptr(t), _stream_handle(device, stream))
+    if st:
+        raise BdAttnError(st, "bd_rope_table")
+    return t
+
+
+def bd_qk_norm_rope_fwd(q, k, v, q_weight, k_weight, rope, positions, eps: float = 1e-6, q_out=None, k_out=None,
+                        v_out=None, stream=None):
+    """Heads normalised (q, k), rotated (q, k) and laid out (q, k, v) for the attention.
+
+    q [B,N,Hq,D], k, v [B,N,Hkv,D] in bfloat16 or float32, any strides that
+    are multiples of 8 with D contiguous (views of a fused projection; without
+    B for packed sequences); q_weight, k_weight [D] in that type or float32;
+    rope: bd_rope_table; positions: int32 [B,N] or [N].  Returns q [B,Hq,N,D],
+    k, v [B,Hkv,N,D], contiguous."""
+    B, N, Hq, Hkv, D, dev, code, wcode, strides, middle, lead = _rope_args(q, k, v, q_weight, k_weight, rope, positions)
+    with _launch_context(dev, stream):
+        outs = []
+        for name, t, H in (("q_out", q_out, Hq), ("k_out", k_out, Hkv), ("v_out", v_out, Hkv)):
+            shape = lead + (H, N, D)
+            if t is None:
+                t = torch.empty(shape, dtype=q.dtype, device=dev)
+            _check(name, t, shape, q.dtype, dev)
+            outs.append(t)
+        st = lib().bd_qk_norm_rope_fwd(_ptr(q), _ptr(k), _ptr(v), _span(strides), *middle, B, N, Hq, Hkv, D, float(eps),
+                                       code, wcode, *map(_ptr, outs), _stream_handle(dev, stream))
+    if st:
+        raise BdAttnError(st, "bd_qk_norm_rope_fwd")
+    return tuple(outs)
+
+
+def bd_qk_norm_rope_workspace_bytes(B, N, Hq, Hkv, D, dtype=BD_ATTN_BF16) -> int:
+    return int(lib().bd_qk_norm_rope_workspace_bytes(B, N, Hq, Hkv, D, int(dtype)))
+
+
+def bd_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, rope, positions, eps: float = 1e-6, grad_q=None,
+                        grad_k=None, grad_v=None, grad_q_weight=None, grad_k_weight=None, workspace=None, stream=None):
+    """Gradients of bd_qk_norm_rope_fwd for those of its results, dq [B,Hq,N,D] and dk, dv
+    [B,Hkv,N,D] (contiguous): returns those of q, k, v (new, or the given arrays with any non-overlapping
+    strides) and of the weights."""
+    B, N, Hq, Hkv, D, dev, code, wcode, strides, middle, lead = _rope_args(q, k, None, q_weight, k_weight, rope, positions)
+    for name, t, H in (("dq", dq, Hq), ("dk", dk, Hkv), ("dv", dv, Hkv)):
+        _check(name, t, lead + (H, N, D), q.dtype, dev)
+    with _launch_context(dev, stream):
+        grads, gstrides = [], []
+        for name, t, H in (("grad_q", grad_q, Hq), ("grad_k", grad_k, Hkv), ("grad_v", grad_v, Hkv)):
+            shape = lead + (N, H, D)
+            if t is None:
+                t = torch.empty(shape, dtype=q.dtype, device=dev)
+            gstrides += _head_rows(name, t, shape, q.dtype, dev)
+            grads.append(t)
+        for name, t, w in (("grad_q_weight", grad_q_weight, q_weight), ("grad_k_weight", grad_k_weight, k_weight)):
+            t = torch.empty_like(w) if t is None else t
+            _check(name, t, (D,), w.dtype, dev)
+            grads.append(t)
+        nbytes = _known_size("bd_qk_norm_rope_workspace_bytes", B, N, Hq, Hkv, D, code)
+        ws, wp, wn = _workspace(nbytes, dev, workspace)
+        st = lib().bd_qk_norm_rope_bwd(_ptr(dq), _ptr(dk), _ptr(dv), _ptr(q), _ptr(k), _span(strides), *middle, B, N, Hq,
+                                       Hkv, D, float(eps), code, wcode, *map(_ptr, grads[:3]), _span(gstrides),
+                                       *map(_ptr, grads[3:]), wp, wn, _stream_handle(dev, stream))
+    if st:
+        raise BdAttnError(st, "bd_qk_norm_rope_bwd")
+    return tuple(grads)
+
+
+class QkNormRopeFunction(torch.autograd.Function):
+    """Autograd wrapper over separate projections."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, q_weight, k_weight, rope, positions, eps):
+        ctx.save_for_backward(q, k, q_weight, k_weight, rope, positions)
+        ctx.eps = eps
+        return bd_qk_norm_rope_fwd(q, k, v, q_weight, k_weight, rope, positions, eps)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq, dk, dv):
+        q, k, *rest = ctx.saved_tensors
+        grads = bd_qk_norm_rope_bwd(dq.contiguous(), dk.contiguous(), dv.contiguous(), q, k, *rest, ctx.eps)
+        return (*grads, None, None, None)
+
+
+def _qkv_views(qkv, Hq, Hkv, D):
+    """q, k, v [.., H, D] of a fused projection [.., (Hq + 2 Hkv) D]."""
+    x = qkv.unflatten(-1, (Hq + 2 * Hkv, D))
+    return x[..., :Hq, :], x[..., Hq:Hq + Hkv, :], x[..., Hq + Hkv:, :]
+
+
+class QkvNormRopeFunction(torch.autograd.Function):
+    """Autograd wrapper over a fused projection, whose gradient is written in place of three."""
+
+    @staticmethod
+    def forward(ctx, qkv, Hq, Hkv, q_weight, k_weight, rope, positions, eps):
+        ctx.save_for_backward(qkv, q_weight, k_weight, rope, positions)
+        ctx.heads, ctx.eps = (Hq, Hkv), eps
+        return bd_qk_norm_rope_fwd(*_qkv_views(qkv, Hq, Hkv, q_weight.numel()), q_weight, k_weight, rope, positions, eps)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq, dk, dv):
+        qkv, q_weight, *rest = ctx.saved_tensors
+        D = q_weight.numel()
+        q, k, _ = _qkv_views(qkv, *ctx.heads, D)
+        grad = torch.empty(qkv.shape, dtype=qkv.dtype, device=qkv.device)
+        gq, gk, gv = _qkv_views(grad, *ctx.heads, D)
+        *_, dwq, dwk = bd_qk_norm_rope_bwd(dq.contiguous(), dk.contiguous(), dv.contiguous(), q, k, q_weight, *rest,
+                                           ctx.eps, gq, gk, gv)
+        return grad, None, None, dwq, dwk, None, None, None
+
+
+def qk_norm_rope(q, k, v, q_weight, k_weight, rope, positions, eps: float = 1e-6):
+    """bd_qk_norm_rope_fwd, differentiable in q, k, v and the weights."""
+    return QkNormRopeFunction.apply(q, k, v, q_weight, k_weight, rope, positions, eps)
+
+
+def qkv_norm_rope(qkv, Hq: int, Hkv: int, q_weight, k_weight, rope, positions, eps: float = 1e-6):
+    """The same on a fused projection qkv [B, N, (Hq + 2 Hkv) D] (queries, keys, values)."""
+    return QkvNormRopeFunction.apply(qkv, Hq, Hkv, q_weight, k_weight, rope, positions, eps)
+
+
+# ---------------------------------------------------------------------------
+# Paged KV cache: k_pages, v_pages [pages, Hkv, page_size, D] bfloat16 with any
+# equal strides (a cache kept token-major is passed as its permuted view).
+
+def _pages(k_pages, v_pages, Hkv, D, device):
+    """Page arguments of the C calls: (pages, page size) and the strides."""
+    if k_pages.dim() != 4:
+        raise ValueError("k_pages and v_pages [pages,Hkv,page_size,D] expected")
+    n, P = k_pages.shape[0], k_pages.shape[2]
+    for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+        if tuple(t.shape) != (n, Hkv, P, D):
+            raise ValueError(f"{name}: expected shape {(n, Hkv, P, D)}, got {tuple(t.shape)}")
+        if t.dtype != torch.bfloat16:
+            raise TypeError(f"{name}: expected {torch.bfloat16}, got {t.dtype}")
+        if t.device != device:
+            raise ValueError(f"{name}: expected device {device}, got {t.device}")
+    if k_pages.stride() != v_pages.stride() or k_pages.stride(3) != 1:
+        raise ValueError("k_pages and v_pages: equal strides with the last dimension contiguous expected")
+    # (a dimension of one page or head has no stride of its own)
+    sp, sh, sr = (s if m > 1 else 0 for m, s in zip(k_pages.shape[:3], k_pages.stride()[:3]))
+    if sp % 8 or sh % 8 or sr % 8:
+        raise ValueError(f"k_pages: strides must be multiples of 8 elements, got {k_pages.stride()}")
+    return n, P, sp, sh, sr
+
+
+def bd_qk_norm_rope_paged(q, k, v, q_weight, k_weight, rope, positions, slots, k_pages, v_pages, eps: float = 1e-6,
+                          q_out=None, stream=None):
+    """bd_qk_norm_rope_fwd for serving: returns the queries [B,Hq,N,D] and writes keys and values into
+    the pages, token (b, n) at row slots[b, n] (int32 [B,N] of bd_paged_plan; outside the pages: not written)."""
+    B, N, Hq, Hkv, D, dev, code, wcode, strides, middle, lead = _rope_args(q, k, v, q_weight, k_weight, rope, positions)
+    if q.dtype != torch.bfloat16:
+        raise TypeError(f"bd_qk_norm_rope_paged supports bfloat16 tensors, got {q.dtype}")
+    _check("slots", slots, lead + (N,), torch.int32, dev)
+    n, P, sp, sh, sr = _pages(k_pages, v_pages, Hkv, D, dev)
+    with _launch_context(dev, stream):
+        o = torch.empty(lead + (Hq, N, D), dtype=q.dtype, device=dev) if q_out is None else q_out
+        _check("q_out", o, lead + (Hq, N, D), q.dtype, dev)
+        st = lib().bd_qk_norm_rope_paged(_ptr(q), _ptr(k), _ptr(v), _span(strides), *middle, _ptr(slots), B, N, Hq, Hkv, D,
+                                         float(eps), code, wcode, _ptr(o), _ptr(k_pages), _ptr(v_pages), n, P, sp, sh, sr,
+                                         _stream_handle(dev, stream))
+    if st:
+        raise BdAttnError(st, "bd_qk_norm_rope_paged")
+    return o
+
+
+PagedPlan = collections.namedtuple("PagedPlan", "lens cu slots positions state")
+
+
+def bd_paged_plan(cache_lens, new_lens, page_table, free_pages, free_head, num_pages: int, page_size: int, S=None,
+                  total=None, lens=None, cu=None, slots=None, positions=None, state=None, stream=None):
+    """Pages and slots for the next tokens of a batch, from lengths on the device.
+
+    cache_lens, new_lens: int32 [B]; page_table: int32 [B, max_pages] (rows may
+    be strided), updated in place; free_pages: int32 [n]; free_head: int32 [1].
+    With S, slots and positions are [B, S] (up to S new tokens a sequence),
+    else [total], packed (total: at least the sum of new_lens).  Returns
+    PagedPlan(lens [B], cu [B+1], slots, positions, state [2]): state[0] is the
+    new head of the free list, state[1] the tokens without a slot."""
+    dev = cache_lens.device
+    B = cache_lens.numel()
+    _check("cache_lens", cache_lens, (B,), torch.int32, dev)
+    _check("new_lens", new_lens, (B,), torch.int32, dev)
+    if page_table.dim() != 2 or page_table.shape[0] != B:
+        raise ValueError(f"page_table: expected shape ({B}, max_pages), got {tuple(page_table.shape)}")
+    if page_table.dtype != torch.int32:
+        raise TypeError(f"page_table: expected {torch.int32}, got {page_table.dtype}")
+    if page_table.device != dev or (page_table.stride(1) != 1 and page_table.shape[1] > 1):
+        raise ValueError(f"page_table: contiguous rows on {dev} expected")
+    if free_pages.dim() != 1:
+        raise ValueError("free_pages: 1-D expected")
+    _check("free_pages", free_pages, (free_pages.numel(),), torch.int32, dev)
+    _check("free_head", free_head, (1,), torch.int32, dev)
+    if S is None and total is None:
+        raise ValueError("S (rows of S tokens a sequence) or total (packed tokens) expected")
+    if S is not None and S < 1:
+        raise ValueError(f"S: at least 1 expected, got {S}")
+    shape = (int(total),) if S is None else (B, int(S))
+    width = page_table.shape[1]
+    with _launch_context(dev, stream):
+        out = []
+        for name, t, shp in (("lens", lens, (B,)), ("cu", cu, (B + 1,)), ("slots", slots, shape),
+                             ("positions", positions, shape), ("state", state, (2,))):
+            t = torch.empty(shp, dtype=torch.int32, device=dev) if t is None else t
+            _check(name, t, shp, torch.int32, dev)
+            out.append(t)
+        st = lib().bd_paged_plan(_ptr(cache_lens), _ptr(new_lens), _ptr(page_table), B, width,
+                                 page_table.stride(0) if B > 1 else width, _ptr(free_pages), free_pages.numel(),
+                                 _ptr(free_head), num_pages, page_size, 0 if S is None else S, shape[0] if S is None else 0,
+                                 *map(_ptr, out), _stream_handle(dev, stream))
+    if st:
+        raise BdAttnError(st, "bd_paged_plan")
+    return PagedPlan(*out)
+
+
+def bd_attn_paged_decode_workspace_bytes(B, S, Hq, Hkv, D, page_size, max_pages, dtype=BD_ATTN_BF16) -> int:
+    return int(lib().bd_attn_paged_decode_workspace_bytes(B, S, Hq, Hkv, D, page_size, max_pages, int(dtype)))
+
+
+def bd_attn_paged_decode_fwd(q, k_pages, v_pages, page_table, cache_lens, k_new=None, v_new=None, scale=None, out=None,
+                             lse=None, workspace=None, stream=None):
+    """bd_attn_decode_fwd over a paged cache; returns (O [B,Hq,S,D], LSE [B,Hq,S] float32).
+
+    q [B,Hq,S,D] (S = 1: the next token of each sequence); k_pages, v_pages
+    [pages,Hkv,page_size,D]; page_table int32 [B,max_pages] (rows may be
+    strided); cache_lens int32 [B], clamped to [0, max_pages * page_size];
+    k_new, v_new [B,Hkv,S,D]: the block's own keys, or None where the queries
+    see the cache alone.  Rows that see no key: O = 0, LSE = -inf."""
+    if q.dim() != 4 or k_pages.dim() != 4:
+        raise ValueError("q [B,Hq,S,D] and k_pages/v_pages [pages,Hkv,page_size,D] expected")
+    B, Hq, S, D = q.shape
+    Hkv = k_pages.shape[1]
+    dev = q.device
+    if q.dtype != torch.bfloat16:
+        raise TypeError(f"bd_attn_paged_decode_fwd supports bfloat16 tensors, got {q.dtype}")
+    _check("q", q, (B, Hq, S, D), torch.bfloat16, dev)
+    n, P, sp, sh, sr = _pages(k_pages, v_pages, Hkv, D, dev)
+    if page_table.dim() != 2 or page_table.shape[0] != B:
+        raise ValueError(f"page_table: expected shape ({B}, max_pages), got {tuple(page_table.shape)}")
+    if page_table.dtype != torch.int32:
+        raise TypeError(f"page_table: expected {torch.int32}, got {page_table.dtype}")
+    width = page_table.shape[1]
+    if page_table.device != dev or (page_table.stride(1) != 1 and width > 1):
+        raise ValueError(f"page_table: contiguous rows on {dev} expected")
+    _check("cache_lens", cache_lens, (B,), torch.int32, dev)
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new: both or neither expected")
+    kn = vn = None
+    if k_new is not None:
+        _check("k_new", k_new, (B, Hkv, S, D), torch.bfloat16, dev)
+        _check("v_new", v_new, (B, Hkv, S, D), torch.bfloat16, dev)
+        kn, vn = _ptr(k_new), _ptr(v_new)
+    with _launch_context(dev, stream):
+        o = torch.empty_like(q) if out is None else out
+        l_ = torch.empty((B, Hq, S), dtype=torch.float32, device=dev) if lse is None else lse
+        _check("out", o, q.shape, torch.bfloat16, dev)
+        _check("lse", l_, (B, Hq, S), torch.float32, dev)
+        nbytes = _known_size("bd_attn_paged_decode_workspace_bytes", B, S, Hq, Hkv, D, P, width, BD_ATTN_BF16)
+        ws, wp, wn = _workspace(nbytes, dev, workspace)
+        st = lib().bd_attn_paged_decode_fwd(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(cache_lens), kn,
+                                            vn, B, S, Hq, Hkv, D, n, P, width, page_table.stride(0) if B > 1 else 0,
+                                            sp, sh, sr, _scale_arg(scale), BD_ATTN_BF16, _ptr(o), _ptr(l_), wp, wn,
+                                            _stream_handle(dev, stream))
+    if st:
+        raise BdAttnError(st, "bd_attn_paged_decode_fwd")
+    return o, l_

@@ -63,6 +63,25 @@ def lib() -> ctypes.CDLL:
     L.bd_lce_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
     L.bd_lce_objective.restype = ci
     L.bd_lce_objective.argtypes = [vp, vp, vp, vp, vp, ci, ci, cf, cf, vp, vp, vp]
+    i64, s64 = ctypes.c_int64, ctypes.POINTER(ctypes.c_int64)
+    L.bd_rope_table.restype = ci
+    L.bd_rope_table.argtypes = [vp, ci, ci, vp, vp]
+    rope = [vp, vp, vp, ci, vp, i64, ci, ci, ci, ci, ci, cf, ci, ci]  # weights ... wdtype (without slots)
+    L.bd_qk_norm_rope_fwd.restype = ci
+    L.bd_qk_norm_rope_fwd.argtypes = [vp, vp, vp, s64] + rope + [vp, vp, vp, vp]
+    L.bd_qk_norm_rope_bwd.restype = ci
+    L.bd_qk_norm_rope_bwd.argtypes = [vp, vp, vp, vp, vp, s64] + rope + [vp, vp, vp, s64, vp, vp, vp, sz, vp]
+    L.bd_qk_norm_rope_workspace_bytes.restype = sz
+    L.bd_qk_norm_rope_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci]
+    L.bd_qk_norm_rope_paged.restype = ci
+    L.bd_qk_norm_rope_paged.argtypes = ([vp, vp, vp, s64] + rope[:6] + [vp] + rope[6:]
+                                        + [vp, vp, vp, ci, ci, i64, i64, i64, vp])
+    L.bd_paged_plan.restype = ci
+    L.bd_paged_plan.argtypes = [vp, vp, vp, ci, ci, i64, vp, ci, vp, ci, ci, ci, ci, vp, vp, vp, vp, vp, vp]
+    L.bd_attn_paged_decode_fwd.restype = ci
+    L.bd_attn_paged_decode_fwd.argtypes = [vp] * 7 + [ci] * 8 + [i64] * 4 + [cf, ci, vp, vp, vp, sz, vp]
+    L.bd_attn_paged_decode_workspace_bytes.restype = sz
+    L.bd_attn_paged_decode_workspace_bytes.argtypes = [ci] * 8
     L.bd_attn_stage_names.restype = ctypes.c_char_p
     L.bd_attn_stage_names.argtypes = [ci, ci]
     L.bd_attn_workspace_bytes.restype = sz

@@ -161,6 +161,141 @@ int validate_lce(int N, int V, int Dm, int dtype, bd::LceShape& s) {
   return BD_ATTN_OK;
 }
 
+// ---- strided arrays of head rows and of pages ----
+
+constexpr int64_t kMaxStride = (int64_t)1 << 40;  // elements: extents below stay far inside 64 bits
+
+struct Dim {
+  int64_t n, stride;
+};
+// Elements from the first to past the last one of rows of D values at the given
+// (non-negative) strides.
+int64_t extent(const Dim* d, int k, int D) {
+  int64_t e = D;
+  for (int i = 0; i < k; ++i) e += (d[i].n - 1) * d[i].stride;
+  return e;
+}
+// Do no two of those rows share an element?  (Sufficient: sorted by stride, each
+// stride spans all that lies below it.)
+bool rows_apart(const Dim* dims, int k, int D) {
+  Dim d[4];
+  for (int i = 0; i < k; ++i) {
+    int at = i;
+    for (; at > 0 && d[at - 1].stride > dims[i].stride; --at) d[at] = d[at - 1];
+    d[at] = dims[i];
+  }
+  int64_t span = D;
+  for (int i = 0; i < k; ++i) {
+    if (d[i].n <= 1) continue;
+    if (d[i].stride < span) return false;
+    span += (d[i].n - 1) * d[i].stride;
+  }
+  return true;
+}
+
+// Head rows of B x N tokens and H heads, and their strides (validated).
+struct Rows {
+  const void* p;
+  Dim d[3];
+  size_t esz;
+  int D;
+  Range range() const { return Range{p, (size_t)extent(d, 3, D) * esz}; }
+};
+bool make_rows(const void* p, const int64_t* st, int B, int N, int H, int D, size_t esz, Rows& r) {
+  for (int i = 0; i < 3; ++i)
+    if (st[i] < 0 || st[i] % 8 != 0 || st[i] > kMaxStride) return false;
+  r = Rows{p, {{B, st[0]}, {N, st[1]}, {H, st[2]}}, esz, D};
+  return p != nullptr && aligned(p, 16);
+}
+bd::HeadRows head_rows(const int64_t* st) { return bd::HeadRows{st[0], st[1], st[2]}; }
+
+// Two outputs apart: their ranges do not meet, or they are interleaved token by
+// token (views of one fused array).
+bool outputs_apart(const Rows& a, const Rows& b) {
+  if (!overlap(a.range(), b.range())) return true;
+  if ((uintptr_t)a.p > (uintptr_t)b.p) return outputs_apart(b, a);
+  const int64_t off = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p) / (int64_t)a.esz;
+  const int64_t wa = (a.d[2].n - 1) * a.d[2].stride + a.D, wb = (b.d[2].n - 1) * b.d[2].stride + b.D;
+  if (off < wa) return false;
+  for (int i = 0; i < 2; ++i)  // the same outer strides, each past both
+    if (a.d[i].n > 1 && (a.d[i].stride != b.d[i].stride || a.d[i].stride < off + wb)) return false;
+  return true;
+}
+
+// log2 of a page size, or -1 if it is none.
+int page_log(int page_size) {
+  for (int l = 4; l <= 15; ++l)
+    if (page_size == 1 << l) return l;
+  return -1;
+}
+// Pages of K and V (validated; the arrays' ranges in `k`, `v`).  write: rows of
+// both must be apart, also where K and V are interleaved.
+bool make_pages(const void* K, const void* V, int num, int page_size, int64_t sp, int64_t sh, int64_t sr, int Hkv, int D,
+                bool write, bd::PageLayout& g, Range& k, Range& v) {
+  g = bd::PageLayout{num, page_log(page_size), sp, sh, sr};
+  if (num < 1 || g.log_size < 0 || (int64_t)num << g.log_size > INT32_MAX) return false;
+  for (const int64_t st : {sp, sh, sr})
+    if (st < 0 || st % 8 != 0 || st > kMaxStride) return false;
+  if (!K || !V || !aligned(K, 16) || !aligned(V, 16)) return false;
+  Dim d[4] = {{num, sp}, {Hkv, sh}, {page_size, sr}, {2, 0}};
+  const size_t n = (size_t)extent(d, 3, D) * 2;
+  k = Range{K, n};
+  v = Range{V, n};
+  if (!write) return true;
+  if (!rows_apart(d, 3, D)) return false;
+  if (overlap(k, v)) {  // interleaved: K or V as one more dimension
+    const uintptr_t a = (uintptr_t)K, b = (uintptr_t)V;
+    d[3].stride = (int64_t)((a < b ? b - a : a - b) / 2);
+    return rows_apart(d, 4, D);
+  }
+  return true;
+}
+
+// Validation common to the calls of the norm with the rotary embedding.
+int validate_rope(const float* rope, int n_rope, const int32_t* pos, int64_t pos_stride, int B, int N, int Hq, int Hkv,
+                  int D, float eps, int dtype, int wdtype, bd::RopeShape& s) {
+  // (a launch counts its threads, at most 8 a token and run of heads, in 32 bits)
+  if (B < 0 || N < 0 || (int64_t)B * N > (1 << 28) || Hq < 1 || Hkv < 1 || Hq > (1 << 14) || Hkv > (1 << 14))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (!(eps >= 0.f) || std::isinf(eps) || n_rope < 1 || pos_stride < 0) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (D != 64 && D != 128) return BD_ATTN_ERR_UNSUPPORTED;
+  if (dtype != BD_ATTN_BF16 && dtype != BD_ATTN_FP32) return BD_ATTN_ERR_UNSUPPORTED;
+  if (wdtype != BD_ATTN_FP32 && wdtype != dtype) return BD_ATTN_ERR_UNSUPPORTED;
+  s = bd::RopeShape{};
+  s.B = B;
+  s.N = N;
+  s.Hq = Hq;
+  s.Hkv = Hkv;
+  s.D = D;
+  s.eps = eps;
+  s.rope = rope;
+  s.n_rope = n_rope;
+  s.pos = pos;
+  s.pos_stride = pos_stride;
+  s.f32 = dtype == BD_ATTN_FP32;
+  s.w32 = wdtype == BD_ATTN_FP32;
+  return BD_ATTN_OK;
+}
+// Pointers and ranges of the inputs they share: table, positions, weights.
+bool rope_inputs(const bd::RopeShape& s, const void* wq, const void* wk, Range* in) {
+  if (!s.rope || !s.pos || !wq || !wk || !aligned(s.rope, 16) || !aligned(s.pos, 4) || !aligned(wq, 16) || !aligned(wk, 16))
+    return false;
+  const size_t wn = (size_t)s.D * (s.w32 ? 4 : 2);
+  in[0] = Range{s.rope, (size_t)s.n_rope * s.D * 4};
+  in[1] = Range{s.pos, ((size_t)(s.B - 1) * s.pos_stride + s.N) * 4};
+  in[2] = Range{wq, wn};
+  in[3] = Range{wk, wn};
+  return true;
+}
+
+// Validation of a decode call over pages; fills the resolved shape.
+int validate_paged(int B, int S, int Hq, int Hkv, int D, int page_size, int max_pages, float scale, int dtype,
+                   bd::DecodeShape& s) {
+  const int lg = page_log(page_size);
+  if (lg < 0 || max_pages < 1 || (int64_t)max_pages << lg > (1 << 22)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  return validate_decode(B, S, Hq, Hkv, D, max_pages << lg, scale, dtype, s);
+}
+
 #define BD_TRY(expr)                                    \
   do {                                                  \
     if ((expr) != hipSuccess) return BD_ATTN_ERR_HIP;   \
@@ -590,6 +725,225 @@ int bd_lce_objective(const float* logp, const float* logp_old, const float* logp
                  hipSuccess
              ? BD_ATTN_OK
              : BD_ATTN_ERR_HIP;
+}
+
+int bd_rope_table(const double* inv_freq, int n, int D, float* table, hipStream_t stream) {
+  if (n < 1 || n > (1 << 25)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (D != 64 && D != 128) return BD_ATTN_ERR_UNSUPPORTED;
+  if (!inv_freq || !table || !aligned(inv_freq, 8) || !aligned(table, 16)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (overlap(Range{inv_freq, (size_t)D * 4}, Range{table, (size_t)n * D * 4})) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  (void)hipGetLastError();
+  return bd::launch_rope_table(inv_freq, n, D, table, stream) == hipSuccess ? BD_ATTN_OK : BD_ATTN_ERR_HIP;
+}
+
+int bd_qk_norm_rope_fwd(const void* Q, const void* K, const void* V, const int64_t* strides, const void* q_weight,
+                        const void* k_weight, const float* rope, int n_rope, const int32_t* positions,
+                        int64_t pos_stride, int B, int N, int Hq, int Hkv, int D, float eps, int dtype, int wdtype,
+                        void* Qo, void* Ko, void* Vo, hipStream_t stream) {
+  bd::RopeShape s;
+  const int st = validate_rope(rope, n_rope, positions, pos_stride, B, N, Hq, Hkv, D, eps, dtype, wdtype, s);
+  if (st != BD_ATTN_OK) return st;
+  if (B == 0 || N == 0) return BD_ATTN_OK;
+  const size_t esz = s.f32 ? 4 : 2;
+  const void* src[] = {Q, K, V};
+  void* dst[] = {Qo, Ko, Vo};
+  Range in[7], out[3];
+  if (!strides || !rope_inputs(s, q_weight, k_weight, in)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  for (int i = 0; i < 3; ++i) {
+    const int H = i == 0 ? Hq : Hkv;
+    Rows r;
+    if (!make_rows(src[i], strides + 3 * i, B, N, H, D, esz, r) || !dst[i] || !aligned(dst[i], 16))
+      return BD_ATTN_ERR_INVALID_ARGUMENT;
+    in[4 + i] = r.range();
+    out[i] = Range{dst[i], (size_t)B * H * N * D * esz};
+  }
+  for (const Range& o : out)
+    for (const Range& i : in)
+      if (overlap(o, i)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (overlap(out[0], out[1]) || overlap(out[0], out[2]) || overlap(out[1], out[2])) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  const bd::RopeFwdArgs a{Q,  K,  V,  head_rows(strides), head_rows(strides + 3), head_rows(strides + 6), q_weight, k_weight,
+                          Qo, Ko, Vo, nullptr};
+  (void)hipGetLastError();
+  return bd::launch_rope_fwd(s, a, false, stream) == hipSuccess ? BD_ATTN_OK : BD_ATTN_ERR_HIP;
+}
+
+size_t bd_qk_norm_rope_workspace_bytes(int B, int N, int Hq, int Hkv, int D, int dtype) {
+  bd::RopeShape s;
+  if (validate_rope(nullptr, 1, nullptr, 0, B, N, Hq, Hkv, D, 0.f, dtype, dtype, s) != BD_ATTN_OK) return 0;
+  return B == 0 || N == 0 ? 0 : bd::rope_bwd_workspace_bytes(s);
+}
+
+int bd_qk_norm_rope_bwd(const void* dQo, const void* dKo, const void* dVo, const void* Q, const void* K,
+                        const int64_t* strides, const void* q_weight, const void* k_weight, const float* rope,
+                        int n_rope, const int32_t* positions, int64_t pos_stride, int B, int N, int Hq, int Hkv,
+                        int D, float eps, int dtype, int wdtype, void* dQ, void* dK, void* dV,
+                        const int64_t* grad_strides, void* dq_weight, void* dk_weight, void* ws, size_t ws_bytes,
+                        hipStream_t stream) {
+  bd::RopeShape s;
+  const int st = validate_rope(rope, n_rope, positions, pos_stride, B, N, Hq, Hkv, D, eps, dtype, wdtype, s);
+  if (st != BD_ATTN_OK) return st;
+  if (!dq_weight || !dk_weight || !aligned(dq_weight, 16) || !aligned(dk_weight, 16)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  const Range dw[] = {{dq_weight, (size_t)D * (s.w32 ? 4 : 2)}, {dk_weight, (size_t)D * (s.w32 ? 4 : 2)}};
+  if (overlap(dw[0], dw[1])) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  bd::RopeBwdArgs a{};
+  a.dwq = dq_weight;
+  a.dwk = dk_weight;
+  if (B > 0 && N > 0) {
+    const size_t esz = s.f32 ? 4 : 2, need = bd::rope_bwd_workspace_bytes(s);
+    const void *dy[] = {dQo, dKo, dVo}, *x[] = {Q, K};
+    const void* dst[] = {dQ, dK, dV};
+    Range in[9];
+    Rows out[3];
+    if (!strides || !grad_strides || !rope_inputs(s, q_weight, k_weight, in) || !ws || !aligned(ws, 16))
+      return BD_ATTN_ERR_INVALID_ARGUMENT;
+    for (int i = 0; i < 3; ++i) {
+      const int H = i == 0 ? Hq : Hkv;
+      if (!dy[i] || !aligned(dy[i], 16)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+      in[4 + i] = Range{dy[i], (size_t)B * H * N * D * esz};
+      Rows r;
+      if (i < 2) {
+        if (!make_rows(x[i], strides + 3 * i, B, N, H, D, esz, r)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+        in[7 + i] = r.range();
+      }
+      if (!make_rows(dst[i], grad_strides + 3 * i, B, N, H, D, esz, out[i]) || !rows_apart(out[i].d, 3, D))
+        return BD_ATTN_ERR_INVALID_ARGUMENT;
+    }
+    if (ws_bytes < need) return BD_ATTN_ERR_WORKSPACE_TOO_SMALL;
+    const Range o[] = {out[0].range(), out[1].range(), out[2].range(), dw[0], dw[1], {ws, need}};
+    for (int u = 0; u < 6; ++u) {
+      for (const Range& i : in)
+        if (overlap(o[u], i)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+      for (int v = u + 1; v < 6; ++v)
+        if (v < 3 ? !outputs_apart(out[u], out[v]) : overlap(o[u], o[v])) return BD_ATTN_ERR_INVALID_ARGUMENT;
+    }
+    a = bd::RopeBwdArgs{dQo, dKo, dVo, Q, K, head_rows(strides), head_rows(strides + 3), q_weight, k_weight, dQ, dK, dV,
+                        head_rows(grad_strides), head_rows(grad_strides + 3), head_rows(grad_strides + 6),
+                        static_cast<float*>(ws), dq_weight, dk_weight};
+  }
+  (void)hipGetLastError();
+  return bd::launch_rope_bwd(s, a, stream) == hipSuccess ? BD_ATTN_OK : BD_ATTN_ERR_HIP;
+}
+
+int bd_qk_norm_rope_paged(const void* Q, const void* K, const void* V, const int64_t* strides, const void* q_weight,
+                          const void* k_weight, const float* rope, int n_rope, const int32_t* positions,
+                          int64_t pos_stride, const int32_t* slots, int B, int N, int Hq, int Hkv, int D, float eps,
+                          int dtype, int wdtype, void* Qo, void* K_pages, void* V_pages, int num_pages, int page_size,
+                          int64_t page_stride, int64_t head_stride, int64_t row_stride, hipStream_t stream) {
+  bd::RopeShape s;
+  const int st = validate_rope(rope, n_rope, positions, pos_stride, B, N, Hq, Hkv, D, eps, dtype, wdtype, s);
+  if (st != BD_ATTN_OK) return st;
+  if (dtype != BD_ATTN_BF16) return BD_ATTN_ERR_UNSUPPORTED;
+  Range pages[2];
+  if (!make_pages(K_pages, V_pages, num_pages, page_size, page_stride, head_stride, row_stride, Hkv, D, true, s.pages,
+                  pages[0], pages[1]))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (B == 0 || N == 0) return BD_ATTN_OK;
+  const void* src[] = {Q, K, V};
+  Range in[8];
+  if (!strides || !rope_inputs(s, q_weight, k_weight, in) || !slots || !aligned(slots, 4) || !Qo || !aligned(Qo, 16))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  in[4] = Range{slots, (size_t)B * N * 4};
+  for (int i = 0; i < 3; ++i) {
+    Rows r;
+    if (!make_rows(src[i], strides + 3 * i, B, N, i == 0 ? Hq : Hkv, D, 2, r)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+    in[5 + i] = r.range();
+  }
+  const Range out[] = {{Qo, (size_t)B * Hq * N * D * 2}, pages[0], pages[1]};
+  for (const Range& o : out)
+    for (const Range& i : in)
+      if (overlap(o, i)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (overlap(out[0], out[1]) || overlap(out[0], out[2])) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  const bd::RopeFwdArgs a{Q,  K,       V,       head_rows(strides), head_rows(strides + 3), head_rows(strides + 6),
+                          q_weight, k_weight, Qo, K_pages, V_pages, slots};
+  (void)hipGetLastError();
+  return bd::launch_rope_fwd(s, a, true, stream) == hipSuccess ? BD_ATTN_OK : BD_ATTN_ERR_HIP;
+}
+
+int bd_paged_plan(const int32_t* cache_lens, const int32_t* new_lens, int32_t* page_table, int B, int max_pages,
+                  int64_t table_stride, const int32_t* free_pages, int n_free, const int32_t* free_head,
+                  int num_pages, int page_size, int S, int total, int32_t* lens, int32_t* cu, int32_t* slots,
+                  int32_t* positions, int32_t* state, hipStream_t stream) {
+  const int lg = page_log(page_size);
+  if (B < 1 || B > (1 << 16) || max_pages < 1 || lg < 0 || (int64_t)max_pages << lg > (1 << 30) || num_pages < 1 ||
+      (int64_t)num_pages << lg > INT32_MAX || n_free < 0 || S < 0 || (int64_t)B * S > (1 << 30) ||
+      table_stride < max_pages || table_stride > kMaxStride)
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  const int T = S > 0 ? B * S : total;
+  if (T < 0 || T > (1 << 30)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (!cache_lens || !new_lens || !page_table || (n_free > 0 && !free_pages) || !free_head || !lens || !cu || !state ||
+      (T > 0 && (!slots || !positions)))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  const Range in[] = {{cache_lens, (size_t)B * 4}, {new_lens, (size_t)B * 4}, {free_pages, (size_t)n_free * 4},
+                      {free_head, 4}};
+  const Range out[] = {{page_table, ((size_t)(B - 1) * table_stride + max_pages) * 4},
+                       {lens, (size_t)B * 4}, {cu, (size_t)(B + 1) * 4}, {slots, (size_t)T * 4},
+                       {positions, (size_t)T * 4}, {state, 8}};
+  for (const Range& i : in)
+    if (!aligned(i.p, 4)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  for (int u = 0; u < 6; ++u) {
+    if (!aligned(out[u].p, 4)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+    for (const Range& i : in)
+      if (overlap(out[u], i)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+    for (int v = u + 1; v < 6; ++v)
+      if (overlap(out[u], out[v])) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  }
+  const bd::PlanArgs a{cache_lens, new_lens, page_table, B, max_pages, table_stride, free_pages, n_free, free_head,
+                       num_pages, lg, S, T, lens, cu, slots, positions, state};
+  (void)hipGetLastError();
+  return bd::launch_plan(a, stream) == hipSuccess ? BD_ATTN_OK : BD_ATTN_ERR_HIP;
+}
+
+size_t bd_attn_paged_decode_workspace_bytes(int B, int S, int Hq, int Hkv, int D, int page_size, int max_pages,
+                                            int dtype) {
+  bd::DecodeShape s;
+  if (validate_paged(B, S, Hq, Hkv, D, page_size, max_pages, 0.f, dtype, s) != BD_ATTN_OK) return 0;
+  return bd::decode_workspace_bytes(s);
+}
+
+int bd_attn_paged_decode_fwd(const void* Q, const void* K_pages, const void* V_pages, const int32_t* page_table,
+                             const int32_t* cache_lens, const void* K_new, const void* V_new, int B, int S, int Hq,
+                             int Hkv, int D, int num_pages, int page_size, int max_pages, int64_t table_stride,
+                             int64_t page_stride, int64_t head_stride, int64_t row_stride, float scale, int dtype,
+                             void* O, float* LSE, void* ws, size_t ws_bytes, hipStream_t stream) {
+  bd::DecodeShape s;
+  const int st = validate_paged(B, S, Hq, Hkv, D, page_size, max_pages, scale, dtype, s);
+  if (st != BD_ATTN_OK) return st;
+  bd::PagedArgs a{};
+  Range pages[2];
+  if (!make_pages(K_pages, V_pages, num_pages, page_size, page_stride, head_stride, row_stride, Hkv, D, false, a.pages,
+                  pages[0], pages[1]) ||
+      row_stride < D || row_stride > (1 << 20) || table_stride < 0 || table_stride > kMaxStride ||
+      (B > 1 && table_stride != 0 && table_stride < max_pages))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  const size_t need = bd::decode_workspace_bytes(s);
+  if (!Q || !page_table || !cache_lens || !O || !LSE || !ws || (K_new == nullptr) != (V_new == nullptr))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (!aligned(Q, 16) || !aligned(page_table, 4) || !aligned(cache_lens, 4) || !aligned(K_new, 16) ||
+      !aligned(V_new, 16) || !aligned(O, 16) || !aligned(LSE, 4) || !aligned(ws, 16))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (ws_bytes < need) return BD_ATTN_ERR_WORKSPACE_TOO_SMALL;
+  const size_t nq = (size_t)B * Hq * S, nkn = K_new ? (size_t)B * Hkv * S * D * 2 : 0;
+  const Range in[] = {{Q, nq * D * 2}, pages[0], pages[1], {page_table, ((size_t)(B - 1) * table_stride + max_pages) * 4},
+                      {cache_lens, (size_t)B * 4}, {K_new, nkn}, {V_new, nkn}};
+  const Range out[] = {{O, nq * D * 2}, {LSE, nq * 4}, {ws, need}};
+  for (const Range& o : out)
+    for (const Range& i : in)
+      if (i.p && overlap(o, i)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (overlap(out[0], out[1]) || overlap(out[0], out[2]) || overlap(out[1], out[2]))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  a.Q = Q;
+  a.Kp = K_pages;
+  a.Vp = V_pages;
+  a.table = page_table;
+  a.width = max_pages;
+  a.table_stride = table_stride;
+  a.cache_lens = cache_lens;
+  a.Kn = K_new;
+  a.Vn = V_new;
+  a.O = O;
+  a.LSE = LSE;
+  (void)hipGetLastError();
+  return bd::launch_paged_decode(s, a, ws, stream) == hipSuccess ? BD_ATTN_OK : BD_ATTN_ERR_HIP;
 }
 
 const char* bd_attn_stage_names(int for_bwd, int dtype) {

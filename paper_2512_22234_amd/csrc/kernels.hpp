@@ -272,4 +272,87 @@ hipError_t launch_lce_objective(int N, int kind, float eps, float beta, const fl
                                 const float* logp_ref, const float* adv, const float* weight, float* loss,
                                 float* dlogp, hipStream_t st);
 
+// Strides (in elements) of head rows x[b][n][h][0..D).
+struct HeadRows {
+  int64_t sb, sn, sh;
+};
+
+// Pages of a KV cache: row r of KV head h of page g starts at element
+// g * sp + h * sh + r * sr of the K and of the V array; num pages of
+// 2^log_size rows.
+struct PageLayout {
+  int num, log_size;
+  int64_t sp, sh, sr;
+};
+
+// Norms of queries and keys with the rotary embedding: B x N tokens of Hq
+// query, Hkv key and Hkv value heads of D.
+struct RopeShape {
+  int B, N, Hq, Hkv, D;
+  float eps;
+  const float* rope;  // [n_rope][D]: cos, sin of each position's angles
+  int n_rope;
+  const int* pos;  // position of token (b, n): pos[b * pos_stride + n]
+  int64_t pos_stride;
+  bool f32, w32;     // float32 rows (else bf16), float32 weights
+  PageLayout pages;  // paged form: where keys and values go
+  int hpb;           // heads a workgroup takes (set by the launcher)
+};
+struct RopeFwdArgs {
+  const void *q, *k, *v;
+  HeadRows sq, sk, sv;
+  const void *wq, *wk;
+  void *qo, *ko, *vo;  // [B][H][N][D]; paged form: ko, vo are the pages
+  const int* slots;    // paged form: row of the pages of token b * N + n (negative: none)
+};
+struct RopeBwdArgs {
+  const void *dqo, *dko, *dvo;  // [B][H][N][D]
+  const void *q, *k;
+  HeadRows sq, sk;
+  const void *wq, *wk;
+  void *dq, *dk, *dv;
+  HeadRows gq, gk, gv;
+  float* part;  // sums of g n per workgroup (rope_bwd_workspace_bytes)
+  void *dwq, *dwk;
+};
+// Workgroups along the tokens: 256 / (D / 16) rows each.
+inline int rope_token_blocks(const RopeShape& s) {
+  const int rpb = 256 / (s.D / 16);
+  return (int)(((long long)s.B * s.N + rpb - 1) / rpb);
+}
+size_t rope_bwd_workspace_bytes(const RopeShape& s);
+hipError_t launch_rope_fwd(const RopeShape& s, const RopeFwdArgs& a, bool paged, hipStream_t st);
+hipError_t launch_rope_bwd(const RopeShape& s, const RopeBwdArgs& a, hipStream_t st);
+hipError_t launch_rope_table(const double* inv_freq, int n, int D, float* table, hipStream_t st);
+
+// Pages and slots for the next tokens of B sequences.
+struct PlanArgs {
+  const int *lens, *fresh;  // [B]: cached tokens, new tokens
+  int* table;               // [B][width], rows table_stride apart
+  int B, width;
+  int64_t table_stride;
+  const int* free_pages;  // [n_free]
+  int n_free;
+  const int* free_head;
+  int num_pages, log_size;
+  int S, T;  // S > 0: rows of S tokens a sequence (T = B * S); S = 0: T tokens, packed
+  int *lens_out, *cu, *slots, *positions, *state;
+};
+hipError_t launch_plan(const PlanArgs& a, hipStream_t st);
+
+// Decoding over a paged cache: DecodeShape with C = width * page size (S new
+// keys if block, else none), and where the pages are.
+struct PagedArgs {
+  const void *Q, *Kp, *Vp;
+  const int* table;  // [B][width], rows table_stride apart
+  int width;
+  int64_t table_stride;
+  PageLayout pages;
+  const int* cache_lens;
+  const void *Kn, *Vn;  // null: the queries see the cache alone
+  void* O;
+  float* LSE;
+};
+hipError_t launch_paged_decode(const DecodeShape& s, const PagedArgs& a, void* ws, hipStream_t st);
+
 }  // namespace bd

@@ -1,0 +1,373 @@
+// Norms of queries and keys for each head with the rotary embedding, in one
+// pass from the projections' layout into the attention's, for gfx950.
+//
+// For a head row x of D values at position p, with the norm's weight w:
+//   r = (mean(x^2) + eps)^(-1/2),   n = x r,   y = w n
+//   out1 = y1 c - y2 s,   out2 = y2 c + y1 s        (halves 1, 2 of the head)
+// where c, s are row p of the table (cos and sin of p f_j).  Values are only
+// laid out.  The backward, for gradients d of the outputs, recomputes r from x:
+//   g1 = d1 c + d2 s,   g2 = d2 c - d1 s            (the rotation's inverse)
+//   dw = sum over rows of g n,   h = g w,   dx = r (h - n mean(h n)).
+// Float32 throughout; each result is rounded once, when it is stored.
+//
+// Projections are token-major (any batch, token and head strides), outputs
+// head-major [B][H][N][D]: the pass is the transposition that the attention
+// needs anyway, and is bound by HBM.  A lane holds the same 8 values of both
+// halves of a row (16-byte accesses, pairs of the rotation in one lane), D / 16
+// lanes a row; a workgroup takes 256 / (D / 16) consecutive tokens, whose cos
+// and sin stay in registers, and a run of heads of one kind (q, k or v).
+#include "device.hpp"
+#include "kernels.hpp"
+
+namespace bd {
+namespace {
+
+constexpr int ROPE_NT = 256;
+// Lanes of a row, and rows (tokens) of a workgroup.
+template <int D>
+constexpr int ROPE_LPR = D / 16;
+template <int D>
+constexpr int ROPE_RPB = ROPE_NT / ROPE_LPR<D>;
+
+__device__ inline void ld8(const bf16* p, float* x) {
+  const bf16x8 v = *reinterpret_cast<const bf16x8*>(p);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+}
+__device__ inline void ld8(const float* p, float* x) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[e] = a[e];
+    x[e + 4] = b[e];
+  }
+}
+__device__ inline void st8(bf16* p, const float* x) {
+  bf16x8 v;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = (bf16)x[e];
+  *reinterpret_cast<bf16x8*>(p) = v;
+}
+__device__ inline void st8(float* p, const float* x) {
+  *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
+  *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+}
+
+// Sum over the 4 or 8 consecutive lanes of a row.
+template <int LPR>
+__device__ inline float row_sum(float x) {
+  x += __shfl_xor(x, 1);
+  x += __shfl_xor(x, 2);
+  if constexpr (LPR == 8) x += __shfl_xor(x, 4);
+  return x;
+}
+
+// What a workgroup works on: heads [h0, h1) of a kind (0: q, 1: k, 2: v).  The
+// grid's second index counts runs of hpb heads, those of q first, then k, then v.
+struct HeadRun {
+  int kind, h0, h1, part;  // part: the run among those of its kind
+};
+__device__ inline HeadRun head_run(const RopeShape& s, int y) {
+  const int cq = cdiv(s.Hq, s.hpb), ck = cdiv(s.Hkv, s.hpb);
+  HeadRun r;
+  r.kind = y < cq ? 0 : y < cq + ck ? 1 : 2;
+  r.part = y - (r.kind == 0 ? 0 : r.kind == 1 ? cq : cq + ck);
+  r.h0 = r.part * s.hpb;
+  r.h1 = imin(r.h0 + s.hpb, r.kind == 0 ? s.Hq : s.Hkv);
+  return r;
+}
+
+// A lane's token: row t of the B*N (the last one again past the end, not stored).
+struct Token {
+  bool valid;
+  int t, b, n;
+};
+template <int D>
+__device__ inline Token lane_token(const RopeShape& s, int x) {
+  const unsigned rows = (unsigned)s.B * (unsigned)s.N;
+  const unsigned t = (unsigned)x * ROPE_RPB<D> + threadIdx.x / ROPE_LPR<D>;
+  Token k;
+  k.valid = t < rows;
+  k.t = (int)(k.valid ? t : rows - 1);
+  k.b = (int)((unsigned)k.t / (unsigned)s.N);
+  k.n = k.t - k.b * s.N;
+  return k;
+}
+// cos and sin of this lane's 8 pairs at its token's position (clamped to the table).
+template <int D>
+__device__ inline void lane_angles(const RopeShape& s, const Token& k, int i, float* c, float* sn) {
+  const int p = imin(imax(s.pos[(size_t)k.b * s.pos_stride + k.n], 0), s.n_rope - 1);
+  const float* row = s.rope + (size_t)p * D + 8 * i;
+  ld8(row, c);
+  ld8(row + D / 2, sn);
+}
+
+template <typename T, typename W, int D, bool PAGED>
+__global__ __launch_bounds__(ROPE_NT) void rope_fwd_kernel(RopeShape s, RopeFwdArgs a) {
+  constexpr int LPR = ROPE_LPR<D>;
+  const int i = threadIdx.x % LPR;
+  const HeadRun run = head_run(s, blockIdx.y);
+  const Token k = lane_token<D>(s, blockIdx.x);
+  const int H = run.kind == 0 ? s.Hq : s.Hkv;
+  const HeadRows in = run.kind == 0 ? a.sq : run.kind == 1 ? a.sk : a.sv;
+  const T* src = static_cast<const T*>(run.kind == 0 ? a.q : run.kind == 1 ? a.k : a.v) + k.b * in.sb + k.n * in.sn + 8 * i;
+  // where the rows go: [B][H][N][D], or the token's slot of the pages
+  T* dst;
+  int64_t dst_h;
+  bool store = k.valid;
+  if (PAGED && run.kind != 0) {
+    const int slot = a.slots[k.t];
+    const int page = slot >> s.pages.log_size;
+    store = store && slot >= 0 && page < s.pages.num;
+    dst = static_cast<T*>(run.kind == 1 ? a.ko : a.vo) +
+          (store ? page * s.pages.sp + (slot & ((1 << s.pages.log_size) - 1)) * s.pages.sr : 0) + 8 * i;
+    dst_h = s.pages.sh;
+  } else {
+    dst = static_cast<T*>(run.kind == 0 ? a.qo : run.kind == 1 ? a.ko : a.vo) + ((size_t)k.b * H * s.N + k.n) * D + 8 * i;
+    dst_h = (int64_t)s.N * D;
+  }
+  if (run.kind == 2) {
+    for (int h = run.h0; h < run.h1; ++h) {
+      float x1[8], x2[8];
+      ld8(src + h * in.sh, x1);
+      ld8(src + h * in.sh + D / 2, x2);
+      if (store) {
+        st8(dst + h * dst_h, x1);
+        st8(dst + h * dst_h + D / 2, x2);
+      }
+    }
+    return;
+  }
+  float c[8], sn[8], w1[8], w2[8];
+  lane_angles<D>(s, k, i, c, sn);
+  const W* w = static_cast<const W*>(run.kind == 0 ? a.wq : a.wk) + 8 * i;
+  ld8(w, w1);
+  ld8(w + D / 2, w2);
+  for (int h = run.h0; h < run.h1; ++h) {
+    float x1[8], x2[8];
+    ld8(src + h * in.sh, x1);
+    ld8(src + h * in.sh + D / 2, x2);
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss += x1[e] * x1[e] + x2[e] * x2[e];
+    const float r = rsqrtf(row_sum<LPR>(ss) * (1.f / D) + s.eps);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float y1 = x1[e] * r * w1[e], y2 = x2[e] * r * w2[e];
+      x1[e] = y1 * c[e] - y2 * sn[e];
+      x2[e] = y2 * c[e] + y1 * sn[e];
+    }
+    if (store) {
+      st8(dst + h * dst_h, x1);
+      st8(dst + h * dst_h + D / 2, x2);
+    }
+  }
+}
+
+// The gradients of the projections, and of each workgroup's rows the sums g n
+// per weight (`part`: [workgroup of a kind][D], those of q first).
+template <typename T, typename W, int D>
+__global__ __launch_bounds__(ROPE_NT) void rope_bwd_kernel(RopeShape s, RopeBwdArgs a) {
+  constexpr int LPR = ROPE_LPR<D>;
+  __shared__ float sums[ROPE_NT / 64][D];
+  const int i = threadIdx.x % LPR;
+  const HeadRun run = head_run(s, blockIdx.y);
+  const Token k = lane_token<D>(s, blockIdx.x);
+  const int H = run.kind == 0 ? s.Hq : s.Hkv;
+  const HeadRows gs = run.kind == 0 ? a.gq : run.kind == 1 ? a.gk : a.gv;
+  const T* dy = static_cast<const T*>(run.kind == 0 ? a.dqo : run.kind == 1 ? a.dko : a.dvo) +
+                ((size_t)k.b * H * s.N + k.n) * D + 8 * i;
+  const int64_t dy_h = (int64_t)s.N * D;
+  T* dst = static_cast<T*>(run.kind == 0 ? a.dq : run.kind == 1 ? a.dk : a.dv) + k.b * gs.sb + k.n * gs.sn + 8 * i;
+  if (run.kind == 2) {
+    for (int h = run.h0; h < run.h1; ++h) {
+      float x1[8], x2[8];
+      ld8(dy + h * dy_h, x1);
+      ld8(dy + h * dy_h + D / 2, x2);
+      if (k.valid) {
+        st8(dst + h * gs.sh, x1);
+        st8(dst + h * gs.sh + D / 2, x2);
+      }
+    }
+    return;
+  }
+  const HeadRows in = run.kind == 0 ? a.sq : a.sk;
+  const T* src = static_cast<const T*>(run.kind == 0 ? a.q : a.k) + k.b * in.sb + k.n * in.sn + 8 * i;
+  float c[8], sn[8], w1[8], w2[8], a1[8], a2[8];
+  lane_angles<D>(s, k, i, c, sn);
+  const W* w = static_cast<const W*>(run.kind == 0 ? a.wq : a.wk) + 8 * i;
+  ld8(w, w1);
+  ld8(w + D / 2, w2);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) a1[e] = a2[e] = 0.f;
+  for (int h = run.h0; h < run.h1; ++h) {
+    float x1[8], x2[8], d1[8], d2[8];
+    ld8(src + h * in.sh, x1);
+    ld8(src + h * in.sh + D / 2, x2);
+    ld8(dy + h * dy_h, d1);
+    ld8(dy + h * dy_h + D / 2, d2);
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss += x1[e] * x1[e] + x2[e] * x2[e];
+    const float r = rsqrtf(row_sum<LPR>(ss) * (1.f / D) + s.eps);
+    float hn = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float g1 = d1[e] * c[e] + d2[e] * sn[e], g2 = d2[e] * c[e] - d1[e] * sn[e];
+      x1[e] *= r;
+      x2[e] *= r;
+      if (k.valid) {
+        a1[e] += g1 * x1[e];
+        a2[e] += g2 * x2[e];
+      }
+      d1[e] = g1 * w1[e];
+      d2[e] = g2 * w2[e];
+      hn += d1[e] * x1[e] + d2[e] * x2[e];
+    }
+    const float m = row_sum<LPR>(hn) * (1.f / D);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      d1[e] = r * (d1[e] - x1[e] * m);
+      d2[e] = r * (d2[e] - x2[e] * m);
+    }
+    if (k.valid) {
+      st8(dst + h * gs.sh, d1);
+      st8(dst + h * gs.sh + D / 2, d2);
+    }
+  }
+  // sums over the workgroup's rows, in a fixed order
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int o = LPR; o < 64; o <<= 1) {
+      a1[e] += __shfl_xor(a1[e], o);
+      a2[e] += __shfl_xor(a2[e], o);
+    }
+  if (lane < LPR) {
+    st8(&sums[wave][8 * i], a1);
+    st8(&sums[wave][8 * i + D / 2], a2);
+  }
+  __syncthreads();
+  if (threadIdx.x < D) {
+    float v = 0.f;
+#pragma unroll
+    for (int u = 0; u < ROPE_NT / 64; ++u) v += sums[u][threadIdx.x];
+    const int cq = cdiv(s.Hq, s.hpb), ck = cdiv(s.Hkv, s.hpb);
+    const size_t row = run.kind == 0 ? (size_t)blockIdx.x * cq + run.part
+                                     : (size_t)gridDim.x * cq + (size_t)blockIdx.x * ck + run.part;
+    a.part[row * D + threadIdx.x] = v;
+  }
+}
+
+// dw: column sums of the rows of `part` of each kind (blockIdx.y: 0 q, 1 k), 32
+// columns a workgroup, in a fixed order.
+template <typename W>
+__global__ __launch_bounds__(1024) void rope_dw_kernel(const float* part, int nq, int nk, int D, W* dwq, W* dwk) {
+  __shared__ float sums[32][33];
+  const int col = threadIdx.x & 31, r = threadIdx.x >> 5;
+  const int n = blockIdx.y == 0 ? nq : nk;
+  const float* p = part + (size_t)(blockIdx.y == 0 ? 0 : nq) * D + blockIdx.x * 32 + col;
+  float v = 0.f;
+#pragma unroll 8
+  for (int u = r; u < n; u += 32) v += p[(size_t)u * D];
+  sums[r][col] = v;
+  __syncthreads();
+  if (r == 0) {
+    v = 0.f;
+#pragma unroll
+    for (int u = 0; u < 32; ++u) v += sums[u][col];
+    (blockIdx.y == 0 ? dwq : dwk)[blockIdx.x * 32 + col] = (W)v;
+  }
+}
+
+// Row p of the table: cos(p f_j), then sin(p f_j), from angles in float64 (a
+// float32 angle is off by up to p 2^-24 rad).
+__global__ __launch_bounds__(256) void rope_table_kernel(const double* inv_freq, int n, int half, float* table) {
+  const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= (size_t)n * half) return;
+  const size_t p = at / half;
+  const int j = (int)(at - p * half);
+  double sn, c;
+  sincos((double)p * inv_freq[j], &sn, &c);
+  table[p * 2 * half + j] = (float)c;
+  table[p * 2 * half + half + j] = (float)sn;
+}
+
+// Heads a workgroup takes: up to 8, so that its tokens' cos and sin are read
+// once for all of them, but no more than leave 2048 workgroups.
+RopeShape with_runs(const RopeShape& shape) {
+  RopeShape s = shape;
+  const long long work = (long long)rope_token_blocks(s) * (s.Hq + 2 * s.Hkv);
+  s.hpb = (int)(work / 2048);
+  s.hpb = s.hpb < 1 ? 1 : s.hpb > 8 ? 8 : s.hpb;
+  return s;
+}
+dim3 rope_grid(const RopeShape& s) {
+  return dim3((unsigned)rope_token_blocks(s), (unsigned)(cdiv(s.Hq, s.hpb) + 2 * cdiv(s.Hkv, s.hpb)));
+}
+
+template <typename T, typename W, int D>
+hipError_t launch_rope_fwd_t(const RopeShape& s, const RopeFwdArgs& a, bool paged, hipStream_t st) {
+  if (paged) {
+    if constexpr (std::is_same_v<T, bf16>)
+      hipLaunchKernelGGL((rope_fwd_kernel<T, W, D, true>), rope_grid(s), dim3(ROPE_NT), 0, st, s, a);
+  } else {
+    hipLaunchKernelGGL((rope_fwd_kernel<T, W, D, false>), rope_grid(s), dim3(ROPE_NT), 0, st, s, a);
+  }
+  return hipGetLastError();
+}
+template <typename T, typename W, int D>
+hipError_t launch_rope_bwd_t(const RopeShape& s, const RopeBwdArgs& a, hipStream_t st) {
+  int nq = 0, nk = 0;
+  if (s.B > 0 && s.N > 0) {
+    hipLaunchKernelGGL((rope_bwd_kernel<T, W, D>), rope_grid(s), dim3(ROPE_NT), 0, st, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    nq = rope_token_blocks(s) * cdiv(s.Hq, s.hpb);
+    nk = rope_token_blocks(s) * cdiv(s.Hkv, s.hpb);
+  }
+  hipLaunchKernelGGL((rope_dw_kernel<W>), dim3(D / 32, 2), dim3(1024), 0, st, a.part, nq, nk, D,
+                     static_cast<W*>(a.dwq), static_cast<W*>(a.dwk));
+  return hipGetLastError();
+}
+
+// f(T, W, D) for the element type, the weights' type and the head size of s.
+template <typename F>
+hipError_t rope_dispatch(const RopeShape& s, F f) {
+  auto with_d = [&](auto t, auto w) {
+    return s.D == 128 ? f(t, w, std::integral_constant<int, 128>()) : f(t, w, std::integral_constant<int, 64>());
+  };
+  if (s.f32) return with_d(float(), float());
+  if (s.w32) return with_d(bf16(), float());
+  return with_d(bf16(), bf16());
+}
+
+}  // namespace
+
+size_t rope_bwd_workspace_bytes(const RopeShape& shape) {
+  const RopeShape s = with_runs(shape);
+  return (size_t)rope_token_blocks(s) * (cdiv(s.Hq, s.hpb) + cdiv(s.Hkv, s.hpb)) * s.D * 4;
+}
+
+hipError_t launch_rope_fwd(const RopeShape& shape, const RopeFwdArgs& a, bool paged, hipStream_t st) {
+  const RopeShape s = with_runs(shape);
+  return rope_dispatch(s, [&](auto t, auto w, auto d) {
+    return launch_rope_fwd_t<decltype(t), decltype(w), decltype(d)::value>(s, a, paged, st);
+  });
+}
+
+hipError_t launch_rope_bwd(const RopeShape& shape, const RopeBwdArgs& a, hipStream_t st) {
+  const RopeShape s = with_runs(shape);
+  return rope_dispatch(s, [&](auto t, auto w, auto d) {
+    return launch_rope_bwd_t<decltype(t), decltype(w), decltype(d)::value>(s, a, st);
+  });
+}
+
+hipError_t launch_rope_table(const double* inv_freq, int n, int D, float* table, hipStream_t st) {
+  const size_t work = (size_t)n * (D / 2);
+  hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)((work + 255) / 256)), dim3(256), 0, st, inv_freq, n, D / 2, table);
+  return hipGetLastError();
+}
+
+}  // namespace bd
