@@ -2,73 +2,496 @@
 // attend to the first cache_lens[b] keys of its pages (row b of the page table)
 // and, if given, to the block's own S keys.  A page outside the pool holds no
 // keys; a row that sees no key at all gets O = 0 and LSE = -inf.
-#include "device.hpp"
-#include "kernels.hpp"
+//
+// For each query row, over the keys j that it sees:
+//   s_j = scale q . k_j,   M = max_j s_j,   l = sum_j exp(s_j - M),
+//   O = sum_j exp(s_j - M) v_j / l,   LSE = M + log l.
+// Every cached K and V row is read once and serves all G*S query rows of its KV
+// head: 4 D bytes of HBM a key for 4 D G S flops, so the work is bound by HBM.
+//
+// The work is shared out as over a dense cache (decode.hip): the KT-key tiles of
+// all (sequence, KV head, row group) items end to end, in equal contiguous runs
+// over teams of TW waves, one per 32 query rows; a run that holds part of an
+// item leaves unnormalised sums, which a second kernel joins.  What differs:
+//   - A tile's rows lie in pages: each 16 rows (a page holds a multiple of 16)
+//     have a buffer descriptor of their own, which ends with the last valid row.
+//     A copy instruction fills 1 KiB of the tile (4 rows of 128, 8 of 64) from
+//     one of them, so pages cost scalar work only, whatever their size and
+//     strides.  The page ids of the next tile are read (scalar loads) while the
+//     current one is waited for.
+//   - Items have at least one tile, empty where there is no key, so that their
+//     rows are written.  Tiles without a key are not computed; 16-row pieces
+//     without one are masked.
+#include "decode.hpp"
 
 namespace bd {
 namespace {
 
 struct PagedParams {
-  PagedArgs a;
-  int B, S, Hq, Hkv, G;
-  float c;  // scale * log2(e)
+  DecParams d;  // Kc, Vc: the pages; C: the table's room in keys
+  int Sn;       // the block's own keys (0: none)
+  int table_width;
+  int64_t table_stride;
+  PageLayout pages;
 };
 
-// One wave per query row: the keys one after another, a lane holds D / 64
-// features, running maximum and sum of the softmax.
-template <int D>
-__global__ __launch_bounds__(64) void paged_row_kernel(PagedParams p) {
-  constexpr int E = D / 64;
-  const int lane = threadIdx.x;
-  const unsigned row = blockIdx.x;  // (b * Hq + h) * S + s
-  const int bh = (int)(row / (unsigned)p.S), b = bh / p.Hq, h = bh - b * p.Hq, hkv = h / p.G;
-  float q[E], o[E], m = -INFINITY, l = 0.f;
+// Key tiles of an item of a sequence with cache length len.
+template <int KT>
+__device__ inline int paged_tiles(const PagedParams& p, int len) {
+  return imax(cdiv(len, KT) + cdiv(p.Sn, KT), 1);
+}
+
+template <int D, int TW, int KT, int NST>
+struct PagedSmem {
+  static constexpr int TEAMS = TW == 1 ? 4 : 1;  // teams per workgroup
+  static constexpr int NW = TW * TEAMS;          // waves per workgroup
+  static constexpr uint32_t TILE = KT * D * 2;   // bytes of one swizzled K or V tile
+  alignas(256) char buf[TEAMS][NST * 2 * TILE];  // per team: a ring of K and V tiles
+  int wsum[NW];                                  // prologue: per-wave sums of the scan
+  int start_b[TEAMS], start_off[TEAMS];          // where each team's run starts
+};
+
+// Position of a tile: sequence b (cache length len, nt tiles per item), item
+// r of the sequence (KV head r / ng, row group r % ng), tile j of the item.
+struct PagedPos {
+  int b, len, nt, r, j;
+};
+
+// `lens` and `table` are the parameters' arrays as restrict kernel arguments, read
+// through the scalar cache where the index is uniform.
+template <int D, int TW, int KT, int NST>
+__global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(PagedParams p, const int* __restrict__ lens,
+                                                                           const int* __restrict__ table) {
+  constexpr int DS = D / 16, DB = D / 32, PST = D + 4, KB = KT / 32;
+  using Smem = PagedSmem<D, TW, KT, NST>;
+  constexpr int TEAMS = Smem::TEAMS, NW = Smem::NW, NT = 64 * NW;
+  constexpr int NP = KT / 16;  // 16-row pieces of a tile
+  static_assert(NP * NST <= 32, "pieces of the tiles in flight fit a word");
+  __shared__ Smem sm;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, g2 = lane >> 5;
+  const int tm = TW == 1 ? w : 0, tw = TW == 1 ? 0 : w;  // team of the workgroup, wave of the team
+  const int ng = TW < 4 ? 1 : p.d.ng;                    // (decode_groups: smaller teams hold all rows of a KV head)
+  const int I = p.d.Hkv * ng;                            // items per sequence
+
+  // ---- prologue: T, and the position of each team's first tile (as over a dense cache) ----
+  const int cpt = cdiv(p.d.B, NT);
+  const int c0 = imin(p.d.B, tid * cpt), c1 = imin(p.d.B, c0 + cpt);
+  int csum = 0;
+#pragma unroll 4
+  for (int b = c0; b < c1; ++b) csum += paged_tiles<KT>(p, dec_len(p.d, lens, b));
+  int incl = csum;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    q[e] = (float)static_cast<const bf16*>(p.a.Q)[(size_t)row * D + lane * E + e];
-    o[e] = 0.f;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += u;
   }
-  auto key = [&](const bf16* k, const bf16* v) {
-    float x = 0.f;
+  if (lane == 63) sm.wsum[w] = incl;
+  __syncthreads();
+  int before = 0, total = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) x += q[e] * (float)k[lane * E + e];
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
-    x *= p.c;
-    const float mn = fmaxf(m, x), al = m == mn ? 1.f : fast_exp2(m - mn), w = fast_exp2(x - mn);
-    l = l * al + w;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * al + w * (float)v[lane * E + e];
-    m = mn;
-  };
-  const PageLayout& g = p.a.pages;
-  const int len = imin(imax(p.a.cache_lens[b], 0), p.a.width << g.log_size);
-  for (int j = 0; j < len; ++j) {
-    const int id = p.a.table[b * p.a.table_stride + (j >> g.log_size)];
-    if (id < 0 || id >= g.num) continue;
-    const int64_t at = id * g.sp + hkv * g.sh + (j & ((1 << g.log_size) - 1)) * g.sr;
-    key(static_cast<const bf16*>(p.a.Kp) + at, static_cast<const bf16*>(p.a.Vp) + at);
+  for (int v = 0; v < NW; ++v) {
+    const int s = sm.wsum[v];
+    before += v < w ? s : 0;
+    total += s;
   }
-  if (p.a.Kn)
-    for (int j = 0; j < p.S; ++j) {
-      const size_t at = (((size_t)b * p.Hkv + hkv) * p.S + j) * D;
-      key(static_cast<const bf16*>(p.a.Kn) + at, static_cast<const bf16*>(p.a.Vn) + at);
+  const int excl = before + incl - csum;  // tiles per item of the sequences before c0
+  total = __builtin_amdgcn_readfirstlane(total);
+  const int T = total * I;  // checked on the host to fit in 31 bits
+  constexpr int RUNS = DEC_WAVES / TW;
+  const int n = dec_runs<TW>(RUNS, T);
+  const bool stream = total * p.d.Hkv > (int)(DEC_STREAM_BYTES / (2 * Smem::TILE));
+  auto run_of = [&](int v) { return n == RUNS ? (int)blockIdx.x * TEAMS + v : v * (int)gridDim.x + (int)blockIdx.x; };
+#pragma unroll
+  for (int v = 0; v < TEAMS; ++v) {
+    const int x0 = dec_run_start<RUNS>(run_of(v), n, T);
+    if (csum > 0 && excl * I <= x0 && x0 < (excl + csum) * I) {
+      int pb = excl;
+      for (int b = c0; b < c1; ++b) {
+        const int nt = paged_tiles<KT>(p, dec_len(p.d, lens, b));
+        if (x0 < (pb + nt) * I) {
+          sm.start_b[v] = b;
+          sm.start_off[v] = x0 - pb * I;
+          break;
+        }
+        pb += nt;
+      }
     }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  }
+  __syncthreads();
+
+  // ---- this team's run ----
+  const int gw = run_of(tm);
+  if (gw >= n) return;
+  const int x0 = dec_run_start<RUNS>(gw, n, T), x1 = dec_run_start<RUNS>(gw + 1, n, T);
+  PagedPos pc;
+  pc.b = __builtin_amdgcn_readfirstlane(sm.start_b[tm]);
+  const int off = __builtin_amdgcn_readfirstlane(sm.start_off[tm]);
+  pc.len = __builtin_amdgcn_readfirstlane(dec_len(p.d, lens, pc.b));
+  pc.nt = paged_tiles<KT>(p, pc.len);
+  pc.r = off / pc.nt;
+  pc.j = off - pc.r * pc.nt;
+
+  auto advance = [&](PagedPos q) __attribute__((always_inline)) {
+    if (++q.j == q.nt) {
+      q.j = 0;
+      if (++q.r == I) {
+        q.r = 0;
+        if (++q.b < p.d.B) {
+          q.len = __builtin_amdgcn_readfirstlane(dec_len(p.d, lens, q.b));
+          q.nt = paged_tiles<KT>(p, q.len);
+        }
+      }
+    }
+    return q;
+  };
+  // The kernel's arguments, read again (those needed once per item would take
+  // scalar registers from the tile loop).
+  auto arguments = [&]() __attribute__((always_inline)) -> DecParams {
+    auto* a = (const __attribute__((address_space(4))) DecParams*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(a));
+    return *(const DecParams*)a;
+  };
+  // this lane's query row of item (b, r): row g*grows + 32*tw + l32 of the G*S
+  // rows of its KV head.  A lane past the last row takes the last row instead:
+  // its column is computed like the others and never stored.
+  auto query_row = [&](const DecParams& p, PagedPos q, bool& valid) __attribute__((always_inline)) {
+    const int hkv = q.r / ng, g = q.r - hkv * ng, rl = 32 * tw + l32, R = g * p.grows + rl;
+    valid = R < p.G * p.S && (TW == 1 || rl < p.grows);
+    return ((size_t)q.b * p.Hq + (size_t)hkv * p.G) * p.S + (R < p.G * p.S ? R : p.G * p.S - 1);
+  };
+  struct QRows {
+    bf16x8 v[DS];
+  };
+  auto load_q = [&](PagedPos q) __attribute__((always_inline)) {
+    const DecParams a = arguments();
+    bool valid;
+    const size_t row = query_row(a, q, valid);
+    QRows r;
 #pragma unroll
-  for (int e = 0; e < E; ++e) static_cast<bf16*>(p.a.O)[(size_t)row * D + lane * E + e] = (bf16)(o[e] * inv);
-  if (lane == 0) p.a.LSE[row] = l > 0.f ? (m + __log2f(l)) * LN2 : -INFINITY;
+    for (int s = 0; s < DS; ++s) r.v[s] = *reinterpret_cast<const bf16x8*>(a.Q + row * D + 16 * s + 8 * g2);
+    return r;
+  };
+
+  // ---- copies ----
+  // Instruction u of the team's wave tw fills rows (u * TW + tw) * RPI ... of a
+  // tile, all of one 16-row piece; per lane, the row within the piece and the
+  // 16-byte chunk (swizzled) repeat every PER instructions.
+  constexpr int RPI = 512 / D, CPR = D / 8, NI = KT / (RPI * TW);
+  constexpr int PER = TW * RPI < 16 ? 16 / (TW * RPI) : 1;
+  int crow[PER], cchunk[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    crow[u] = ((u * TW + tw) * RPI + lane / CPR) & 15;
+    cchunk[u] = 16 * ((lane % CPR) ^ chunk_swizzle<D>(crow[u]));
+  }
+  struct Pages {
+    int id[NP];
+  };
+  // Ids of the pages of the cache tile at q (of no meaning, but loaded from the table, for others).
+  auto load_pages = [&](PagedPos q) __attribute__((always_inline)) {
+    Pages g;
+    const int* row = table + (int64_t)imin(q.b, p.d.B - 1) * p.table_stride;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) g.id[i] = row[imin((q.j * KT + 16 * i) >> p.pages.log_size, p.table_width - 1)];
+    return g;
+  };
+  // Copies K and V of the tile at q to dst, dst + TILE; returns the pieces that
+  // may hold keys (bit i: rows 16 i ... of the tile).
+  auto issue = [&](PagedPos q, const Pages& g, char* dst, auto streamed) __attribute__((always_inline)) {
+    constexpr int POLICY = decltype(streamed)::value ? COPY_STREAM : 0;
+    const int ntc = cdiv(q.len, KT), hkv = q.r / ng;
+    const bool cached = q.j < ntc;
+    const int row0 = (cached ? q.j : q.j - ntc) * KT, end = cached ? q.len : p.Sn;
+    const int row_bytes = cached ? (int)p.pages.sr * 2 : D * 2;
+    uint32_t mask = 0;
+    __amdgpu_buffer_rsrc_t rk[NP], rv[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int r = row0 + 16 * i;
+      bool ok = true;
+      int64_t at;
+      if (cached) {
+        ok = (unsigned)g.id[i] < (unsigned)p.pages.num;
+        at = (ok ? g.id[i] : 0) * p.pages.sp + hkv * p.pages.sh + (r & ((1 << p.pages.log_size) - 1)) * p.pages.sr;
+      } else {
+        at = ((int64_t)((size_t)q.b * p.d.Hkv + hkv) * p.Sn + r) * D;
+      }
+      const int left = ok ? imin(imax(end - r, 0), 16) : 0;
+      rk[i] = make_buffer((cached ? p.d.Kc : p.d.Kn) + at, (uint32_t)(left * row_bytes));
+      rv[i] = make_buffer((cached ? p.d.Vc : p.d.Vn) + at, (uint32_t)(left * row_bytes));
+      mask |= ok ? 1u << i : 0u;
+    }
+    auto copy = [&](const __amdgpu_buffer_rsrc_t* rs, char* to) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < NI; ++u) {
+        const int at = crow[u % PER] * row_bytes + cchunk[u % PER];
+        auto* d = (__attribute__((address_space(3))) void*)(to + (u * TW + tw) * 1024);
+        if constexpr (TW * RPI <= 16) {
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(rs[u * TW * RPI / 16], d, 16, at, 0, 0, POLICY);
+        } else {  // two pieces an instruction of the team, by halves of its waves
+          static_assert(TW * RPI <= 32, "pieces an instruction");
+          if (tw < TW / 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs[2 * u], d, 16, at, 0, 0, POLICY);
+          else __builtin_amdgcn_raw_ptr_buffer_load_lds(rs[2 * u + 1], d, 16, at, 0, 0, POLICY);
+        }
+      }
+    };
+    copy(rk, dst);
+    copy(rv, dst + Smem::TILE);
+    return mask;
+  };
+
+  // The whole run, with or without the streaming hint on its copies.
+  auto run = [&](auto streamed) __attribute__((always_inline)) {
+    const LdsOperands<D> ops(lane);
+    QRows qreg, qnext;
+    f32x16 oacc[DB];
+    float m, lsum;
+    auto reset = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) oacc[db][e] = 0.f;
+      m = -INFINITY;
+      lsum = 0.f;
+    };
+    reset();
+    char* const ring = sm.buf[tm];
+    PagedPos pa = pc;  // the next tile to copy, and its pages
+    Pages ga = load_pages(pa);
+    qreg = load_q(pc);
+    // pieces of the tiles in flight, NP bits each, the current tile's lowest
+    uint32_t pieces = issue(pa, ga, ring, streamed);
+    pa = advance(pa);
+#pragma unroll
+    for (int u = 1; u < NST - 1; ++u)
+      if (x0 + u < x1) {
+        ga = load_pages(pa);
+        pieces |= issue(pa, ga, ring + u * 2 * Smem::TILE, streamed) << (NP * u);
+        pa = advance(pa);
+      }
+    ga = load_pages(pa);
+    // Teams: the query rows have landed once all but the newest tile have.
+    if (TW > 1) wait_global_loads_but<2 * NI>();
+
+    // Write out the state of the current item's segment, which ends at tile pc.j
+    // (tile x of all).
+    auto flush = [&](int x) __attribute__((always_inline)) {
+      const DecParams p = arguments();
+      const int item = pc.b * I + pc.r;
+      const int item_start = x - pc.j;  // flat index of the item's first tile
+      const bool ends = pc.j == pc.nt - 1;
+      bool valid;
+      const size_t qrow = query_row(p, pc, valid);
+      const float Lrow = halves_sum(lsum);
+      if (item_start >= x0 && ends) {
+        if (valid) {
+          const bool none = !(Lrow > 0.f);
+          const float inv = none ? 0.f : 1.f / Lrow;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            bf16* op = p.O + qrow * D + 32 * db + 4 * g2;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              st_bf16x4(op + 8 * i, oacc[db][4 * i] * inv, oacc[db][4 * i + 1] * inv, oacc[db][4 * i + 2] * inv,
+                        oacc[db][4 * i + 3] * inv);
+          }
+          if (g2 == 0) p.LSE[qrow] = none ? -INFINITY : (m + __log2f(Lrow)) * LN2;
+        }
+        if (lane == 0 && tw == 0) p.desc[item] = DecRuns{0, -1};
+        return;
+      }
+      if (valid) {
+        const int hkv = pc.r / ng;
+        float* pr = p.part + (dec_slot_row(p, gw, (size_t)pc.b * p.Hkv + hkv, pc.r - hkv * ng) + 32 * tw + l32) * PST;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const f32x4 v = {oacc[db][4 * i], oacc[db][4 * i + 1], oacc[db][4 * i + 2], oacc[db][4 * i + 3]};
+            *reinterpret_cast<f32x4*>(pr + 32 * db + 8 * i + 4 * g2) = v;
+          }
+        if (g2 == 0) *reinterpret_cast<f32x4*>(pr + D) = f32x4{m, Lrow, 0.f, 0.f};
+      }
+      if (ends && lane == 0 && tw == 0) {
+        // the runs holding this item: from the one holding its first tile to this one
+        const int first = (int)((((long long)item_start + 1) * n - 1) / T);
+        p.desc[item] = DecRuns{first, gw};
+      }
+    };
+
+    // One tile: `cur` holds the tile at pc; the copy of the tile NST - 1 ahead
+    // (at pa, if this run has one) goes to `nxt`, whose last readers are done.
+    auto step = [&](const char* __restrict__ cur, char* __restrict__ nxt, PagedPos pn, bool more, bool copies,
+                    bool new_item) __attribute__((always_inline)) {
+      compute_fence();  // the reads of the buffer about to be refilled are done
+      if constexpr (TW == 1) {
+        // (query rows of the next item: a tile ahead, behind the wait, in both branches, as over a dense cache)
+        if (copies) {
+          pieces |= issue(pa, ga, nxt, streamed) << (NP * (NST - 1));
+          pa = advance(pa);
+          ga = load_pages(pa);
+          wait_global_loads_but<(NST - 1) * 2 * NI>();  // the tile at pc has landed (this wave's own copy)
+          if (new_item) qreg = qnext;
+          if (pn.j == 0) qnext = load_q(pn);
+        } else {
+          wait_global_loads();
+          if (new_item) qreg = qnext;
+        }
+      } else {
+        if (new_item) {
+          wait_global_loads();
+          qreg = qnext;
+          compute_fence();  // (keeps this wait from being merged with those below)
+        } else if (copies) {
+          wait_global_loads_but<(NST - 2) * 2 * NI>();  // this wave's part of the tile at pc has landed
+        } else {
+          wait_global_loads();
+        }
+        barrier_lds_only();  // ... every wave's; and all are done with `nxt`
+        if (more && pn.j == 0) qnext = load_q(pn);
+        if (copies) {
+          pieces |= issue(pa, ga, nxt, streamed) << (NP * (NST - 1));
+          pa = advance(pa);
+          ga = load_pages(pa);
+        }
+      }
+      // (the page ids are waited for here: a scalar load in flight would turn every wait for an LDS read
+      // below into one for all of them)
+#pragma unroll
+      for (int i = 0; i < NP; ++i) asm volatile("" : "+s"(ga.id[i]));
+      const int ntc = cdiv(pc.len, KT);
+      const int nvalid = pc.j < ntc ? pc.len - pc.j * KT : p.Sn - (pc.j - ntc) * KT;  // keys before the end
+      const uint32_t here = pieces & ((1u << NP) - 1);
+      pieces >>= NP;
+      // no piece of the tile holds a key
+      if (nvalid <= 0 || (here & ((2u << ((imin(nvalid, KT) - 1) >> 4)) - 1)) == 0) return;
+
+      // S^T[key][query] = sum_d K[key][d] Q[query][d]
+      f32x16 sacc[KB];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sacc[kb][e] = 0.f;
+#pragma unroll
+      for (int s = 0; s < DS; ++s)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) sacc[kb] = mfma32(lds_rows<D>(cur, ops.row_rel, s, kb), qreg.v[s], sacc[kb]);
+      pipeline_lds_reads<DS * KB, 4, 1>();  // operand reads four MFMAs ahead
+      if (nvalid < KT || here != (1u << NP) - 1) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4) {
+            const bool piece = here >> (2 * kb + i4 / 2) & 1;
+#pragma unroll
+            for (int jj = 0; jj < 4; ++jj)
+              if (!piece || 32 * kb + 8 * i4 + 4 * g2 + jj >= nvalid) sacc[kb][4 * i4 + jj] = -INFINITY;
+          }
+      }
+      float m3[KB * 8];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) m3[kb * 8 + e / 2] = fmaxf(sacc[kb][e], sacc[kb][e + 1]);
+      const float mx = halves_max(tree_max<KB * 8>(m3)) * p.d.c;
+      const bool grow = mx > m + DEC_SLACK;
+      if (__any(grow)) {
+        const float alpha = grow ? fast_exp2(m - mx) : 1.f;
+        m = grow ? mx : m;
+        lsum *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) oacc[db][e] *= alpha;
+      }
+      bf16x8 pb[2 * KB];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sacc[kb][e] = fast_exp2(sacc[kb][e] * p.d.c - m);
+        pb[2 * kb] = pack8(sacc[kb], 0);
+        pb[2 * kb + 1] = pack8(sacc[kb], 8);
+      }
+      lsum += tree_sum<KB>(sacc);
+      // O^T[d][query] += sum_key V^T[d][key] P^T[key][query]
+#pragma unroll
+      for (int c = 0; c < 2 * KB; ++c)
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          oacc[db] = mfma32(lds_tr<D>(cur + Smem::TILE, ops.tr_rel0, ops.tr_rel1, c, db), pb[c], oacc[db]);
+      pipeline_lds_reads<2 * KB * DB, (TW == 1 ? 3 : 4), 2>();
+    };
+
+    uint32_t bcur = 0;                           // ring offset of the tile at pc
+    uint32_t bnxt = (NST - 1) * 2 * Smem::TILE;  // ring offset the copy NST - 1 ahead goes to
+    for (int x = x0; x < x1; ++x) {
+      const PagedPos pn = advance(pc);
+      const bool more = x + 1 < x1, copies = x + NST - 1 < x1;
+      step(ring + bcur, ring + bnxt, pn, more, copies, x > x0 && pc.j == 0);
+      bnxt = bcur;
+      bcur = bcur == (NST - 1) * 2 * Smem::TILE ? 0u : bcur + 2 * Smem::TILE;
+      if (!more || pn.j == 0) {
+        flush(x);
+        if (more) reset();  // the next tile starts the next item
+      }
+      pc = pn;
+    }
+  };
+  if (stream) run(Flag<true>());
+  else run(Flag<false>());
+}
+
+template <int D, int TW, int KT, int NST>
+void launch_paged_kernel(const PagedParams& p, const int* table, hipStream_t st) {
+  using Smem = PagedSmem<D, TW, KT, NST>;
+  hipLaunchKernelGGL((paged_kernel<D, TW, KT, NST>), dim3(p.d.runs / Smem::TEAMS), dim3(64 * Smem::NW), 0, st, p,
+                     p.d.cache_lens, table);
+}
+
+template <int D>
+hipError_t launch_paged_d(const DecodeShape& s, const PagedArgs& a, void* ws, hipStream_t st) {
+  PagedParams p;
+  p.d.Q = static_cast<const bf16*>(a.Q);
+  p.d.Kc = static_cast<const bf16*>(a.Kp);
+  p.d.Vc = static_cast<const bf16*>(a.Vp);
+  p.d.Kn = static_cast<const bf16*>(a.Kn);
+  p.d.Vn = static_cast<const bf16*>(a.Vn);
+  p.d.cache_lens = a.cache_lens;
+  p.d.O = static_cast<bf16*>(a.O);
+  p.d.LSE = a.LSE;
+  p.d.desc = static_cast<DecRuns*>(ws);
+  p.d.part = reinterpret_cast<float*>(static_cast<char*>(ws) + decode_desc_bytes(s));
+  p.d.B = s.B;
+  p.d.S = s.S;
+  p.d.Hq = s.Hq;
+  p.d.Hkv = s.Hkv;
+  p.d.G = s.Hq / s.Hkv;
+  p.d.C = s.C;
+  p.d.c = s.scale * LOG2E;
+  const DecodeGroups g = decode_groups(s);
+  p.d.ng = g.ng;
+  p.d.grows = g.rows;
+  p.d.hrows = DEC_QT * decode_query_tiles(s);
+  p.d.runs = g.runs;
+  p.Sn = a.Kn ? s.S : 0;
+  p.table_width = a.width;
+  p.table_stride = a.table_stride;
+  p.pages = a.pages;
+  if (g.waves == 1) launch_paged_kernel<D, 1, 32, 2>(p, a.table, st);
+  else if (g.waves == 2) launch_paged_kernel<D, 2, (D == 64 ? 64 : 32), 4>(p, a.table, st);
+  else launch_paged_kernel<D, 4, 64, 512 / D>(p, a.table, st);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  return launch_dec_combine<D, true>(s, g, p.d, st);
 }
 
 }  // namespace
 
 hipError_t launch_paged_decode(const DecodeShape& s, const PagedArgs& a, void* ws, hipStream_t st) {
-  (void)ws;
-  const PagedParams p{a, s.B, s.S, s.Hq, s.Hkv, s.Hq / s.Hkv, s.scale * LOG2E};
-  const dim3 grid((unsigned)((size_t)s.B * s.Hq * s.S));
-  if (s.D == 128) hipLaunchKernelGGL((paged_row_kernel<128>), grid, dim3(64), 0, st, p);
-  else hipLaunchKernelGGL((paged_row_kernel<64>), grid, dim3(64), 0, st, p);
-  return hipGetLastError();
+  return s.D == 128 ? launch_paged_d<128>(s, a, ws, st) : launch_paged_d<64>(s, a, ws, st);
 }
 
 }  // namespace bd
