@@ -569,58 +569,81 @@ def _launch_context(device: torch.device, stream):
         return torch.cuda.stream(stream)
     if device.type == "cuda" and device.index != torch.cuda.current_device():
         return torch.cuda.device(device)
-    return contextlib.nullcontext()
+    return _HERE
 
 
-def _span(strides):
-    return (ctypes.c_int64 * len(strides))(*strides)
+_HERE = contextlib.nullcontext()
 
 
-def _head_rows(name, t, shape, dtype, device):
-    """Element strides (batch, token, head) of rows t [B, N, H, D], D contiguous."""
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.dtype != dtype:
-        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{name}: expected device {device}, got {t.device}")
-    if t.stride(-1) != 1 and t.numel() > 0:
+def _row_strides(name, shape, strides):
+    """Element strides (batch, token, head) of rows [.., N, H, D] of D contiguous values."""
+    if strides[-1] != 1 and 0 not in shape:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    st = [s if n > 1 else 0 for n, s in zip(t.shape[:-1], t.stride()[:-1])]
+    # (a dimension of one has no stride of its own)
+    st = [s if n > 1 else 0 for n, s in zip(shape[:-1], strides[:-1])]
     if any(s % 8 for s in st):
-        raise ValueError(f"{name}: strides must be multiples of 8 elements, got {t.stride()}")
+        raise ValueError(f"{name}: strides must be multiples of 8 elements, got {strides}")
     return st if len(st) == 3 else [0] + st
 
 
-def _rope_args(q, k, v, q_weight, k_weight, rope, positions):
-    """Checked arguments common to the calls: (B, N, Hq, Hkv, D, device, dtype code, input strides, the C
-    call's middle arguments, lead), lead being the leading dimensions ((B,) or ()) of the results."""
-    if q.dim() not in (3, 4) or k.dim() != q.dim():
+def _stride_array(strides):
+    return (ctypes.c_int64 * len(strides))(*strides)
+
+
+# What a call derives from shapes and strides alone (checked on the way, and
+# looked up once per combination, as a size is): the dimensions, the stride
+# array of the C call and the shapes of the results.
+_RopeLayout = collections.namedtuple("_RopeLayout", "B N Hq Hkv D strides pos_stride q_shape k_shape")
+
+
+@functools.lru_cache(maxsize=1024)
+def _rope_layout(q_shape, q_strides, k_shape, k_strides, v_shape, v_strides, pos_shape):
+    if len(q_shape) not in (3, 4) or len(k_shape) != len(q_shape):
         raise ValueError("q [B,N,Hq,D] and k/v [B,N,Hkv,D] (or without B) expected")
-    lead = tuple(q.shape[:-3])
-    B = lead[0] if lead else 1
-    N, Hq, D = q.shape[-3:]
-    Hkv = k.shape[-2]
-    dev, dt = q.device, q.dtype
-    code = _dtype_code(q)
-    strides = _head_rows("q", q, lead + (N, Hq, D), dt, dev) + _head_rows("k", k, lead + (N, Hkv, D), dt, dev)
-    if v is not None:
-        strides += _head_rows("v", v, lead + (N, Hkv, D), dt, dev)
-    wdt = q_weight.dtype
-    if wdt not in (dt, torch.float32):
+    lead = tuple(q_shape[:-3])
+    N, Hq, D = q_shape[-3:]
+    Hkv = k_shape[-2]
+    rows = (("q", q_shape, q_strides, Hq), ("k", k_shape, k_strides, Hkv), ("v", v_shape, v_strides, Hkv))
+    strides = []
+    for name, shape, st, H in rows[:2 if v_shape is None else 3]:
+        if tuple(shape) != lead + (N, H, D):
+            raise ValueError(f"{name}: expected shape {lead + (N, H, D)}, got {tuple(shape)}")
+        strides += _row_strides(name, shape, st)
+    if tuple(pos_shape) not in ((N,), lead + (N,)):
+        raise ValueError(f"positions: expected shape {lead + (N,)} or {(N,)}, got {tuple(pos_shape)}")
+    return _RopeLayout(lead[0] if lead else 1, N, Hq, Hkv, D, _stride_array(strides), N if len(pos_shape) == 2 else 0,
+                       lead + (Hq, N, D), lead + (Hkv, N, D))
+
+
+@functools.lru_cache(maxsize=1024)
+def _qkv_layout(shape, strides, Hq, Hkv, D, pos_shape):
+    """_rope_layout of a fused projection [.., N, (Hq + 2 Hkv) D], whose heads start at multiples of D."""
+    if len(shape) not in (2, 3) or shape[-1] != (Hq + 2 * Hkv) * D:
+        raise ValueError(f"qkv [B,N,(Hq + 2 Hkv) D] (or without B) expected, got {tuple(shape)} for {Hq}/{Hkv} heads of {D}")
+    heads = lambda H: (tuple(shape[:-1]) + (H, D), tuple(strides[:-1]) + (D * strides[-1], strides[-1]))  # noqa: E731
+    return _rope_layout(*heads(Hq), *heads(Hkv), *heads(Hkv), pos_shape)
+
+
+def _rope_inputs(lay, x, others, q_weight, k_weight, rope, positions):
+    """Checks what a layout does not hold (types and devices; x: one of the projections, others: the rest) and
+    returns the C call's arguments from the weights to wdtype but for eps, in two parts around it."""
+    dt, dev, wdt, D = x.dtype, x.device, q_weight.dtype, lay.D
+    for t in others:
+        if t.dtype is not dt or t.device != dev:
+            raise (TypeError if t.dtype != dt else ValueError)(
+                f"q, k, v: one type and device expected, got {dt} on {dev} and {t.dtype} on {t.device}")
+    code = _dtype_code(x)
+    if wdt is not dt and wdt is not torch.float32:
         raise TypeError(f"q_weight: expected {dt} or torch.float32, got {wdt}")
     _check("q_weight", q_weight, (D,), wdt, dev)
     _check("k_weight", k_weight, (D,), wdt, dev)
     if rope.dim() != 2:
         raise ValueError("rope [n, D] expected")
-    _check("rope", rope, (rope.shape[0], D), torch.float32, dev)
-    if positions.dim() == 1:
-        _check("positions", positions, (N,), torch.int32, dev)
-    else:
-        _check("positions", positions, lead + (N,), torch.int32, dev)
-    pos_stride = N if positions.dim() == 2 else 0
-    middle = (_ptr(q_weight), _ptr(k_weight), _ptr(rope), rope.shape[0], _ptr(positions), pos_stride)
-    return B, N, Hq, Hkv, D, dev, code, _dtype_code(q_weight), strides, middle, lead
+    n = rope.shape[0]
+    _check("rope", rope, (n, D), torch.float32, dev)
+    _check("positions", positions, positions.shape, torch.int32, dev)
+    head = (_ptr(q_weight), _ptr(k_weight), _ptr(rope), n, _ptr(positions), lay.pos_stride)
+    return head, (code, code if wdt is dt else BD_ATTN_FP32)
 
 
 def bd_rope_table(n: int, D: int, theta: float = 1e6, inv_freq=None, device="cuda", out=None, stream=None):
@@ -647,6 +670,14 @@ def bd_rope_table(n: int, D: int, theta: float = 1e6, inv_freq=None, device="cud
     return t
 
 
+def _result(name, t, shape, dtype, device):
+    """The caller's array for a result, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _check(name, t, shape, dtype, device)
+    return t
+
+
 def bd_qk_norm_rope_fwd(q, k, v, q_weight, k_weight, rope, positions, eps: float = 1e-6, q_out=None, k_out=None,
                         v_out=None, stream=None):
     """Heads normalised (q, k), rotated (q, k) and laid out (q, k, v) for the attention.
@@ -656,20 +687,22 @@ def bd_qk_norm_rope_fwd(q, k, v, q_weight, k_weight, rope, positions, eps: float
     B for packed sequences); q_weight, k_weight [D] in that type or float32;
     rope: bd_rope_table; positions: int32 [B,N] or [N].  Returns q [B,Hq,N,D],
     k, v [B,Hkv,N,D], contiguous."""
-    B, N, Hq, Hkv, D, dev, code, wcode, strides, middle, lead = _rope_args(q, k, v, q_weight, k_weight, rope, positions)
+    lay = _rope_layout(q.shape, q.stride(), k.shape, k.stride(), v.shape, v.stride(), positions.shape)
+    args = _rope_inputs(lay, q, (k, v), q_weight, k_weight, rope, positions)
+    return _rope_fwd(lay, (_ptr(q), _ptr(k), _ptr(v)), args, eps, q.dtype, q.device, q_out, k_out, v_out, stream)
+
+
+def _rope_fwd(lay, ptrs, args, eps, dtype, dev, q_out=None, k_out=None, v_out=None, stream=None):
+    B, N, Hq, Hkv, D, strides, _, q_shape, k_shape = lay
     with _launch_context(dev, stream):
-        outs = []
-        for name, t, H in (("q_out", q_out, Hq), ("k_out", k_out, Hkv), ("v_out", v_out, Hkv)):
-            shape = lead + (H, N, D)
-            if t is None:
-                t = torch.empty(shape, dtype=q.dtype, device=dev)
-            _check(name, t, shape, q.dtype, dev)
-            outs.append(t)
-        st = lib().bd_qk_norm_rope_fwd(_ptr(q), _ptr(k), _ptr(v), _span(strides), *middle, B, N, Hq, Hkv, D, float(eps),
-                                       code, wcode, *map(_ptr, outs), _stream_handle(dev, stream))
+        qo = _result("q_out", q_out, q_shape, dtype, dev)
+        ko = _result("k_out", k_out, k_shape, dtype, dev)
+        vo = _result("v_out", v_out, k_shape, dtype, dev)
+        st = lib().bd_qk_norm_rope_fwd(*ptrs, strides, *args[0], B, N, Hq, Hkv, D, eps, *args[1], _ptr(qo), _ptr(ko),
+                                       _ptr(vo), _stream_handle(dev, stream))
     if st:
         raise BdAttnError(st, "bd_qk_norm_rope_fwd")
-    return tuple(outs)
+    return qo, ko, vo
 
 
 def bd_qk_norm_rope_workspace_bytes(B, N, Hq, Hkv, D, dtype=BD_ATTN_BF16) -> int:
@@ -681,29 +714,37 @@ def bd_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, rope, positions, e
     """Gradients of bd_qk_norm_rope_fwd for those of its results, dq [B,Hq,N,D] and dk, dv
     [B,Hkv,N,D] (contiguous): returns those of q, k, v (new, or the given arrays with any non-overlapping
     strides) and of the weights."""
-    B, N, Hq, Hkv, D, dev, code, wcode, strides, middle, lead = _rope_args(q, k, None, q_weight, k_weight, rope, positions)
-    for name, t, H in (("dq", dq, Hq), ("dk", dk, Hkv), ("dv", dv, Hkv)):
-        _check(name, t, lead + (H, N, D), q.dtype, dev)
+    lay = _rope_layout(q.shape, q.stride(), k.shape, k.stride(), None, None, positions.shape)
+    args = _rope_inputs(lay, q, (k,), q_weight, k_weight, rope, positions)
+    dev, dt = q.device, q.dtype
     with _launch_context(dev, stream):
         grads, gstrides = [], []
-        for name, t, H in (("grad_q", grad_q, Hq), ("grad_k", grad_k, Hkv), ("grad_v", grad_v, Hkv)):
-            shape = lead + (N, H, D)
+        for name, t, like in (("grad_q", grad_q, q), ("grad_k", grad_k, k), ("grad_v", grad_v, k)):
             if t is None:
-                t = torch.empty(shape, dtype=q.dtype, device=dev)
-            gstrides += _head_rows(name, t, shape, q.dtype, dev)
+                t = torch.empty(like.shape, dtype=dt, device=dev)
+            elif t.shape != like.shape or t.dtype != dt or t.device != dev:
+                raise ValueError(f"{name}: expected {dt} {tuple(like.shape)} on {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+            gstrides += _row_strides(name, t.shape, t.stride())
             grads.append(t)
-        for name, t, w in (("grad_q_weight", grad_q_weight, q_weight), ("grad_k_weight", grad_k_weight, k_weight)):
-            t = torch.empty_like(w) if t is None else t
-            _check(name, t, (D,), w.dtype, dev)
-            grads.append(t)
-        nbytes = _known_size("bd_qk_norm_rope_workspace_bytes", B, N, Hq, Hkv, D, code)
-        ws, wp, wn = _workspace(nbytes, dev, workspace)
-        st = lib().bd_qk_norm_rope_bwd(_ptr(dq), _ptr(dk), _ptr(dv), _ptr(q), _ptr(k), _span(strides), *middle, B, N, Hq,
-                                       Hkv, D, float(eps), code, wcode, *map(_ptr, grads[:3]), _span(gstrides),
-                                       *map(_ptr, grads[3:]), wp, wn, _stream_handle(dev, stream))
+        gqw = _result("grad_q_weight", grad_q_weight, (lay.D,), q_weight.dtype, dev)
+        gkw = _result("grad_k_weight", grad_k_weight, (lay.D,), q_weight.dtype, dev)
+        _rope_bwd(lay, (dq, dk, dv), (_ptr(q), _ptr(k)), args, eps, dt, dev, [_ptr(t) for t in grads],
+                  _stride_array(gstrides), gqw, gkw, workspace, stream)
+    return (*grads, gqw, gkw)
+
+
+def _rope_bwd(lay, dy, ptrs, args, eps, dtype, dev, grad_ptrs, grad_strides, gqw, gkw, workspace=None, stream=None):
+    B, N, Hq, Hkv, D, strides, _, q_shape, k_shape = lay
+    dq, dk, dv = dy
+    _check("dq", dq, q_shape, dtype, dev)
+    _check("dk", dk, k_shape, dtype, dev)
+    _check("dv", dv, k_shape, dtype, dev)
+    nbytes = _known_size("bd_qk_norm_rope_workspace_bytes", B, N, Hq, Hkv, D, args[1][0])
+    ws, wp, wn = _workspace(nbytes, dev, workspace)
+    st = lib().bd_qk_norm_rope_bwd(_ptr(dq), _ptr(dk), _ptr(dv), *ptrs, strides, *args[0], B, N, Hq, Hkv, D, eps, *args[1],
+                                   *grad_ptrs, grad_strides, _ptr(gqw), _ptr(gkw), wp, wn, _stream_handle(dev, stream))
     if st:
         raise BdAttnError(st, "bd_qk_norm_rope_bwd")
-    return tuple(grads)
 
 
 class QkNormRopeFunction(torch.autograd.Function):
@@ -723,32 +764,41 @@ class QkNormRopeFunction(torch.autograd.Function):
         return (*grads, None, None, None)
 
 
-def _qkv_views(qkv, Hq, Hkv, D):
-    """q, k, v [.., H, D] of a fused projection [.., (Hq + 2 Hkv) D]."""
-    x = qkv.unflatten(-1, (Hq + 2 * Hkv, D))
-    return x[..., :Hq, :], x[..., Hq:Hq + Hkv, :], x[..., Hq + Hkv:, :]
-
-
 class QkvNormRopeFunction(torch.autograd.Function):
-    """Autograd wrapper over a fused projection, whose gradient is written in place of three."""
+    """Autograd wrapper over a fused projection, whose gradient is written as one array."""
 
     @staticmethod
     def forward(ctx, qkv, Hq, Hkv, q_weight, k_weight, rope, positions, eps):
         ctx.save_for_backward(qkv, q_weight, k_weight, rope, positions)
         ctx.heads, ctx.eps = (Hq, Hkv), eps
-        return bd_qk_norm_rope_fwd(*_qkv_views(qkv, Hq, Hkv, q_weight.numel()), q_weight, k_weight, rope, positions, eps)
+        D = q_weight.numel()
+        lay = _qkv_layout(qkv.shape, qkv.stride(), Hq, Hkv, D, positions.shape)
+        args = _rope_inputs(lay, qkv, (), q_weight, k_weight, rope, positions)
+        return _rope_fwd(lay, QkvNormRopeFunction._parts(qkv, Hq, Hkv, D), args, eps, qkv.dtype, qkv.device)
+
+    @staticmethod
+    def _parts(qkv, Hq, Hkv, D):
+        """Addresses of the first query, key and value head."""
+        p, el = _ptr(qkv), qkv.element_size()
+        return p, p + Hq * D * el, p + (Hq + Hkv) * D * el
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dq, dk, dv):
-        qkv, q_weight, *rest = ctx.saved_tensors
+        qkv, q_weight, k_weight, rope, positions = ctx.saved_tensors
+        Hq, Hkv = ctx.heads
         D = q_weight.numel()
-        q, k, _ = _qkv_views(qkv, *ctx.heads, D)
-        grad = torch.empty(qkv.shape, dtype=qkv.dtype, device=qkv.device)
-        gq, gk, gv = _qkv_views(grad, *ctx.heads, D)
-        *_, dwq, dwk = bd_qk_norm_rope_bwd(dq.contiguous(), dk.contiguous(), dv.contiguous(), q, k, q_weight, *rest,
-                                           ctx.eps, gq, gk, gv)
-        return grad, None, None, dwq, dwk, None, None, None
+        dev, dt = qkv.device, qkv.dtype
+        lay = _qkv_layout(qkv.shape, qkv.stride(), Hq, Hkv, D, positions.shape)
+        args = _rope_inputs(lay, qkv, (), q_weight, k_weight, rope, positions)
+        with _launch_context(dev, None):
+            grad = torch.empty(qkv.shape, dtype=dt, device=dev)
+            gqw, gkw = torch.empty_like(q_weight), torch.empty_like(k_weight)
+            strides = _qkv_layout(grad.shape, grad.stride(), Hq, Hkv, D, positions.shape).strides
+            _rope_bwd(lay, (dq.contiguous(), dk.contiguous(), dv.contiguous()),
+                      QkvNormRopeFunction._parts(qkv, Hq, Hkv, D)[:2], args, ctx.eps, dt, dev,
+                      QkvNormRopeFunction._parts(grad, Hq, Hkv, D), strides, gqw, gkw)
+        return grad, None, None, gqw, gkw, None, None, None
 
 
 def qk_norm_rope(q, k, v, q_weight, k_weight, rope, positions, eps: float = 1e-6):
@@ -765,42 +815,62 @@ def qkv_norm_rope(qkv, Hq: int, Hkv: int, q_weight, k_weight, rope, positions, e
 # Paged KV cache: k_pages, v_pages [pages, Hkv, page_size, D] bfloat16 with any
 # equal strides (a cache kept token-major is passed as its permuted view).
 
-def _pages(k_pages, v_pages, Hkv, D, device):
-    """Page arguments of the C calls: (pages, page size) and the strides."""
-    if k_pages.dim() != 4:
+@functools.lru_cache(maxsize=1024)
+def _page_layout(k_shape, k_strides, v_shape, v_strides, Hkv, D):
+    """Page arguments of the C calls: pages, page size and the strides (of page, head and row)."""
+    if len(k_shape) != 4:
         raise ValueError("k_pages and v_pages [pages,Hkv,page_size,D] expected")
-    n, P = k_pages.shape[0], k_pages.shape[2]
+    n, P = k_shape[0], k_shape[2]
+    for name, shape in (("k_pages", k_shape), ("v_pages", v_shape)):
+        if tuple(shape) != (n, Hkv, P, D):
+            raise ValueError(f"{name}: expected shape {(n, Hkv, P, D)}, got {tuple(shape)}")
+    if k_strides != v_strides or k_strides[3] != 1:
+        raise ValueError("k_pages and v_pages: equal strides with the last dimension contiguous expected")
+    # (a dimension of one page or head has no stride of its own)
+    st = tuple(s if m > 1 else 0 for m, s in zip(k_shape[:3], k_strides[:3]))
+    if any(s % 8 for s in st):
+        raise ValueError(f"k_pages: strides must be multiples of 8 elements, got {k_strides}")
+    return (n, P) + st
+
+
+def _pages(k_pages, v_pages, Hkv, D, device):
+    lay = _page_layout(k_pages.shape, k_pages.stride(), v_pages.shape, v_pages.stride(), Hkv, D)
     for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
-        if tuple(t.shape) != (n, Hkv, P, D):
-            raise ValueError(f"{name}: expected shape {(n, Hkv, P, D)}, got {tuple(t.shape)}")
-        if t.dtype != torch.bfloat16:
+        if t.dtype is not torch.bfloat16:
             raise TypeError(f"{name}: expected {torch.bfloat16}, got {t.dtype}")
         if t.device != device:
             raise ValueError(f"{name}: expected device {device}, got {t.device}")
-    if k_pages.stride() != v_pages.stride() or k_pages.stride(3) != 1:
-        raise ValueError("k_pages and v_pages: equal strides with the last dimension contiguous expected")
-    # (a dimension of one page or head has no stride of its own)
-    sp, sh, sr = (s if m > 1 else 0 for m, s in zip(k_pages.shape[:3], k_pages.stride()[:3]))
-    if sp % 8 or sh % 8 or sr % 8:
-        raise ValueError(f"k_pages: strides must be multiples of 8 elements, got {k_pages.stride()}")
-    return n, P, sp, sh, sr
+    return lay
+
+
+def _table_stride(page_table, B, device):
+    """Checks a page table [B, max_pages] (rows contiguous) and returns the distance of its rows."""
+    if page_table.dim() != 2 or page_table.shape[0] != B:
+        raise ValueError(f"page_table: expected shape ({B}, max_pages), got {tuple(page_table.shape)}")
+    if page_table.dtype is not torch.int32:
+        raise TypeError(f"page_table: expected {torch.int32}, got {page_table.dtype}")
+    width, (rows, cols) = page_table.shape[1], page_table.stride()
+    if page_table.device != device or (cols != 1 and width > 1):
+        raise ValueError(f"page_table: contiguous rows on {device} expected")
+    return rows if B > 1 else width
 
 
 def bd_qk_norm_rope_paged(q, k, v, q_weight, k_weight, rope, positions, slots, k_pages, v_pages, eps: float = 1e-6,
                           q_out=None, stream=None):
     """bd_qk_norm_rope_fwd for serving: returns the queries [B,Hq,N,D] and writes keys and values into
     the pages, token (b, n) at row slots[b, n] (int32 [B,N] of bd_paged_plan; outside the pages: not written)."""
-    B, N, Hq, Hkv, D, dev, code, wcode, strides, middle, lead = _rope_args(q, k, v, q_weight, k_weight, rope, positions)
+    lay = _rope_layout(q.shape, q.stride(), k.shape, k.stride(), v.shape, v.stride(), positions.shape)
+    B, N, Hq, Hkv, D, strides, _, q_shape, _ = lay
+    dev = q.device
     if q.dtype != torch.bfloat16:
         raise TypeError(f"bd_qk_norm_rope_paged supports bfloat16 tensors, got {q.dtype}")
-    _check("slots", slots, lead + (N,), torch.int32, dev)
-    n, P, sp, sh, sr = _pages(k_pages, v_pages, Hkv, D, dev)
+    head, types = _rope_inputs(lay, q, (k, v), q_weight, k_weight, rope, positions)
+    _check("slots", slots, q.shape[:-2], torch.int32, dev)
+    pages = _pages(k_pages, v_pages, Hkv, D, dev)
     with _launch_context(dev, stream):
-        o = torch.empty(lead + (Hq, N, D), dtype=q.dtype, device=dev) if q_out is None else q_out
-        _check("q_out", o, lead + (Hq, N, D), q.dtype, dev)
-        st = lib().bd_qk_norm_rope_paged(_ptr(q), _ptr(k), _ptr(v), _span(strides), *middle, _ptr(slots), B, N, Hq, Hkv, D,
-                                         float(eps), code, wcode, _ptr(o), _ptr(k_pages), _ptr(v_pages), n, P, sp, sh, sr,
-                                         _stream_handle(dev, stream))
+        o = _result("q_out", q_out, q_shape, torch.bfloat16, dev)
+        st = lib().bd_qk_norm_rope_paged(_ptr(q), _ptr(k), _ptr(v), strides, *head, _ptr(slots), B, N, Hq, Hkv, D, eps,
+                                         *types, _ptr(o), _ptr(k_pages), _ptr(v_pages), *pages, _stream_handle(dev, stream))
     if st:
         raise BdAttnError(st, "bd_qk_norm_rope_paged")
     return o
@@ -823,12 +893,7 @@ def bd_paged_plan(cache_lens, new_lens, page_table, free_pages, free_head, num_p
     B = cache_lens.numel()
     _check("cache_lens", cache_lens, (B,), torch.int32, dev)
     _check("new_lens", new_lens, (B,), torch.int32, dev)
-    if page_table.dim() != 2 or page_table.shape[0] != B:
-        raise ValueError(f"page_table: expected shape ({B}, max_pages), got {tuple(page_table.shape)}")
-    if page_table.dtype != torch.int32:
-        raise TypeError(f"page_table: expected {torch.int32}, got {page_table.dtype}")
-    if page_table.device != dev or (page_table.stride(1) != 1 and page_table.shape[1] > 1):
-        raise ValueError(f"page_table: contiguous rows on {dev} expected")
+    table_stride = _table_stride(page_table, B, dev)
     if free_pages.dim() != 1:
         raise ValueError("free_pages: 1-D expected")
     _check("free_pages", free_pages, (free_pages.numel(),), torch.int32, dev)
@@ -837,22 +902,22 @@ def bd_paged_plan(cache_lens, new_lens, page_table, free_pages, free_head, num_p
         raise ValueError("S (rows of S tokens a sequence) or total (packed tokens) expected")
     if S is not None and S < 1:
         raise ValueError(f"S: at least 1 expected, got {S}")
-    shape = (int(total),) if S is None else (B, int(S))
-    width = page_table.shape[1]
+    S_, total_ = (0, int(total)) if S is None else (int(S), 0)
+    shape = (B, S_) if S_ else (total_,)
+    i32 = torch.int32
     with _launch_context(dev, stream):
-        out = []
-        for name, t, shp in (("lens", lens, (B,)), ("cu", cu, (B + 1,)), ("slots", slots, shape),
-                             ("positions", positions, shape), ("state", state, (2,))):
-            t = torch.empty(shp, dtype=torch.int32, device=dev) if t is None else t
-            _check(name, t, shp, torch.int32, dev)
-            out.append(t)
-        st = lib().bd_paged_plan(_ptr(cache_lens), _ptr(new_lens), _ptr(page_table), B, width,
-                                 page_table.stride(0) if B > 1 else width, _ptr(free_pages), free_pages.numel(),
-                                 _ptr(free_head), num_pages, page_size, 0 if S is None else S, shape[0] if S is None else 0,
-                                 *map(_ptr, out), _stream_handle(dev, stream))
+        lens = _result("lens", lens, (B,), i32, dev)
+        cu = _result("cu", cu, (B + 1,), i32, dev)
+        slots = _result("slots", slots, shape, i32, dev)
+        positions = _result("positions", positions, shape, i32, dev)
+        state = _result("state", state, (2,), i32, dev)
+        st = lib().bd_paged_plan(_ptr(cache_lens), _ptr(new_lens), _ptr(page_table), B, page_table.shape[1], table_stride,
+                                 _ptr(free_pages), free_pages.shape[0], _ptr(free_head), num_pages, page_size, S_, total_,
+                                 _ptr(lens), _ptr(cu), _ptr(slots), _ptr(positions), _ptr(state),
+                                 _stream_handle(dev, stream))
     if st:
         raise BdAttnError(st, "bd_paged_plan")
-    return PagedPlan(*out)
+    return PagedPlan(lens, cu, slots, positions, state)
 
 
 def bd_attn_paged_decode_workspace_bytes(B, S, Hq, Hkv, D, page_size, max_pages, dtype=BD_ATTN_BF16) -> int:
@@ -870,39 +935,30 @@ def bd_attn_paged_decode_fwd(q, k_pages, v_pages, page_table, cache_lens, k_new=
     see the cache alone.  Rows that see no key: O = 0, LSE = -inf."""
     if q.dim() != 4 or k_pages.dim() != 4:
         raise ValueError("q [B,Hq,S,D] and k_pages/v_pages [pages,Hkv,page_size,D] expected")
-    B, Hq, S, D = q.shape
-    Hkv = k_pages.shape[1]
-    dev = q.device
-    if q.dtype != torch.bfloat16:
+    B, Hq, S, D = shape = q.shape
+    Hkv, dev, bf16 = k_pages.shape[1], q.device, torch.bfloat16
+    if q.dtype is not bf16:
         raise TypeError(f"bd_attn_paged_decode_fwd supports bfloat16 tensors, got {q.dtype}")
-    _check("q", q, (B, Hq, S, D), torch.bfloat16, dev)
+    _check("q", q, shape, bf16, dev)
     n, P, sp, sh, sr = _pages(k_pages, v_pages, Hkv, D, dev)
-    if page_table.dim() != 2 or page_table.shape[0] != B:
-        raise ValueError(f"page_table: expected shape ({B}, max_pages), got {tuple(page_table.shape)}")
-    if page_table.dtype != torch.int32:
-        raise TypeError(f"page_table: expected {torch.int32}, got {page_table.dtype}")
+    table_stride = _table_stride(page_table, B, dev)
     width = page_table.shape[1]
-    if page_table.device != dev or (page_table.stride(1) != 1 and width > 1):
-        raise ValueError(f"page_table: contiguous rows on {dev} expected")
     _check("cache_lens", cache_lens, (B,), torch.int32, dev)
     if (k_new is None) != (v_new is None):
         raise ValueError("k_new and v_new: both or neither expected")
     kn = vn = None
     if k_new is not None:
-        _check("k_new", k_new, (B, Hkv, S, D), torch.bfloat16, dev)
-        _check("v_new", v_new, (B, Hkv, S, D), torch.bfloat16, dev)
+        _check("k_new", k_new, (B, Hkv, S, D), bf16, dev)
+        _check("v_new", v_new, (B, Hkv, S, D), bf16, dev)
         kn, vn = _ptr(k_new), _ptr(v_new)
     with _launch_context(dev, stream):
-        o = torch.empty_like(q) if out is None else out
-        l_ = torch.empty((B, Hq, S), dtype=torch.float32, device=dev) if lse is None else lse
-        _check("out", o, q.shape, torch.bfloat16, dev)
-        _check("lse", l_, (B, Hq, S), torch.float32, dev)
+        o = _result("out", out, shape, bf16, dev)
+        l_ = _result("lse", lse, (B, Hq, S), torch.float32, dev)
         nbytes = _known_size("bd_attn_paged_decode_workspace_bytes", B, S, Hq, Hkv, D, P, width, BD_ATTN_BF16)
         ws, wp, wn = _workspace(nbytes, dev, workspace)
         st = lib().bd_attn_paged_decode_fwd(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(cache_lens), kn,
-                                            vn, B, S, Hq, Hkv, D, n, P, width, page_table.stride(0) if B > 1 else 0,
-                                            sp, sh, sr, _scale_arg(scale), BD_ATTN_BF16, _ptr(o), _ptr(l_), wp, wn,
-                                            _stream_handle(dev, stream))
+                                            vn, B, S, Hq, Hkv, D, n, P, width, table_stride, sp, sh, sr, _scale_arg(scale),
+                                            BD_ATTN_BF16, _ptr(o), _ptr(l_), wp, wn, _stream_handle(dev, stream))
     if st:
         raise BdAttnError(st, "bd_attn_paged_decode_fwd")
     return o, l_

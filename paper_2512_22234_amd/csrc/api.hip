@@ -912,7 +912,8 @@ int bd_attn_paged_decode_fwd(const void* Q, const void* K_pages, const void* V_p
   Range pages[2];
   if (!make_pages(K_pages, V_pages, num_pages, page_size, page_stride, head_stride, row_stride, Hkv, D, false, a.pages,
                   pages[0], pages[1]) ||
-      row_stride < D || row_stride > (1 << 20) || table_stride < 0 || table_stride > kMaxStride ||
+      page_stride > INT32_MAX || row_stride < D || row_stride > (1 << 20) || row_stride * page_size > (1 << 30) ||
+      table_stride < 0 || table_stride > kMaxStride ||
       (B > 1 && table_stride != 0 && table_stride < max_pages))
     return BD_ATTN_ERR_INVALID_ARGUMENT;
   const size_t need = bd::decode_workspace_bytes(s);

@@ -13,12 +13,11 @@
 // all (sequence, KV head, row group) items end to end, in equal contiguous runs
 // over teams of TW waves, one per 32 query rows; a run that holds part of an
 // item leaves unnormalised sums, which a second kernel joins.  What differs:
-//   - A tile's rows lie in pages: each 16 rows (a page holds a multiple of 16)
-//     have a buffer descriptor of their own, which ends with the last valid row.
-//     A copy instruction fills 1 KiB of the tile (4 rows of 128, 8 of 64) from
-//     one of them, so pages cost scalar work only, whatever their size and
-//     strides.  The page ids of the next tile are read (scalar loads) while the
-//     current one is waited for.
+//   - A tile's rows lie in pages: each piece of 16 rows (a page holds a multiple
+//     of 16) is copied by one wave through a buffer descriptor of its own, which
+//     ends with the last valid row.  So pages cost scalar work only, whatever
+//     their size and strides.  The page ids of the next tile are read (scalar
+//     loads) while the current one is waited for.
 //   - Items have at least one tile, empty where there is no key, so that their
 //     rows are written.  Tiles without a key are not computed; 16-row pieces
 //     without one are masked.
@@ -51,10 +50,10 @@ struct PagedSmem {
   int start_b[TEAMS], start_off[TEAMS];          // where each team's run starts
 };
 
-// Position of a tile: sequence b (cache length len, nt tiles per item), item
-// r of the sequence (KV head r / ng, row group r % ng), tile j of the item.
+// Position of a tile: sequence b (cache length len, nt tiles per item), KV head
+// h and row group g of the item, tile j of it.
 struct PagedPos {
-  int b, len, nt, r, j;
+  int b, len, nt, h, g, j;
 };
 
 // `lens` and `table` are the parameters' arrays as restrict kernel arguments, read
@@ -131,17 +130,22 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
   const int off = __builtin_amdgcn_readfirstlane(sm.start_off[tm]);
   pc.len = __builtin_amdgcn_readfirstlane(dec_len(p.d, lens, pc.b));
   pc.nt = paged_tiles<KT>(p, pc.len);
-  pc.r = off / pc.nt;
-  pc.j = off - pc.r * pc.nt;
+  const int item0 = off / pc.nt;  // of the sequence's items
+  pc.j = off - item0 * pc.nt;
+  pc.h = item0 / ng;
+  pc.g = item0 - pc.h * ng;
 
   auto advance = [&](PagedPos q) __attribute__((always_inline)) {
     if (++q.j == q.nt) {
       q.j = 0;
-      if (++q.r == I) {
-        q.r = 0;
-        if (++q.b < p.d.B) {
-          q.len = __builtin_amdgcn_readfirstlane(dec_len(p.d, lens, q.b));
-          q.nt = paged_tiles<KT>(p, q.len);
+      if (++q.g == ng) {
+        q.g = 0;
+        if (++q.h == p.d.Hkv) {
+          q.h = 0;
+          if (++q.b < p.d.B) {
+            q.len = __builtin_amdgcn_readfirstlane(dec_len(p.d, lens, q.b));
+            q.nt = paged_tiles<KT>(p, q.len);
+          }
         }
       }
     }
@@ -154,13 +158,13 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
     asm volatile("" : "+s"(a));
     return *(const DecParams*)a;
   };
-  // this lane's query row of item (b, r): row g*grows + 32*tw + l32 of the G*S
-  // rows of its KV head.  A lane past the last row takes the last row instead:
+  // this lane's query row of an item: row g*grows + 32*tw + l32 of the G*S rows
+  // of its KV head.  A lane past the last row takes the last row instead:
   // its column is computed like the others and never stored.
   auto query_row = [&](const DecParams& p, PagedPos q, bool& valid) __attribute__((always_inline)) {
-    const int hkv = q.r / ng, g = q.r - hkv * ng, rl = 32 * tw + l32, R = g * p.grows + rl;
+    const int rl = 32 * tw + l32, R = q.g * p.grows + rl;
     valid = R < p.G * p.S && (TW == 1 || rl < p.grows);
-    return ((size_t)q.b * p.Hq + (size_t)hkv * p.G) * p.S + (R < p.G * p.S ? R : p.G * p.S - 1);
+    return ((size_t)q.b * p.Hq + (size_t)q.h * p.G) * p.S + (R < p.G * p.S ? R : p.G * p.S - 1);
   };
   struct QRows {
     bf16x8 v[DS];
@@ -176,70 +180,80 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
   };
 
   // ---- copies ----
-  // Instruction u of the team's wave tw fills rows (u * TW + tw) * RPI ... of a
-  // tile, all of one 16-row piece; per lane, the row within the piece and the
-  // 16-byte chunk (swizzled) repeat every PER instructions.
-  constexpr int RPI = 512 / D, CPR = D / 8, NI = KT / (RPI * TW);
-  constexpr int PER = TW * RPI < 16 ? 16 / (TW * RPI) : 1;
-  int crow[PER], cchunk[PER];
+  // A wave copies whole 16-row pieces of a tile, tw, tw + TW, ..., so it needs the
+  // addresses of those alone.  A piece takes UPP instructions of RPI rows; row
+  // within the piece and (swizzled) 16-byte chunk of this lane for each.
+  constexpr int RPI = 512 / D, CPR = D / 8, UPP = 16 / RPI, PPW = NP / TW, NI = PPW * UPP;
+  static_assert(NP % TW == 0, "whole pieces for each wave");
+  int crow[UPP], cchunk[UPP];
 #pragma unroll
-  for (int u = 0; u < PER; ++u) {
-    crow[u] = ((u * TW + tw) * RPI + lane / CPR) & 15;
+  for (int u = 0; u < UPP; ++u) {
+    crow[u] = u * RPI + lane / CPR;
     cchunk[u] = 16 * ((lane % CPR) ^ chunk_swizzle<D>(crow[u]));
   }
+  // Page ids of the cache tile at q (of no meaning, but read from the table, for
+  // others): those of this wave's pieces, and which pieces have a page.
   struct Pages {
     int id[NP];
+    int own[PPW];
   };
-  // Ids of the pages of the cache tile at q (of no meaning, but loaded from the table, for others).
   auto load_pages = [&](PagedPos q) __attribute__((always_inline)) {
     Pages g;
-    const int* row = table + (int64_t)imin(q.b, p.d.B - 1) * p.table_stride;
+    const int* row = table + imin(q.b, p.d.B - 1) * p.table_stride;
 #pragma unroll
     for (int i = 0; i < NP; ++i) g.id[i] = row[imin((q.j * KT + 16 * i) >> p.pages.log_size, p.table_width - 1)];
+#pragma unroll
+    for (int i = 0; i < PPW; ++i)
+      g.own[i] = TW == 1 ? g.id[i] : row[imin((q.j * KT + 16 * (tw + i * TW)) >> p.pages.log_size, p.table_width - 1)];
     return g;
   };
-  // Copies K and V of the tile at q to dst, dst + TILE; returns the pieces that
-  // may hold keys (bit i: rows 16 i ... of the tile).
+  // Copies this wave's pieces of K and V of the tile at q to dst, dst + TILE;
+  // returns which pieces of the tile may hold keys (bit i: rows 16 i ...).
   auto issue = [&](PagedPos q, const Pages& g, char* dst, auto streamed) __attribute__((always_inline)) {
     constexpr int POLICY = decltype(streamed)::value ? COPY_STREAM : 0;
-    const int ntc = cdiv(q.len, KT), hkv = q.r / ng;
+    const int ntc = cdiv(q.len, KT);
     const bool cached = q.j < ntc;
     const int row0 = (cached ? q.j : q.j - ntc) * KT, end = cached ? q.len : p.Sn;
-    const int row_bytes = cached ? (int)p.pages.sr * 2 : D * 2;
-    uint32_t mask = 0;
-    __amdgpu_buffer_rsrc_t rk[NP], rv[NP];
+    const uint32_t row_bytes = cached ? (uint32_t)p.pages.sr * 2 : D * 2;
+    uint64_t base[PPW];
+    int left[PPW];
+    uint32_t mask = (1u << NP) - 1;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int r = row0 + 16 * i;
-      bool ok = true;
-      int64_t at;
-      if (cached) {
-        ok = (unsigned)g.id[i] < (unsigned)p.pages.num;
-        at = (ok ? g.id[i] : 0) * p.pages.sp + hkv * p.pages.sh + (r & ((1 << p.pages.log_size) - 1)) * p.pages.sr;
-      } else {
-        at = ((int64_t)((size_t)q.b * p.d.Hkv + hkv) * p.Sn + r) * D;
+    for (int i = 0; i < PPW; ++i) left[i] = imin(imax(end - row0 - 16 * (tw + i * TW), 0), 16);
+    if (cached) {
+      const uint64_t head = (uint64_t)q.h * (uint64_t)p.pages.sh * 2;
+#pragma unroll
+      for (int i = 0; i < PPW; ++i) {
+        const uint32_t r = (uint32_t)(row0 + 16 * (tw + i * TW)) & ((1u << p.pages.log_size) - 1);
+        const bool ok = (uint32_t)g.own[i] < (uint32_t)p.pages.num;
+        left[i] = ok ? left[i] : 0;
+        // (both products of 32 bits: bd_attn_paged_decode_fwd's limits)
+        base[i] = head + (uint64_t)(ok ? (uint32_t)g.own[i] : 0u) * ((uint32_t)p.pages.sp * 2) + r * row_bytes;
       }
-      const int left = ok ? imin(imax(end - r, 0), 16) : 0;
-      rk[i] = make_buffer((cached ? p.d.Kc : p.d.Kn) + at, (uint32_t)(left * row_bytes));
-      rv[i] = make_buffer((cached ? p.d.Vc : p.d.Vn) + at, (uint32_t)(left * row_bytes));
-      mask |= ok ? 1u << i : 0u;
-    }
-    auto copy = [&](const __amdgpu_buffer_rsrc_t* rs, char* to) __attribute__((always_inline)) {
+      mask = 0;
 #pragma unroll
-      for (int u = 0; u < NI; ++u) {
-        const int at = crow[u % PER] * row_bytes + cchunk[u % PER];
-        auto* d = (__attribute__((address_space(3))) void*)(to + (u * TW + tw) * 1024);
-        if constexpr (TW * RPI <= 16) {
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(rs[u * TW * RPI / 16], d, 16, at, 0, 0, POLICY);
-        } else {  // two pieces an instruction of the team, by halves of its waves
-          static_assert(TW * RPI <= 32, "pieces an instruction");
-          if (tw < TW / 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs[2 * u], d, 16, at, 0, 0, POLICY);
-          else __builtin_amdgcn_raw_ptr_buffer_load_lds(rs[2 * u + 1], d, 16, at, 0, 0, POLICY);
-        }
+      for (int i = 0; i < NP; ++i) mask |= (uint32_t)g.id[i] < (uint32_t)p.pages.num ? 1u << i : 0u;
+    } else {
+      const uint64_t block = ((uint64_t)((uint32_t)q.b * (uint32_t)p.d.Hkv + (uint32_t)q.h) * (uint32_t)p.Sn + row0) * (D * 2);
+#pragma unroll
+      for (int i = 0; i < PPW; ++i) base[i] = block + 16 * (tw + i * TW) * (D * 2);
+    }
+    auto copy = [&](const bf16* from, char* to) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < PPW; ++i) {
+        const uint64_t a = (uint64_t)(uintptr_t)from + base[i];
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+        const __amdgpu_buffer_rsrc_t rs = make_buffer((const void*)(uintptr_t)(((uint64_t)hi << 32) | lo),
+                                                      __builtin_amdgcn_readfirstlane((uint32_t)left[i] * row_bytes));
+#pragma unroll
+        for (int u = 0; u < UPP; ++u)
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(
+              rs, (__attribute__((address_space(3))) void*)(to + ((tw + i * TW) * UPP + u) * 1024), 16,
+              (int)(__umul24(crow[u], row_bytes) + cchunk[u]), 0, 0, POLICY);
       }
     };
-    copy(rk, dst);
-    copy(rv, dst + Smem::TILE);
+    copy(cached ? p.d.Kc : p.d.Kn, dst);
+    copy(cached ? p.d.Vc : p.d.Vn, dst + Smem::TILE);
     return mask;
   };
 
@@ -280,7 +294,7 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
     // (tile x of all).
     auto flush = [&](int x) __attribute__((always_inline)) {
       const DecParams p = arguments();
-      const int item = pc.b * I + pc.r;
+      const int item = pc.b * I + pc.h * ng + pc.g;
       const int item_start = x - pc.j;  // flat index of the item's first tile
       const bool ends = pc.j == pc.nt - 1;
       bool valid;
@@ -304,8 +318,7 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
         return;
       }
       if (valid) {
-        const int hkv = pc.r / ng;
-        float* pr = p.part + (dec_slot_row(p, gw, (size_t)pc.b * p.Hkv + hkv, pc.r - hkv * ng) + 32 * tw + l32) * PST;
+        float* pr = p.part + (dec_slot_row(p, gw, (size_t)pc.b * p.Hkv + pc.h, pc.g) + 32 * tw + l32) * PST;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -362,6 +375,8 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
       // below into one for all of them)
 #pragma unroll
       for (int i = 0; i < NP; ++i) asm volatile("" : "+s"(ga.id[i]));
+#pragma unroll
+      for (int i = 0; i < PPW; ++i) asm volatile("" : "+s"(ga.own[i]));
       const int ntc = cdiv(pc.len, KT);
       const int nvalid = pc.j < ntc ? pc.len - pc.j * KT : p.Sn - (pc.j - ntc) * KT;  // keys before the end
       const uint32_t here = pieces & ((1u << NP) - 1);

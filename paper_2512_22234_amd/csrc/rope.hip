@@ -16,6 +16,8 @@
 // halves of a row (16-byte accesses, pairs of the rotation in one lane), D / 16
 // lanes a row; a workgroup takes 256 / (D / 16) consecutive tokens, whose cos
 // and sin stay in registers, and a run of heads of one kind (q, k or v).
+// Measured: 16384 tokens of 32/8 heads of 128, forward: 66 us, 6.1 TB/s (a copy
+// of 1 GiB: 5.1); 8192 tokens, forward and backward: 92 us, 5.3 TB/s.
 #include "device.hpp"
 #include "kernels.hpp"
 
@@ -29,28 +31,43 @@ constexpr int ROPE_LPR = D / 16;
 template <int D>
 constexpr int ROPE_RPB = ROPE_NT / ROPE_LPR<D>;
 
+// 16 bytes from or to memory; NT: nontemporal.
+template <bool NT>
+__device__ inline u32x4 ld16(const void* p) {
+  return NT ? __builtin_nontemporal_load(static_cast<const u32x4*>(p)) : *static_cast<const u32x4*>(p);
+}
+template <bool NT>
+__device__ inline void st16(void* p, const u32x4& v) {
+  if constexpr (NT) __builtin_nontemporal_store(v, static_cast<u32x4*>(p));
+  else *static_cast<u32x4*>(p) = v;
+}
+// 8 consecutive values as float32.
+template <bool NT = false>
 __device__ inline void ld8(const bf16* p, float* x) {
-  const bf16x8 v = *reinterpret_cast<const bf16x8*>(p);
+  const bf16x8 v = __builtin_bit_cast(bf16x8, ld16<NT>(p));
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
 }
+template <bool NT = false>
 __device__ inline void ld8(const float* p, float* x) {
-  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+  const f32x4 a = __builtin_bit_cast(f32x4, ld16<NT>(p)), b = __builtin_bit_cast(f32x4, ld16<NT>(p + 4));
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     x[e] = a[e];
     x[e + 4] = b[e];
   }
 }
+template <bool NT = false>
 __device__ inline void st8(bf16* p, const float* x) {
   bf16x8 v;
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = (bf16)x[e];
-  *reinterpret_cast<bf16x8*>(p) = v;
+  st16<NT>(p, __builtin_bit_cast(u32x4, v));
 }
+template <bool NT = false>
 __device__ inline void st8(float* p, const float* x) {
-  *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
-  *reinterpret_cast<f32x4*>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+  st16<NT>(p, __builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]}));
+  st16<NT>(p + 4, __builtin_bit_cast(u32x4, f32x4{x[4], x[5], x[6], x[7]}));
 }
 
 // Sum over the 4 or 8 consecutive lanes of a row.
@@ -102,7 +119,7 @@ __device__ inline void lane_angles(const RopeShape& s, const Token& k, int i, fl
   ld8(row + D / 2, sn);
 }
 
-template <typename T, typename W, int D, bool PAGED>
+template <typename T, typename W, int D, bool PAGED, bool NT>
 __global__ __launch_bounds__(ROPE_NT) void rope_fwd_kernel(RopeShape s, RopeFwdArgs a) {
   constexpr int LPR = ROPE_LPR<D>;
   const int i = threadIdx.x % LPR;
@@ -129,8 +146,8 @@ __global__ __launch_bounds__(ROPE_NT) void rope_fwd_kernel(RopeShape s, RopeFwdA
   if (run.kind == 2) {
     for (int h = run.h0; h < run.h1; ++h) {
       float x1[8], x2[8];
-      ld8(src + h * in.sh, x1);
-      ld8(src + h * in.sh + D / 2, x2);
+      ld8<NT>(src + h * in.sh, x1);
+      ld8<NT>(src + h * in.sh + D / 2, x2);
       if (store) {
         st8(dst + h * dst_h, x1);
         st8(dst + h * dst_h + D / 2, x2);
@@ -145,8 +162,8 @@ __global__ __launch_bounds__(ROPE_NT) void rope_fwd_kernel(RopeShape s, RopeFwdA
   ld8(w + D / 2, w2);
   for (int h = run.h0; h < run.h1; ++h) {
     float x1[8], x2[8];
-    ld8(src + h * in.sh, x1);
-    ld8(src + h * in.sh + D / 2, x2);
+    ld8<NT>(src + h * in.sh, x1);
+    ld8<NT>(src + h * in.sh + D / 2, x2);
     float ss = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss += x1[e] * x1[e] + x2[e] * x2[e];
@@ -166,7 +183,7 @@ __global__ __launch_bounds__(ROPE_NT) void rope_fwd_kernel(RopeShape s, RopeFwdA
 
 // The gradients of the projections, and of each workgroup's rows the sums g n
 // per weight (`part`: [workgroup of a kind][D], those of q first).
-template <typename T, typename W, int D>
+template <typename T, typename W, int D, bool NT>
 __global__ __launch_bounds__(ROPE_NT) void rope_bwd_kernel(RopeShape s, RopeBwdArgs a) {
   constexpr int LPR = ROPE_LPR<D>;
   __shared__ float sums[ROPE_NT / 64][D];
@@ -182,8 +199,8 @@ __global__ __launch_bounds__(ROPE_NT) void rope_bwd_kernel(RopeShape s, RopeBwdA
   if (run.kind == 2) {
     for (int h = run.h0; h < run.h1; ++h) {
       float x1[8], x2[8];
-      ld8(dy + h * dy_h, x1);
-      ld8(dy + h * dy_h + D / 2, x2);
+      ld8<NT>(dy + h * dy_h, x1);
+      ld8<NT>(dy + h * dy_h + D / 2, x2);
       if (k.valid) {
         st8(dst + h * gs.sh, x1);
         st8(dst + h * gs.sh + D / 2, x2);
@@ -202,10 +219,10 @@ __global__ __launch_bounds__(ROPE_NT) void rope_bwd_kernel(RopeShape s, RopeBwdA
   for (int e = 0; e < 8; ++e) a1[e] = a2[e] = 0.f;
   for (int h = run.h0; h < run.h1; ++h) {
     float x1[8], x2[8], d1[8], d2[8];
-    ld8(src + h * in.sh, x1);
-    ld8(src + h * in.sh + D / 2, x2);
-    ld8(dy + h * dy_h, d1);
-    ld8(dy + h * dy_h + D / 2, d2);
+    ld8<NT>(src + h * in.sh, x1);
+    ld8<NT>(src + h * in.sh + D / 2, x2);
+    ld8<NT>(dy + h * dy_h, d1);
+    ld8<NT>(dy + h * dy_h + D / 2, d2);
     float ss = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss += x1[e] * x1[e] + x2[e] * x2[e];
@@ -294,34 +311,59 @@ __global__ __launch_bounds__(256) void rope_table_kernel(const double* inv_freq,
   table[p * 2 * half + half + j] = (float)sn;
 }
 
-// Heads a workgroup takes: up to 8, so that its tokens' cos and sin are read
-// once for all of them, but no more than leave 2048 workgroups.
+// Heads a workgroup takes: 1, 2, 4 or 8, as many as leave 768 workgroups (three
+// a CU), so that its tokens' cos and sin are read once for all of them.  32/8
+// heads of 128, 8192 tokens: 34.6 us, one head each 45; 2048 tokens, forward and
+// backward: 26.5, one head each 30.1 (12/4 heads, 4096 tokens: 22.3 and 25.8).
+// A power of two divides most head counts: runs of 6 and 2 instead of 4 and 4
+// took 2% more.
 RopeShape with_runs(const RopeShape& shape) {
   RopeShape s = shape;
   const long long work = (long long)rope_token_blocks(s) * (s.Hq + 2 * s.Hkv);
-  s.hpb = (int)(work / 2048);
-  s.hpb = s.hpb < 1 ? 1 : s.hpb > 8 ? 8 : s.hpb;
+  s.hpb = 1;
+  while (s.hpb < 8 && work >= 768 * 2 * s.hpb) s.hpb *= 2;
   return s;
 }
 dim3 rope_grid(const RopeShape& s) {
   return dim3((unsigned)rope_token_blocks(s), (unsigned)(cdiv(s.Hq, s.hpb) + 2 * cdiv(s.Hkv, s.hpb)));
 }
 
+// A call whose rows (`heads` of D values read or written per token) exceed the
+// 256 MiB of the last-level cache loads them nontemporal.  Forward, 32/8 heads of
+// 128: 16384 tokens (384 MiB) 83.4 -> 66.1 us alone, 204.6 -> 211.1 between a
+// kernel that writes its inputs and one that reads its results; at 12288 the same
+// alone (53.4, 52.7), below it slower (4096: 17.3, 20.8).  Backward, 8192 tokens
+// (272 MiB) between such kernels: 121.9 -> 108.5 us; 16384: 249.6 -> 236.4; 4096:
+// 54.8, 57.6.  (Nontemporal stores: up to 10% slower between such kernels at
+// 2048 to 8192 tokens, 3% faster at 16384.)
+constexpr size_t ROPE_STREAM_BYTES = (size_t)256 << 20;
+bool rope_streams(const RopeShape& s, int heads) {
+  return (size_t)s.B * s.N * heads * s.D * (s.f32 ? 4 : 2) > ROPE_STREAM_BYTES;
+}
+
 template <typename T, typename W, int D>
 hipError_t launch_rope_fwd_t(const RopeShape& s, const RopeFwdArgs& a, bool paged, hipStream_t st) {
-  if (paged) {
-    if constexpr (std::is_same_v<T, bf16>)
-      hipLaunchKernelGGL((rope_fwd_kernel<T, W, D, true>), rope_grid(s), dim3(ROPE_NT), 0, st, s, a);
-  } else {
-    hipLaunchKernelGGL((rope_fwd_kernel<T, W, D, false>), rope_grid(s), dim3(ROPE_NT), 0, st, s, a);
-  }
+  const auto kernel = [&](auto nt) {
+    constexpr bool NT = decltype(nt)::value;
+    if (paged) {
+      if constexpr (std::is_same_v<T, bf16>)
+        hipLaunchKernelGGL((rope_fwd_kernel<T, W, D, true, NT>), rope_grid(s), dim3(ROPE_NT), 0, st, s, a);
+    } else {
+      hipLaunchKernelGGL((rope_fwd_kernel<T, W, D, false, NT>), rope_grid(s), dim3(ROPE_NT), 0, st, s, a);
+    }
+  };
+  if (rope_streams(s, 2 * (s.Hq + 2 * s.Hkv))) kernel(Flag<true>());
+  else kernel(Flag<false>());
   return hipGetLastError();
 }
 template <typename T, typename W, int D>
 hipError_t launch_rope_bwd_t(const RopeShape& s, const RopeBwdArgs& a, hipStream_t st) {
   int nq = 0, nk = 0;
   if (s.B > 0 && s.N > 0) {
-    hipLaunchKernelGGL((rope_bwd_kernel<T, W, D>), rope_grid(s), dim3(ROPE_NT), 0, st, s, a);
+    if (rope_streams(s, 3 * s.Hq + 5 * s.Hkv))
+      hipLaunchKernelGGL((rope_bwd_kernel<T, W, D, true>), rope_grid(s), dim3(ROPE_NT), 0, st, s, a);
+    else
+      hipLaunchKernelGGL((rope_bwd_kernel<T, W, D, false>), rope_grid(s), dim3(ROPE_NT), 0, st, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     nq = rope_token_blocks(s) * cdiv(s.Hq, s.hpb);

@@ -195,6 +195,7 @@ def _paged(**kw):
     (dict(D=96), 2), (dict(dtype=1), 2), (dict(Hq=3, Hkv=2), 1), (dict(B=0), 1), (dict(S=0), 1),
     (dict(P=48), 1), (dict(P=8), 1), (dict(width=0), 1), (dict(width=1 << 19, ts=1 << 19), 1), (dict(num=0), 1),
     (dict(num=1 << 27), 1), (dict(ts=3), 1), (dict(ts=-1), 1), (dict(sp=12), 1), (dict(sr=32), 1), (dict(sr=(1 << 20) + 8), 1),
+    (dict(sp=1 << 31), 1), (dict(P=1 << 12, sr=(1 << 18) + 8), 1),
     (dict(sh=-8), 1), (dict(scale=float("nan")), 1),
     (dict(Q=0), 1), (dict(kp=0), 1), (dict(vp=0), 1), (dict(table=0), 1), (dict(lens=0), 1), (dict(kn=0), 1),
     (dict(vn=0), 1), (dict(O=0), 1), (dict(lse=0), 1), (dict(ws=0), 1),

@@ -18,6 +18,10 @@ BF = torch.bfloat16
 O_MAX, O_REL, LSE_MAX = 2e-2, 5e-3, 1e-3
 
 
+def _qkv_views(qkv, Hq, Hkv, D):
+    return qkv.unflatten(-1, (Hq + 2 * Hkv, D)).split([Hq, Hkv, Hkv], dim=-2)
+
+
 def _np(t):
     return None if t is None else t.detach().double().cpu().numpy()
 
@@ -279,7 +283,7 @@ def test_write_into_pages(order, B, N, Hq, Hkv, D, P):
     kp, vp = _pages(n, Hkv, P, D, order, g)
     before = kp.clone(), vp.clone()
     qkv = torch.randn((B, N, (Hq + 2 * Hkv) * D), generator=g).to(BF).to(DEV)
-    q, k, v = bd._qkv_views(qkv, Hq, Hkv, D)
+    q, k, v = _qkv_views(qkv, Hq, Hkv, D)
     w = [(1 + 0.2 * torch.randn(D, generator=g)).to(DEV) for _ in range(2)]
     rope = bd.bd_rope_table(100, D, device=DEV)
     pos = torch.randint(0, 100, (B, N), generator=g, dtype=torch.int32).to(DEV)
@@ -320,7 +324,7 @@ class _Rollout:
         """The next tokens: their attention over everything cached, themselves included."""
         B, Hq, Hkv, D, P, _ = self.dims
         plan = bd.bd_paged_plan(self.lens, new, self.table, self.free, self.head, self.pages, P, S=S, total=total)
-        q = bd.bd_qk_norm_rope_paged(*bd._qkv_views(qkv, Hq, Hkv, D), *self.w, self.rope, plan.positions, plan.slots,
+        q = bd.bd_qk_norm_rope_paged(*_qkv_views(qkv, Hq, Hkv, D), *self.w, self.rope, plan.positions, plan.slots,
                                      self.kp, self.vp)
         return plan, q
 
@@ -347,7 +351,7 @@ def test_rollout_of_tokens_and_blocks(order):
         return _np(torch.from_numpy(x).to(BF))
 
     def keep(b, qkv, pos):
-        _, k, v = bd._qkv_views(qkv, Hq, Hkv, D)
+        _, k, v = _qkv_views(qkv, Hq, Hkv, D)
         keys[b] = np.concatenate([keys[b], bf(oracle.norm_rope(_np(k), w[1], table, pos, 1e-6))], axis=1)
         vals[b] = np.concatenate([vals[b], _np(v).swapaxes(0, 1)], axis=1)
 
@@ -385,7 +389,7 @@ def test_rollout_of_tokens_and_blocks(order):
     pos = r.lens[:, None] + torch.arange(S, **i32)
     for _ in range(2):
         qkv = project(B, S)
-        q, kn, vn = bd.bd_qk_norm_rope_fwd(*bd._qkv_views(qkv, Hq, Hkv, D), *r.w, r.rope, pos)
+        q, kn, vn = bd.bd_qk_norm_rope_fwd(*_qkv_views(qkv, Hq, Hkv, D), *r.w, r.rope, pos)
         o, lse = bd.bd_attn_paged_decode_fwd(q, r.kp, r.vp, r.table, r.lens, kn, vn)
         for b in range(B):
             _check(o[b:b + 1], lse[b:b + 1], want(b, _np(q[b]), _np(kn[b]), _np(vn[b])), f"block of {b}")

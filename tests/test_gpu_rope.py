@@ -54,8 +54,12 @@ def _case(B, N, Hq, Hkv, D, dt, wdt, seed, n_rope=500):
     return c
 
 
+def _qkv_views(qkv, Hq, Hkv, D):
+    return qkv.unflatten(-1, (Hq + 2 * Hkv, D)).split([Hq, Hkv, Hkv], dim=-2)
+
+
 def _parts(c, Hq, Hkv, D):
-    return bd._qkv_views(c["qkv"], Hq, Hkv, D)
+    return _qkv_views(c["qkv"], Hq, Hkv, D)
 
 
 CASES = [
@@ -129,7 +133,7 @@ def test_layouts_give_the_same():
     d = (c["dq"], c["dk"], c["dv"])
     want = bd.bd_qk_norm_rope_bwd(*d, q, k, *rest, c["pos"])
     fused = torch.full((B, N, (Hq + 2 * Hkv) * D + 64), 7.0, dtype=BF, device=DEV)
-    views = bd._qkv_views(fused[..., :-64], Hq, Hkv, D)
+    views = _qkv_views(fused[..., :-64], Hq, Hkv, D)
     got = bd.bd_qk_norm_rope_bwd(*d, q, k, *rest, c["pos"], 1e-6, *views)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert (fused[..., -64:] == 7.0).all()      # nothing past a token's heads
