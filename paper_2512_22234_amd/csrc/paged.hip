@@ -26,18 +26,30 @@
 namespace bd {
 namespace {
 
-struct PagedParams {
-  DecParams d;  // Kc, Vc: the pages; C: the table's room in keys
-  int Sn;       // the block's own keys (0: none)
-  int table_width;
+// What the copies of a tile need, in bytes.
+struct PagedTile {
+  uint64_t kp, vp, kn, vn;  // addresses: pages, block
+  uint64_t table;           // ... page table
   int64_t table_stride;
-  PageLayout pages;
+  int64_t sh;               // head stride of the pages
+  uint32_t sp, sr;          // page and row stride of the pages
+  int num, log_size;        // pages, log2 of their rows
+  int last;                 // last entry of a table row
+};
+struct PagedParams {
+  DecParams d;  // C: the table's room in keys
+  PagedTile t;
+  int Sn;  // the block's own keys (0: none)
 };
 
 // Key tiles of an item of a sequence with cache length len.
 template <int KT>
+__device__ inline int tiles_of(int keys) {
+  return (int)((unsigned)(keys + KT - 1) / KT);
+}
+template <int KT>
 __device__ inline int paged_tiles(const PagedParams& p, int len) {
-  return imax(cdiv(len, KT) + cdiv(p.Sn, KT), 1);
+  return imax(tiles_of<KT>(len) + tiles_of<KT>(p.Sn), 1);
 }
 
 template <int D, int TW, int KT, int NST>
@@ -56,11 +68,10 @@ struct PagedPos {
   int b, len, nt, h, g, j;
 };
 
-// `lens` and `table` are the parameters' arrays as restrict kernel arguments, read
-// through the scalar cache where the index is uniform.
+// `lens` is the parameters' array as a restrict kernel argument, read through the
+// scalar cache where the index is uniform.
 template <int D, int TW, int KT, int NST>
-__global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(PagedParams p, const int* __restrict__ lens,
-                                                                           const int* __restrict__ table) {
+__global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(PagedParams p, const int* __restrict__ lens) {
   constexpr int DS = D / 16, DB = D / 32, PST = D + 4, KB = KT / 32;
   using Smem = PagedSmem<D, TW, KT, NST>;
   constexpr int TEAMS = Smem::TEAMS, NW = Smem::NW, NT = 64 * NW;
@@ -158,6 +169,14 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
     asm volatile("" : "+s"(a));
     return *(const DecParams*)a;
   };
+  // Those of a tile's copies, read at the start of each step in one go: kept, they
+  // would push the loop's own state out of the scalar registers, and read one by
+  // one where they are needed, each costs a wait.
+  auto tile_arguments = [&]() __attribute__((always_inline)) -> PagedTile {
+    auto* a = (const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(PagedParams, t);
+    asm volatile("" : "+s"(a));
+    return *(const PagedTile*)(const __attribute__((address_space(4))) PagedTile*)a;
+  };
   // this lane's query row of an item: row g*grows + 32*tw + l32 of the G*S rows
   // of its KV head.  A lane past the last row takes the last row instead:
   // its column is computed like the others and never stored.
@@ -192,56 +211,72 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
     cchunk[u] = 16 * ((lane % CPR) ^ chunk_swizzle<D>(crow[u]));
   }
   // Page ids of the cache tile at q (of no meaning, but read from the table, for
-  // others): those of this wave's pieces, and which pieces have a page.
+  // others): those of this wave's pieces, and of all, to know which have a page.
+  // (vectors, not arrays, which the branch below would leave in memory)
+  typedef int Ids __attribute__((ext_vector_type(NP)));
+  typedef int Own __attribute__((ext_vector_type(PPW < 2 ? 2 : PPW)));
   struct Pages {
-    int id[NP];
-    int own[PPW];
+    Ids id;
+    Own own;
   };
-  auto load_pages = [&](PagedPos q) __attribute__((always_inline)) {
+  auto load_pages = [&](const PagedTile& t, PagedPos q) __attribute__((always_inline)) {
     Pages g;
-    const int* row = table + imin(q.b, p.d.B - 1) * p.table_stride;
+    // (constant address space: scalar loads; nothing writes the table while the kernel runs)
+    auto* row = (const __attribute__((address_space(4))) int*)(t.table + (int64_t)imin(q.b, p.d.B - 1) * t.table_stride);
+    auto entry = [&](int piece) { return row[(uint32_t)imin((q.j * KT + 16 * piece) >> t.log_size, t.last)]; };
+    if ((1 << t.log_size) >= KT) {  // the tile lies in one page
+      const int id = entry(0);
 #pragma unroll
-    for (int i = 0; i < NP; ++i) g.id[i] = row[imin((q.j * KT + 16 * i) >> p.pages.log_size, p.table_width - 1)];
+      for (int i = 0; i < NP; ++i) g.id[i] = id;
 #pragma unroll
-    for (int i = 0; i < PPW; ++i)
-      g.own[i] = TW == 1 ? g.id[i] : row[imin((q.j * KT + 16 * (tw + i * TW)) >> p.pages.log_size, p.table_width - 1)];
+      for (int i = 0; i < PPW; ++i) g.own[i] = id;
+    } else {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) g.id[i] = entry(i);
+#pragma unroll
+      for (int i = 0; i < PPW; ++i) g.own[i] = TW == 1 ? g.id[i] : entry(tw + i * TW);
+    }
     return g;
   };
   // Copies this wave's pieces of K and V of the tile at q to dst, dst + TILE;
   // returns which pieces of the tile may hold keys (bit i: rows 16 i ...).
-  auto issue = [&](PagedPos q, const Pages& g, char* dst, auto streamed) __attribute__((always_inline)) {
+  auto issue = [&](const PagedTile& t, PagedPos q, const Pages& g, char* dst, auto streamed) __attribute__((always_inline)) {
     constexpr int POLICY = decltype(streamed)::value ? COPY_STREAM : 0;
-    const int ntc = cdiv(q.len, KT);
+    const int ntc = tiles_of<KT>(q.len);
     const bool cached = q.j < ntc;
     const int row0 = (cached ? q.j : q.j - ntc) * KT, end = cached ? q.len : p.Sn;
-    const uint32_t row_bytes = cached ? (uint32_t)p.pages.sr * 2 : D * 2;
-    uint64_t base[PPW];
+    const uint32_t row_bytes = cached ? t.sr : D * 2;
+    uint64_t base[PPW], kp, vp;
     int left[PPW];
     uint32_t mask = (1u << NP) - 1;
 #pragma unroll
     for (int i = 0; i < PPW; ++i) left[i] = imin(imax(end - row0 - 16 * (tw + i * TW), 0), 16);
     if (cached) {
-      const uint64_t head = (uint64_t)q.h * (uint64_t)p.pages.sh * 2;
-#pragma unroll
-      for (int i = 0; i < PPW; ++i) {
-        const uint32_t r = (uint32_t)(row0 + 16 * (tw + i * TW)) & ((1u << p.pages.log_size) - 1);
-        const bool ok = (uint32_t)g.own[i] < (uint32_t)p.pages.num;
-        left[i] = ok ? left[i] : 0;
-        // (both products of 32 bits: bd_attn_paged_decode_fwd's limits)
-        base[i] = head + (uint64_t)(ok ? (uint32_t)g.own[i] : 0u) * ((uint32_t)p.pages.sp * 2) + r * row_bytes;
-      }
+      kp = t.kp;
+      vp = t.vp;
+      const uint64_t head = (uint64_t)q.h * (uint64_t)t.sh;
       mask = 0;
 #pragma unroll
-      for (int i = 0; i < NP; ++i) mask |= (uint32_t)g.id[i] < (uint32_t)p.pages.num ? 1u << i : 0u;
+      for (int i = 0; i < NP; ++i) mask |= (uint32_t)g.id[i] < (uint32_t)t.num ? 1u << i : 0u;
+#pragma unroll
+      for (int i = 0; i < PPW; ++i) {
+        const uint32_t r = (uint32_t)(row0 + 16 * (tw + i * TW)) & ((1u << t.log_size) - 1);
+        const bool ok = (uint32_t)g.own[i] < (uint32_t)t.num;
+        left[i] = ok ? left[i] : 0;
+        // (products of 32 bits: bd_attn_paged_decode_fwd's limits)
+        base[i] = head + (uint64_t)(ok ? (uint32_t)g.own[i] : 0u) * t.sp + r * row_bytes;
+      }
     } else {
+      kp = t.kn;
+      vp = t.vn;
       const uint64_t block = ((uint64_t)((uint32_t)q.b * (uint32_t)p.d.Hkv + (uint32_t)q.h) * (uint32_t)p.Sn + row0) * (D * 2);
 #pragma unroll
       for (int i = 0; i < PPW; ++i) base[i] = block + 16 * (tw + i * TW) * (D * 2);
     }
-    auto copy = [&](const bf16* from, char* to) __attribute__((always_inline)) {
+    auto copy = [&](uint64_t from, char* to) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < PPW; ++i) {
-        const uint64_t a = (uint64_t)(uintptr_t)from + base[i];
+        const uint64_t a = from + base[i];
         const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
         const __amdgpu_buffer_rsrc_t rs = make_buffer((const void*)(uintptr_t)(((uint64_t)hi << 32) | lo),
                                                       __builtin_amdgcn_readfirstlane((uint32_t)left[i] * row_bytes));
@@ -252,8 +287,10 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
               (int)(__umul24(crow[u], row_bytes) + cchunk[u]), 0, 0, POLICY);
       }
     };
-    copy(cached ? p.d.Kc : p.d.Kn, dst);
-    copy(cached ? p.d.Vc : p.d.Vn, dst + Smem::TILE);
+    // (taken here, or the compiler selects between their places in memory)
+    asm volatile("" : "+s"(kp), "+s"(vp));
+    copy(kp, dst);
+    copy(vp, dst + Smem::TILE);
     return mask;
   };
 
@@ -274,19 +311,23 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
     reset();
     char* const ring = sm.buf[tm];
     PagedPos pa = pc;  // the next tile to copy, and its pages
-    Pages ga = load_pages(pa);
-    qreg = load_q(pc);
-    // pieces of the tiles in flight, NP bits each, the current tile's lowest
-    uint32_t pieces = issue(pa, ga, ring, streamed);
-    pa = advance(pa);
+    Pages ga;
+    uint32_t pieces;  // pieces of the tiles in flight, NP bits each, the current tile's lowest
+    {
+      const PagedTile t = tile_arguments();
+      ga = load_pages(t, pa);
+      qreg = load_q(pc);
+      pieces = issue(t, pa, ga, ring, streamed);
+      pa = advance(pa);
 #pragma unroll
-    for (int u = 1; u < NST - 1; ++u)
-      if (x0 + u < x1) {
-        ga = load_pages(pa);
-        pieces |= issue(pa, ga, ring + u * 2 * Smem::TILE, streamed) << (NP * u);
-        pa = advance(pa);
-      }
-    ga = load_pages(pa);
+      for (int u = 1; u < NST - 1; ++u)
+        if (x0 + u < x1) {
+          ga = load_pages(t, pa);
+          pieces |= issue(t, pa, ga, ring + u * 2 * Smem::TILE, streamed) << (NP * u);
+          pa = advance(pa);
+        }
+      ga = load_pages(t, pa);
+    }
     // Teams: the query rows have landed once all but the newest tile have.
     if (TW > 1) wait_global_loads_but<2 * NI>();
 
@@ -340,12 +381,13 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
     auto step = [&](const char* __restrict__ cur, char* __restrict__ nxt, PagedPos pn, bool more, bool copies,
                     bool new_item) __attribute__((always_inline)) {
       compute_fence();  // the reads of the buffer about to be refilled are done
+      const PagedTile t = tile_arguments();
       if constexpr (TW == 1) {
         // (query rows of the next item: a tile ahead, behind the wait, in both branches, as over a dense cache)
         if (copies) {
-          pieces |= issue(pa, ga, nxt, streamed) << (NP * (NST - 1));
+          pieces |= issue(t, pa, ga, nxt, streamed) << (NP * (NST - 1));
           pa = advance(pa);
-          ga = load_pages(pa);
+          ga = load_pages(t, pa);
           wait_global_loads_but<(NST - 1) * 2 * NI>();  // the tile at pc has landed (this wave's own copy)
           if (new_item) qreg = qnext;
           if (pn.j == 0) qnext = load_q(pn);
@@ -366,9 +408,9 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
         barrier_lds_only();  // ... every wave's; and all are done with `nxt`
         if (more && pn.j == 0) qnext = load_q(pn);
         if (copies) {
-          pieces |= issue(pa, ga, nxt, streamed) << (NP * (NST - 1));
+          pieces |= issue(t, pa, ga, nxt, streamed) << (NP * (NST - 1));
           pa = advance(pa);
-          ga = load_pages(pa);
+          ga = load_pages(t, pa);
         }
       }
       // (the page ids are waited for here: a scalar load in flight would turn every wait for an LDS read
@@ -377,7 +419,7 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
       for (int i = 0; i < NP; ++i) asm volatile("" : "+s"(ga.id[i]));
 #pragma unroll
       for (int i = 0; i < PPW; ++i) asm volatile("" : "+s"(ga.own[i]));
-      const int ntc = cdiv(pc.len, KT);
+      const int ntc = tiles_of<KT>(pc.len);
       const int nvalid = pc.j < ntc ? pc.len - pc.j * KT : p.Sn - (pc.j - ntc) * KT;  // keys before the end
       const uint32_t here = pieces & ((1u << NP) - 1);
       pieces >>= NP;
@@ -460,20 +502,17 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
 }
 
 template <int D, int TW, int KT, int NST>
-void launch_paged_kernel(const PagedParams& p, const int* table, hipStream_t st) {
+void launch_paged_kernel(const PagedParams& p, hipStream_t st) {
   using Smem = PagedSmem<D, TW, KT, NST>;
   hipLaunchKernelGGL((paged_kernel<D, TW, KT, NST>), dim3(p.d.runs / Smem::TEAMS), dim3(64 * Smem::NW), 0, st, p,
-                     p.d.cache_lens, table);
+                     p.d.cache_lens);
 }
 
 template <int D>
 hipError_t launch_paged_d(const DecodeShape& s, const PagedArgs& a, void* ws, hipStream_t st) {
   PagedParams p;
   p.d.Q = static_cast<const bf16*>(a.Q);
-  p.d.Kc = static_cast<const bf16*>(a.Kp);
-  p.d.Vc = static_cast<const bf16*>(a.Vp);
-  p.d.Kn = static_cast<const bf16*>(a.Kn);
-  p.d.Vn = static_cast<const bf16*>(a.Vn);
+  p.d.Kc = p.d.Vc = p.d.Kn = p.d.Vn = nullptr;  // (the copies' own arguments: t)
   p.d.cache_lens = a.cache_lens;
   p.d.O = static_cast<bf16*>(a.O);
   p.d.LSE = a.LSE;
@@ -492,12 +531,21 @@ hipError_t launch_paged_d(const DecodeShape& s, const PagedArgs& a, void* ws, hi
   p.d.hrows = DEC_QT * decode_query_tiles(s);
   p.d.runs = g.runs;
   p.Sn = a.Kn ? s.S : 0;
-  p.table_width = a.width;
-  p.table_stride = a.table_stride;
-  p.pages = a.pages;
-  if (g.waves == 1) launch_paged_kernel<D, 1, 32, 2>(p, a.table, st);
-  else if (g.waves == 2) launch_paged_kernel<D, 2, (D == 64 ? 64 : 32), 4>(p, a.table, st);
-  else launch_paged_kernel<D, 4, 64, 512 / D>(p, a.table, st);
+  p.t.kp = (uint64_t)(uintptr_t)a.Kp;
+  p.t.vp = (uint64_t)(uintptr_t)a.Vp;
+  p.t.kn = (uint64_t)(uintptr_t)a.Kn;
+  p.t.vn = (uint64_t)(uintptr_t)a.Vn;
+  p.t.table = (uint64_t)(uintptr_t)a.table;
+  p.t.table_stride = a.table_stride * 4;
+  p.t.sh = a.pages.sh * 2;
+  p.t.sp = (uint32_t)(a.pages.sp * 2);
+  p.t.sr = (uint32_t)(a.pages.sr * 2);
+  p.t.num = a.pages.num;
+  p.t.log_size = a.pages.log_size;
+  p.t.last = a.width - 1;
+  if (g.waves == 1) launch_paged_kernel<D, 1, 32, 2>(p, st);
+  else if (g.waves == 2) launch_paged_kernel<D, 2, (D == 64 ? 64 : 32), 4>(p, st);
+  else launch_paged_kernel<D, 4, 64, 512 / D>(p, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   return launch_dec_combine<D, true>(s, g, p.d, st);
