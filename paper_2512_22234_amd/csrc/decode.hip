@@ -445,7 +445,7 @@ hipError_t launch_decode_d(const DecodeShape& s, const void* Q, const void* Kc, 
   else launch_dec_kernel<D, 4, 64, 512 / D>(p, st);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  return launch_dec_combine<D, false>(s, g, p, st);
+  return launch_dec_combine<D, false, false>(s, g, p, st);
 }
 
 }  // namespace

@@ -101,15 +101,23 @@ constexpr float DEC_SLACK = 8.0f;
 // thread takes the few runs of each (64 sequences: 6.2 us either way).
 // EMPTY: a run may hold no key of its item (m_r = -inf, l_r = 0), and so may all
 // of them (O = 0, LSE = -inf).
-template <int D, int P, bool EMPTY>
-__global__ __launch_bounds__(256) void dec_combine_kernel(DecParams p) {
-  constexpr int TPR = D / 4, PST = D + 4, RPW = 256 / (TPR * P);  // rows per workgroup
+// COLS: each 32 rows of a slot lie as [D / 4][32] float4, then [32] pairs (max,
+// sum), in place of rows of D + 4 floats (paged_kernel's teams); consecutive
+// threads take consecutive rows, eight at least in a workgroup, so that they read
+// whole cache lines.
+template <int P, bool COLS>
+constexpr int DEC_MERGE_THREADS = COLS && P > 1 ? 1024 : 256;  // of a workgroup
+template <int D, int P, bool EMPTY, bool COLS>
+__global__ __launch_bounds__((DEC_MERGE_THREADS<P, COLS>)) void dec_combine_kernel(DecParams p) {
+  constexpr int NT = DEC_MERGE_THREADS<P, COLS>;
+  constexpr int TPR = D / 4, PST = D + 4, RPW = NT / (TPR * P);  // rows per workgroup
   static_assert(RPW >= 1, "a workgroup holds whole rows");
-  __shared__ f32x4 so[P > 1 ? 256 : 1];
-  __shared__ float2 sml[P > 1 ? 256 : 1];
+  __shared__ f32x4 so[P > 1 ? NT : 1];
+  __shared__ float2 sml[P > 1 ? NT : 1];
   const int tid = threadIdx.x;
-  const int q4 = tid % TPR, part = (tid / TPR) % P;
-  const size_t qrow = (size_t)blockIdx.x * RPW + tid / (TPR * P);  // row of Q: ((b * Hq + h) * S + s)
+  constexpr int APART = COLS ? RPW * TPR : TPR;  // threads between the parts of a row's runs
+  const int q4 = COLS ? tid / RPW % TPR : tid % TPR, part = COLS ? tid / APART : (tid / TPR) % P;
+  const size_t qrow = (size_t)blockIdx.x * RPW + (COLS ? tid % RPW : tid / (TPR * P));  // row of Q: ((b * Hq + h) * S + s)
   const int GS = p.G * p.S;
   auto weight = [](float m, float mn) { return EMPTY && m == mn ? 1.f : fast_exp2(m - mn); };  // 2^(m - mn)
   DecRuns d = {0, -1};
@@ -122,12 +130,21 @@ __global__ __launch_bounds__(256) void dec_combine_kernel(DecParams p) {
     d = p.desc[bh * p.ng + g];  // (last run -1: written by the decode kernel itself)
 #pragma unroll 4
     for (int gw = d.first + part; gw <= d.last; gw += P) {
-      const float* ps = p.part + (dec_slot_row(p, gw, bh, g) + r) * PST;
-      const f32x4 ml = *reinterpret_cast<const f32x4*>(ps + D);
-      const f32x4 v = *reinterpret_cast<const f32x4*>(ps + 4 * q4);
-      const float Mn = fmaxf(M, ml[0]);
-      const float a = weight(M, Mn), c = weight(ml[0], Mn);  // a = 0 for the first run (M = -inf)
-      Lr = Lr * a + ml[1] * c;
+      float2 ml;
+      f32x4 v;
+      if constexpr (COLS) {
+        const float* ps = p.part + (dec_slot_row(p, gw, bh, g) + (r & ~31)) * PST;
+        ml = *reinterpret_cast<const float2*>(ps + 32 * D + 2 * (r & 31));
+        v = *reinterpret_cast<const f32x4*>(ps + 4 * (32 * q4 + (r & 31)));
+      } else {
+        const float* ps = p.part + (dec_slot_row(p, gw, bh, g) + r) * PST;
+        const f32x4 x = *reinterpret_cast<const f32x4*>(ps + D);
+        ml = float2{x[0], x[1]};
+        v = *reinterpret_cast<const f32x4*>(ps + 4 * q4);
+      }
+      const float Mn = fmaxf(M, ml.x);
+      const float a = weight(M, Mn), c = weight(ml.x, Mn);  // a = 0 for the first run (M = -inf)
+      Lr = Lr * a + ml.y * c;
       o = o * a + v * c;
       M = Mn;
     }
@@ -140,8 +157,8 @@ __global__ __launch_bounds__(256) void dec_combine_kernel(DecParams p) {
     // (part 0 holds at least one run, so M is finite unless EMPTY)
 #pragma unroll
     for (int u = 1; u < P; ++u) {
-      const float2 ml = sml[tid + u * TPR];
-      const f32x4 v = so[tid + u * TPR];
+      const float2 ml = sml[tid + u * APART];
+      const f32x4 v = so[tid + u * APART];
       const float Mn = fmaxf(M, ml.x);
       const float a = weight(M, Mn), c = weight(ml.x, Mn);  // c = 0 for a part without runs
       Lr = Lr * a + ml.y * c;
@@ -158,16 +175,15 @@ __global__ __launch_bounds__(256) void dec_combine_kernel(DecParams p) {
 }
 
 // Enqueues the merge of the items held by several runs.
-template <int D, bool EMPTY>
+template <int D, bool EMPTY, bool COLS>
 hipError_t launch_dec_combine(const DecodeShape& s, const DecodeGroups& g, const DecParams& p, hipStream_t st) {
   const size_t rows = (size_t)s.B * s.Hq * s.S, items = (size_t)s.B * s.Hkv * g.ng;
-  if (items * 8 <= (size_t)g.runs) {
-    constexpr int P = 8, RPW = 256 / (D / 4 * P);
-    hipLaunchKernelGGL((dec_combine_kernel<D, P, EMPTY>), dim3((unsigned)((rows + RPW - 1) / RPW)), dim3(256), 0, st, p);
-  } else {
-    constexpr int RPW = 256 / (D / 4);
-    hipLaunchKernelGGL((dec_combine_kernel<D, 1, EMPTY>), dim3((unsigned)((rows + RPW - 1) / RPW)), dim3(256), 0, st, p);
-  }
+  const auto merge = [&](auto parts) {
+    constexpr int P = decltype(parts)::value, NT = DEC_MERGE_THREADS<P, COLS>, RPW = NT / (D / 4 * P);
+    hipLaunchKernelGGL((dec_combine_kernel<D, P, EMPTY, COLS>), dim3((unsigned)((rows + RPW - 1) / RPW)), dim3(NT), 0, st, p);
+  };
+  if (items * 8 <= (size_t)g.runs) merge(std::integral_constant<int, COLS ? 4 : 8>());
+  else merge(std::integral_constant<int, 1>());
   return hipGetLastError();
 }
 

@@ -359,15 +359,18 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
         return;
       }
       if (valid) {
-        float* pr = p.part + (dec_slot_row(p, gw, (size_t)pc.b * p.Hkv + pc.h, pc.g) + 32 * tw + l32) * PST;
+        // Teams leave [D / 4][32] float4 for each wave's rows, a contiguous KiB a store (rows of D + 4 floats: 32
+        // bytes of each row); one wave, with few rows, leaves rows, which the merge reads faster.
+        float* pr = p.part + (dec_slot_row(p, gw, (size_t)pc.b * p.Hkv + pc.h, pc.g) + 32 * tw + (TW == 1 ? l32 : 0)) * PST;
+        float* po = pr + (TW == 1 ? 4 * g2 : 4 * lane);
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const f32x4 v = {oacc[db][4 * i], oacc[db][4 * i + 1], oacc[db][4 * i + 2], oacc[db][4 * i + 3]};
-            *reinterpret_cast<f32x4*>(pr + 32 * db + 8 * i + 4 * g2) = v;
+            *reinterpret_cast<f32x4*>(po + (4 * db + i) * (TW == 1 ? 8 : 256)) = v;
           }
-        if (g2 == 0) *reinterpret_cast<f32x4*>(pr + D) = f32x4{m, Lrow, 0.f, 0.f};
+        if (g2 == 0) *reinterpret_cast<float2*>(pr + (TW == 1 ? D : 32 * D + 2 * l32)) = float2{m, Lrow};
       }
       if (ends && lane == 0 && tw == 0) {
         // the runs holding this item: from the one holding its first tile to this one
@@ -479,7 +482,7 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
 #pragma unroll
         for (int db = 0; db < DB; ++db)
           oacc[db] = mfma32(lds_tr<D>(cur + Smem::TILE, ops.tr_rel0, ops.tr_rel1, c, db), pb[c], oacc[db]);
-      pipeline_lds_reads<2 * KB * DB, (TW == 1 ? 3 : 4), 2>();
+      pipeline_lds_reads<2 * KB * DB, (TW == 1 || D == 128 ? 3 : 4), 2>();
     };
 
     uint32_t bcur = 0;                           // ring offset of the tile at pc
@@ -548,7 +551,7 @@ hipError_t launch_paged_d(const DecodeShape& s, const PagedArgs& a, void* ws, hi
   else launch_paged_kernel<D, 4, 64, 512 / D>(p, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  return launch_dec_combine<D, true>(s, g, p.d, st);
+  return g.waves == 1 ? launch_dec_combine<D, true, false>(s, g, p.d, st) : launch_dec_combine<D, true, true>(s, g, p.d, st);
 }
 
 }  // namespace
