@@ -469,8 +469,8 @@ int bd_paged_plan(const int32_t* cache_lens, const int32_t* new_lens, int32_t* p
  * keys (never written, or dropped): its positions are left out of the softmax.
  * A row that sees no key gets O = 0 and LSE = -inf.
  * Values in K, V and Q must be finite.  bfloat16 only; D, S, B, heads, scale,
- * O [B, Hq, S, D] and LSE [B, Hq, S] as for bd_attn_decode_fwd, max_pages >= 1
- * and max_pages * page_size <= 2^22; page_size, num_pages as for bd_paged_plan;
+ * O [B, Hq, S, D] and LSE [B, Hq, S] as for bd_attn_decode_fwd, B * Hq * S at
+ * most 2^26, max_pages >= 1 and max_pages * page_size <= 2^22; page_size, num_pages as for bd_paged_plan;
  * page_stride is below 2^31, row_stride at least D and at most 2^20 (times
  * page_size at most 2^30), all multiples of 8.
  * ws/ws_bytes: at least bd_attn_paged_decode_workspace_bytes bytes (16-byte

@@ -293,6 +293,8 @@ int validate_paged(int B, int S, int Hq, int Hkv, int D, int page_size, int max_
                    bd::DecodeShape& s) {
   const int lg = page_log(page_size);
   if (lg < 0 || max_pages < 1 || (int64_t)max_pages << lg > (1 << 22)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  // (the merge counts its threads, up to 32 a query row, in 32 bits)
+  if (B > 0 && Hq > 0 && S > 0 && (int64_t)B * Hq > (1 << 26) / S) return BD_ATTN_ERR_INVALID_ARGUMENT;
   return validate_decode(B, S, Hq, Hkv, D, max_pages << lg, scale, dtype, s);
 }
 

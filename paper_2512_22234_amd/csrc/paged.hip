@@ -52,6 +52,34 @@ __device__ inline int paged_tiles(const PagedParams& p, int len) {
   return imax(tiles_of<KT>(len) + tiles_of<KT>(p.Sn), 1);
 }
 
+// Runs that T tiles are cut into.  Every run that holds part of an item leaves
+// partial results, for one wave up to 32 rows of D floats (as many bytes as a
+// tile of keys and values), which are written, read and merged, so a call is cut
+// no finer than its reading needs.  One wave: single tiles for up to 256 runs (one
+// a CU), then three tiles a run; where these come to two runs on most CUs, two on
+// all; three a CU from 24,576 tiles on, and at D = 64, with half the bytes a tile.
+// Measured, us (32/8 heads; * no more than one tile a run):
+//                                               256   cdiv(T, 3)  512   768   1024 runs
+//   one sequence of 1500, S = 8 (384 tiles)     11.3     -        13.7* 13.6* 14.1*
+//   ... of 3000 (760)                           13.6    13.6      16.0  20.1  20.7*
+//   ... of 6000 (1512)                          16.5    17.9      16.8  18.4  20.0
+//   8 sequences of 3000, S = 8 (6080)           34.5     -        27.3  29.9  31.0
+//   64 of 512 to 8192, S = 1 (25,000)             -      -       143.4 138.2 140.5
+//   D = 64: 2 of 3000, S = 4 (1520)               -     12.8       -    13.5    -
+//   D = 64: 64 of 512 to 8192, S = 1              -      -        84.8  70.7  75.6
+// Teams take two tiles at least (dec_runs).
+template <int D, int TW>
+__device__ inline int paged_runs(int T) {
+  if (TW > 1) return dec_runs<TW>(DEC_WAVES / TW, T);
+  const int three = imax(256, cdiv(T, 3));
+  return imin(T, D == 64 ? imin(three, 768) : T < 1152 ? three : T < 24576 ? 512 : 768);
+}
+// First tile of run gw <= n (the runs cut T tiles into n near-equal pieces).
+__device__ inline int paged_run_start(int gw, int n, int T) {
+  if (T < 1 << 22) return (int)((unsigned)(gw * T) / (unsigned)n);
+  return (int)((unsigned)(((unsigned long long)gw * T) >> 8) / ((unsigned)n >> 8));  // (n is a multiple of 256 here)
+}
+
 template <int D, int TW, int KT, int NST>
 struct PagedSmem {
   static constexpr int TEAMS = TW == 1 ? 4 : 1;  // teams per workgroup
@@ -110,13 +138,12 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
   const int excl = before + incl - csum;  // tiles per item of the sequences before c0
   total = __builtin_amdgcn_readfirstlane(total);
   const int T = total * I;  // checked on the host to fit in 31 bits
-  constexpr int RUNS = DEC_WAVES / TW;
-  const int n = dec_runs<TW>(RUNS, T);
+  const int n = paged_runs<D, TW>(T);
   const bool stream = total * p.d.Hkv > (int)(DEC_STREAM_BYTES / (2 * Smem::TILE));
-  auto run_of = [&](int v) { return n == RUNS ? (int)blockIdx.x * TEAMS + v : v * (int)gridDim.x + (int)blockIdx.x; };
+  auto run_of = [&](int v) { return v * (int)gridDim.x + (int)blockIdx.x; };  // run of a workgroup's team v
 #pragma unroll
   for (int v = 0; v < TEAMS; ++v) {
-    const int x0 = dec_run_start<RUNS>(run_of(v), n, T);
+    const int x0 = run_of(v) < n ? paged_run_start(run_of(v), n, T) : T;
     if (csum > 0 && excl * I <= x0 && x0 < (excl + csum) * I) {
       int pb = excl;
       for (int b = c0; b < c1; ++b) {
@@ -135,7 +162,7 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
   // ---- this team's run ----
   const int gw = run_of(tm);
   if (gw >= n) return;
-  const int x0 = dec_run_start<RUNS>(gw, n, T), x1 = dec_run_start<RUNS>(gw + 1, n, T);
+  const int x0 = paged_run_start(gw, n, T), x1 = paged_run_start(gw + 1, n, T);
   PagedPos pc;
   pc.b = __builtin_amdgcn_readfirstlane(sm.start_b[tm]);
   const int off = __builtin_amdgcn_readfirstlane(sm.start_off[tm]);
@@ -386,6 +413,7 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
       compute_fence();  // the reads of the buffer about to be refilled are done
       const PagedTile t = tile_arguments();
       if constexpr (TW == 1) {
+        static_assert(TW > 1 || NST == 2, "a step without a copy is the last one");
         // (query rows of the next item: a tile ahead, behind the wait, in both branches, as over a dense cache)
         if (copies) {
           pieces |= issue(t, pa, ga, nxt, streamed) << (NP * (NST - 1));
@@ -507,7 +535,7 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
 template <int D, int TW, int KT, int NST>
 void launch_paged_kernel(const PagedParams& p, hipStream_t st) {
   using Smem = PagedSmem<D, TW, KT, NST>;
-  hipLaunchKernelGGL((paged_kernel<D, TW, KT, NST>), dim3(p.d.runs / Smem::TEAMS), dim3(64 * Smem::NW), 0, st, p,
+  hipLaunchKernelGGL((paged_kernel<D, TW, KT, NST>), dim3(DEC_WAVES / (TW == 1 ? 4 : TW)), dim3(64 * Smem::NW), 0, st, p,
                      p.d.cache_lens);
 }
 

@@ -176,7 +176,8 @@ def test_paged_decode_workspace_bytes():
     f = bd.bd_attn_paged_decode_workspace_bytes
     assert f(64, 4, 32, 8, 128, 64, 128) == bd.bd_attn_decode_workspace_bytes(64, 4, 32, 8, 128, 8192) > 0
     for bad in [(2, 1, 4, 2, 64, 24, 8), (2, 1, 4, 2, 64, 16, 0), (2, 1, 4, 2, 64, 16, (1 << 18) + 1), (2, 0, 4, 2, 64, 16, 8),
-                (2, 1, 3, 2, 64, 16, 8), (2, 1, 4, 2, 96, 16, 8), (2, 1, 4, 2, 64, 16, 8, 1), (0, 1, 4, 2, 64, 16, 8)]:
+                (2, 1, 3, 2, 64, 16, 8), (2, 1, 4, 2, 96, 16, 8), (2, 1, 4, 2, 64, 16, 8, 1), (0, 1, 4, 2, 64, 16, 8),
+                (1 << 12, 1 << 10, 32, 32, 64, 16, 8)]:
         assert f(*bad) == 0, bad
 
 

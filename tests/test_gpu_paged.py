@@ -171,6 +171,21 @@ def test_strided_table_shared_pages_and_determinism():
         assert all(torch.equal(x, y) for x, y in zip(g, want))
 
 
+def test_many_tiles_on_shared_pages():
+    """More than 2^22 key tiles (16,500 sequences of 1024 tokens on the same pages,
+    8 heads): the runs' cuts in 64 bits.  Equal queries give equal results but for
+    where the runs cut them: float32 sums, P rounded to bf16."""
+    B, H, D, P, n = 16500, 8, 64, 64, 1024
+    g = torch.Generator().manual_seed(4)
+    kp, vp = _pages(n // P, H, P, D, "heads", g)
+    q = (torch.randn((1, H, 1, D), generator=g) * 0.5).to(BF).to(DEV).repeat(B, 1, 1, 1)
+    table = torch.randperm(n // P, generator=g).to(torch.int32).to(DEV).repeat(B, 1)
+    lens = torch.full((B,), n, dtype=torch.int32, device=DEV)
+    o, lse = bd.bd_attn_paged_decode_fwd(q, kp, vp, table, lens)
+    _check(o[:1], lse[:1], _oracle(q[:1], kp, vp, table[:1], lens[:1]), "many tiles")
+    assert float((o.float() - o[:1].float()).abs().max()) <= 1e-2 and float((lse - lse[:1]).abs().max()) <= 1e-4
+
+
 def test_offsets_past_32_bits():
     """Pages behind 2^32 bytes and 2^31 elements of an 8 GiB array."""
     B, Hq, Hkv, D, P, n = 2, 8, 8, 128, 64, 66000
