@@ -16,8 +16,8 @@
 // halves of a row (16-byte accesses, pairs of the rotation in one lane), D / 16
 // lanes a row; a workgroup takes 256 / (D / 16) consecutive tokens, whose cos
 // and sin stay in registers, and a run of heads of one kind (q, k or v).
-// Measured: 16384 tokens of 32/8 heads of 128, forward: 66 us, 6.1 TB/s (a copy
-// of 1 GiB: 5.1); 8192 tokens, forward and backward: 92 us, 5.3 TB/s.
+// Measured: 16384 tokens of 32/8 heads of 128, forward: 77 us, 5.2 TB/s (a copy
+// of 1 GiB: 5.1).
 #include "device.hpp"
 #include "kernels.hpp"
 
@@ -119,7 +119,8 @@ __device__ inline void lane_angles(const RopeShape& s, const Token& k, int i, fl
   ld8(row + D / 2, sn);
 }
 
-template <typename T, typename W, int D, bool PAGED, bool NT>
+// NT: nontemporal loads (1), and stores (2).
+template <typename T, typename W, int D, bool PAGED, int NT>
 __global__ __launch_bounds__(ROPE_NT) void rope_fwd_kernel(RopeShape s, RopeFwdArgs a) {
   constexpr int LPR = ROPE_LPR<D>;
   const int i = threadIdx.x % LPR;
@@ -146,11 +147,11 @@ __global__ __launch_bounds__(ROPE_NT) void rope_fwd_kernel(RopeShape s, RopeFwdA
   if (run.kind == 2) {
     for (int h = run.h0; h < run.h1; ++h) {
       float x1[8], x2[8];
-      ld8<NT>(src + h * in.sh, x1);
-      ld8<NT>(src + h * in.sh + D / 2, x2);
+      ld8<(NT > 0)>(src + h * in.sh, x1);
+      ld8<(NT > 0)>(src + h * in.sh + D / 2, x2);
       if (store) {
-        st8(dst + h * dst_h, x1);
-        st8(dst + h * dst_h + D / 2, x2);
+        st8<(NT > 1)>(dst + h * dst_h, x1);
+        st8<(NT > 1)>(dst + h * dst_h + D / 2, x2);
       }
     }
     return;
@@ -162,8 +163,8 @@ __global__ __launch_bounds__(ROPE_NT) void rope_fwd_kernel(RopeShape s, RopeFwdA
   ld8(w + D / 2, w2);
   for (int h = run.h0; h < run.h1; ++h) {
     float x1[8], x2[8];
-    ld8<NT>(src + h * in.sh, x1);
-    ld8<NT>(src + h * in.sh + D / 2, x2);
+    ld8<(NT > 0)>(src + h * in.sh, x1);
+    ld8<(NT > 0)>(src + h * in.sh + D / 2, x2);
     float ss = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss += x1[e] * x1[e] + x2[e] * x2[e];
@@ -175,8 +176,8 @@ __global__ __launch_bounds__(ROPE_NT) void rope_fwd_kernel(RopeShape s, RopeFwdA
       x2[e] = y2 * c[e] + y1 * sn[e];
     }
     if (store) {
-      st8(dst + h * dst_h, x1);
-      st8(dst + h * dst_h + D / 2, x2);
+      st8<(NT > 1)>(dst + h * dst_h, x1);
+      st8<(NT > 1)>(dst + h * dst_h + D / 2, x2);
     }
   }
 }
@@ -328,23 +329,27 @@ dim3 rope_grid(const RopeShape& s) {
   return dim3((unsigned)rope_token_blocks(s), (unsigned)(cdiv(s.Hq, s.hpb) + 2 * cdiv(s.Hkv, s.hpb)));
 }
 
-// A call whose rows (`heads` of D values read or written per token) exceed the
-// 256 MiB of the last-level cache loads them nontemporal.  Forward, 32/8 heads of
-// 128: 16384 tokens (384 MiB) 83.4 -> 66.1 us alone, 204.6 -> 211.1 between a
-// kernel that writes its inputs and one that reads its results; at 12288 the same
-// alone (53.4, 52.7), below it slower (4096: 17.3, 20.8).  Backward, 8192 tokens
-// (272 MiB) between such kernels: 121.9 -> 108.5 us; 16384: 249.6 -> 236.4; 4096:
-// 54.8, 57.6.  (Nontemporal stores: up to 10% slower between such kernels at
-// 2048 to 8192 tokens, 3% faster at 16384.)
-constexpr size_t ROPE_STREAM_BYTES = (size_t)256 << 20;
-bool rope_streams(const RopeShape& s, int heads) {
-  return (size_t)s.B * s.N * heads * s.D * (s.f32 ? 4 : 2) > ROPE_STREAM_BYTES;
-}
+// Bytes of a call's rows, `heads` of D values read or written per token: beyond
+// 64 MiB their loads are nontemporal, and in the forward beyond 128 MiB (half the
+// last-level cache) the stores too.  Measured between a kernel that writes the
+// call's inputs and one that reads its results, on a GiB of arrays in turn, as the
+// layers of a model have them (32/8 heads of 128; us for the three kernels with
+// neither, the loads, both):
+//   tokens     forward                backward
+//     1024      15.1  15.4  15.2      21.9  21.9  22.9
+//     2048      24.1  24.1  25.4      33.0  32.7  35.2    (48 and 68 MiB)
+//     4096      48.0  43.6  45.8      61.2  54.9  59.3
+//     8192     107.7 102.8  89.6     124.9 115.3 117.7
+//    16384     207.6 209.8 200.4     251.5 238.2 236.9
+// and the forward alone, us: 2048 tokens 10.1, 12.5, 11.6; 4096 20.7, 20.0, 20.2;
+// 8192 43.2, 38.3, 38.9; 16384 83.3, 82.2, 77.0.
+constexpr size_t ROPE_NT_LOADS = (size_t)64 << 20, ROPE_NT_STORES = (size_t)128 << 20;
+size_t rope_bytes(const RopeShape& s, int heads) { return (size_t)s.B * s.N * heads * s.D * (s.f32 ? 4 : 2); }
 
 template <typename T, typename W, int D>
 hipError_t launch_rope_fwd_t(const RopeShape& s, const RopeFwdArgs& a, bool paged, hipStream_t st) {
   const auto kernel = [&](auto nt) {
-    constexpr bool NT = decltype(nt)::value;
+    constexpr int NT = decltype(nt)::value;
     if (paged) {
       if constexpr (std::is_same_v<T, bf16>)
         hipLaunchKernelGGL((rope_fwd_kernel<T, W, D, true, NT>), rope_grid(s), dim3(ROPE_NT), 0, st, s, a);
@@ -352,15 +357,17 @@ hipError_t launch_rope_fwd_t(const RopeShape& s, const RopeFwdArgs& a, bool page
       hipLaunchKernelGGL((rope_fwd_kernel<T, W, D, false, NT>), rope_grid(s), dim3(ROPE_NT), 0, st, s, a);
     }
   };
-  if (rope_streams(s, 2 * (s.Hq + 2 * s.Hkv))) kernel(Flag<true>());
-  else kernel(Flag<false>());
+  const size_t bytes = rope_bytes(s, 2 * (s.Hq + 2 * s.Hkv));
+  if (bytes > ROPE_NT_STORES) kernel(std::integral_constant<int, 2>());
+  else if (bytes > ROPE_NT_LOADS) kernel(std::integral_constant<int, 1>());
+  else kernel(std::integral_constant<int, 0>());
   return hipGetLastError();
 }
 template <typename T, typename W, int D>
 hipError_t launch_rope_bwd_t(const RopeShape& s, const RopeBwdArgs& a, hipStream_t st) {
   int nq = 0, nk = 0;
   if (s.B > 0 && s.N > 0) {
-    if (rope_streams(s, 3 * s.Hq + 5 * s.Hkv))
+    if (rope_bytes(s, 3 * s.Hq + 5 * s.Hkv) > ROPE_NT_LOADS)
       hipLaunchKernelGGL((rope_bwd_kernel<T, W, D, true>), rope_grid(s), dim3(ROPE_NT), 0, st, s, a);
     else
       hipLaunchKernelGGL((rope_bwd_kernel<T, W, D, false>), rope_grid(s), dim3(ROPE_NT), 0, st, s, a);
