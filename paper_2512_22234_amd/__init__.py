@@ -566,6 +566,8 @@ def _launch_context(device: torch.device, stream):
     """Where a call allocates and launches: on the tensors' device, and on
     `stream`, whose pool its results and workspace then come from."""
     if stream is not None:
+        if stream.device != device:
+            raise ValueError(f"stream: expected one of {device}, got one of {stream.device}")
         return torch.cuda.stream(stream)
     if device.type == "cuda" and device.index != torch.cuda.current_device():
         return torch.cuda.device(device)
@@ -584,10 +586,6 @@ def _row_strides(name, shape, strides):
     if any(s % 8 for s in st):
         raise ValueError(f"{name}: strides must be multiples of 8 elements, got {strides}")
     return st if len(st) == 3 else [0] + st
-
-
-def _stride_array(strides):
-    return (ctypes.c_int64 * len(strides))(*strides)
 
 
 # What a call derives from shapes and strides alone (checked on the way, and
@@ -611,7 +609,8 @@ def _rope_layout(q_shape, q_strides, k_shape, k_strides, v_shape, v_strides, pos
         strides += _row_strides(name, shape, st)
     if tuple(pos_shape) not in ((N,), lead + (N,)):
         raise ValueError(f"positions: expected shape {lead + (N,)} or {(N,)}, got {tuple(pos_shape)}")
-    return _RopeLayout(lead[0] if lead else 1, N, Hq, Hkv, D, _stride_array(strides), N if len(pos_shape) == 2 else 0,
+    return _RopeLayout(lead[0] if lead else 1, N, Hq, Hkv, D, (ctypes.c_int64 * len(strides))(*strides),
+                       N if len(pos_shape) == 2 else 0,
                        lead + (Hq, N, D), lead + (Hkv, N, D))
 
 
@@ -718,18 +717,19 @@ def bd_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, rope, positions, e
     args = _rope_inputs(lay, q, (k,), q_weight, k_weight, rope, positions)
     dev, dt = q.device, q.dtype
     with _launch_context(dev, stream):
-        grads, gstrides = [], []
+        grads = []
         for name, t, like in (("grad_q", grad_q, q), ("grad_k", grad_k, k), ("grad_v", grad_v, k)):
             if t is None:
                 t = torch.empty(like.shape, dtype=dt, device=dev)
             elif t.shape != like.shape or t.dtype != dt or t.device != dev:
                 raise ValueError(f"{name}: expected {dt} {tuple(like.shape)} on {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-            gstrides += _row_strides(name, t.shape, t.stride())
             grads.append(t)
+        gq, gk, gv = grads
+        strides = _rope_layout(gq.shape, gq.stride(), gk.shape, gk.stride(), gv.shape, gv.stride(), positions.shape).strides
         gqw = _result("grad_q_weight", grad_q_weight, (lay.D,), q_weight.dtype, dev)
         gkw = _result("grad_k_weight", grad_k_weight, (lay.D,), q_weight.dtype, dev)
-        _rope_bwd(lay, (dq, dk, dv), (_ptr(q), _ptr(k)), args, eps, dt, dev, [_ptr(t) for t in grads],
-                  _stride_array(gstrides), gqw, gkw, workspace, stream)
+        _rope_bwd(lay, (dq, dk, dv), (_ptr(q), _ptr(k)), args, eps, dt, dev, (_ptr(gq), _ptr(gk), _ptr(gv)),
+                  strides, gqw, gkw, workspace, stream)
     return (*grads, gqw, gkw)
 
 
@@ -802,7 +802,11 @@ class QkvNormRopeFunction(torch.autograd.Function):
 
 
 def qk_norm_rope(q, k, v, q_weight, k_weight, rope, positions, eps: float = 1e-6):
-    """bd_qk_norm_rope_fwd, differentiable in q, k, v and the weights."""
+    """bd_qk_norm_rope_fwd, differentiable in q, k, v and the weights.
+
+    (As with any autograd function, a forward and its backward are captured into
+    one graph, with no eager graph of the same leaves alive: torch's accumulation
+    into a leaf runs on the stream of the first graph that used it.)"""
     return QkNormRopeFunction.apply(q, k, v, q_weight, k_weight, rope, positions, eps)
 
 

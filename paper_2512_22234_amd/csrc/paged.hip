@@ -82,7 +82,7 @@ __device__ inline int paged_run_start(int gw, int n, int T) {
 
 template <int D, int TW, int KT, int NST>
 struct PagedSmem {
-  static constexpr int TEAMS = TW == 1 ? 4 : 1;  // teams per workgroup
+  static constexpr int TEAMS = TW == 1 ? 3 : 1;  // teams per workgroup (paged_runs: at most 768 runs)
   static constexpr int NW = TW * TEAMS;          // waves per workgroup
   static constexpr uint32_t TILE = KT * D * 2;   // bytes of one swizzled K or V tile
   alignas(256) char buf[TEAMS][NST * 2 * TILE];  // per team: a ring of K and V tiles
@@ -99,7 +99,7 @@ struct PagedPos {
 // `lens` is the parameters' array as a restrict kernel argument, read through the
 // scalar cache where the index is uniform.
 template <int D, int TW, int KT, int NST>
-__global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(PagedParams p, const int* __restrict__ lens) {
+__global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(PagedParams p, const int* __restrict__ lens) {
   constexpr int DS = D / 16, DB = D / 32, PST = D + 4, KB = KT / 32;
   using Smem = PagedSmem<D, TW, KT, NST>;
   constexpr int TEAMS = Smem::TEAMS, NW = Smem::NW, NT = 64 * NW;
@@ -535,7 +535,7 @@ __global__ __launch_bounds__(TW == 1 ? 256 : 64 * TW, 1) void paged_kernel(Paged
 template <int D, int TW, int KT, int NST>
 void launch_paged_kernel(const PagedParams& p, hipStream_t st) {
   using Smem = PagedSmem<D, TW, KT, NST>;
-  hipLaunchKernelGGL((paged_kernel<D, TW, KT, NST>), dim3(DEC_WAVES / (TW == 1 ? 4 : TW)), dim3(64 * Smem::NW), 0, st, p,
+  hipLaunchKernelGGL((paged_kernel<D, TW, KT, NST>), dim3(TW == 1 ? 256 : DEC_WAVES / TW), dim3(64 * Smem::NW), 0, st, p,
                      p.d.cache_lens);
 }
 
