@@ -47,6 +47,8 @@ def _pages(n, Hkv, P, D, order, g, fill=None):
         return rows(n, Hkv, P, D), rows(n, Hkv, P, D)
     if order == "tokens":
         return tuple(rows(n, P, Hkv, D).permute(0, 2, 1, 3) for _ in range(2))
+    if order == "outer":                      # [heads, pages, rows, D]
+        return tuple(rows(Hkv, n, P, D).permute(1, 0, 2, 3) for _ in range(2))
     if order == "pairs":                      # [pages, 2, heads, rows, D]
         kv = rows(n, 2, Hkv, P, D)
         return kv[:, 0], kv[:, 1]
@@ -95,6 +97,10 @@ DECODE = [
     (300, 4, 2, 64, 2, 16, 4, [i % 65 for i in range(300)], "tokens", True),
     (300, 2, 1, 128, 1, 16, 4, [i % 3 * 30 for i in range(300)], "heads", False),
     (16, 4, 4, 128, 1, 256, 47, [12000, 3] * 8, "heads", False),        # runs cross items
+    (3, 8, 4, 64, 3, 1 << 15, 2, [40000, 0, 32768], "outer", True),     # the largest pages, heads outermost
+    (2, 32, 1, 64, 40, 16, 20, [300, 7], "outer", True),                # 1280 rows: ten groups
+    (5, 4, 2, 128, 1, 16, 2, [0, 0, 0, 0, 0], "heads", False),          # no key at all
+    (2, 12, 3, 64, 16, 64, 30, [1900, 1023], "tokens", True),           # 64 rows at D = 64
 ]
 
 
@@ -106,12 +112,13 @@ def test_decode_matches_oracle(B, Hq, Hkv, D, S, P, width, lens, order, block):
     _check(o, lse, _oracle(*a), f"P{P} S{S}")
 
 
-@pytest.mark.parametrize("S,P,Hq", [(1, 16, 8), (4, 64, 8), (32, 16, 4), (32, 32, 8)])
+@pytest.mark.parametrize("S,P,Hq,D", [(1, 16, 8, 128), (4, 64, 8, 128), (32, 16, 4, 128), (32, 32, 8, 128), (1, 16, 8, 64),
+                                      (16, 16, 8, 64), (32, 64, 8, 64)])
 @pytest.mark.parametrize("block", [False, True])
-def test_pages_that_are_none(S, P, Hq, block):
+def test_pages_that_are_none(S, P, Hq, D, block):
     """Entries outside the pool, singly and in runs: their keys are left out; a
     sequence whose pages are all none sees its own block or nothing."""
-    B, Hkv, D, width = 4, 2, 128, 300 // P + 2
+    B, Hkv, width = 4, 2, 300 // P + 2
     a = list(_inputs(B, Hq, Hkv, D, S, P, width, [300, 299, 150, 33], "heads", 77 + S, block))
     t = a[3]
     t[0, 1] = -1
@@ -186,6 +193,19 @@ def test_many_tiles_on_shared_pages():
     assert float((o.float() - o[:1].float()).abs().max()) <= 1e-2 and float((lse - lse[:1]).abs().max()) <= 1e-4
 
 
+def test_runs_of_a_long_call():
+    """25,600 key tiles at D = 128 (as many runs as the grid holds), rows of pages shared by the sequences."""
+    B, Hq, Hkv, D, P = 400, 16, 8, 128, 32
+    g = torch.Generator().manual_seed(5)
+    kp, vp = _pages(40, Hkv, P, D, "tokens", g)
+    q = (torch.randn((B, Hq, 1, D), generator=g) * 0.5).to(BF).to(DEV)
+    table = torch.randint(0, 40, (B, 8), generator=g, dtype=torch.int32).to(DEV)
+    lens = torch.randint(240, 257, (B,), generator=g, dtype=torch.int32).to(DEV)
+    o, lse = bd.bd_attn_paged_decode_fwd(q, kp, vp, table, lens)
+    pick = [0, 1, 133, 266, 399]
+    _check(o[pick], lse[pick], _oracle(q[pick], kp, vp, table[pick], lens[pick]), "long call")
+
+
 def test_offsets_past_32_bits():
     """Pages behind 2^32 bytes and 2^31 elements of an 8 GiB array."""
     B, Hq, Hkv, D, P, n = 2, 8, 8, 128, 64, 66000
@@ -229,6 +249,7 @@ def _plan_check(lens, new, table, free, head, pages, P, S=None, total=None):
 @pytest.mark.parametrize("B,P,width,S,hi", [
     (1, 16, 4, 1, 60), (1, 16, 4, None, 60), (7, 64, 10, 4, 600), (64, 16, 64, None, 500), (255, 16, 9, 3, 140),
     (256, 32, 9, None, 140), (257, 16, 9, 1, 140), (1000, 16, 30, None, 90), (5000, 16, 3, 2, 47), (3, 1024, 6, None, 5000),
+    (1 << 16, 16, 2, 1, 31), (2, 1 << 15, 8, None, 200000),
 ])
 def test_plan_matches_oracle(B, P, width, S, hi):
     rng = np.random.default_rng(B + P)
@@ -288,7 +309,7 @@ def test_plan_too_small_a_total():
 # ---------------------------------------------------------------------------
 # writing into pages
 
-@pytest.mark.parametrize("order", ["heads", "tokens", "pairs", "sides"])
+@pytest.mark.parametrize("order", ["heads", "tokens", "pairs", "sides", "outer"])
 @pytest.mark.parametrize("B,N,Hq,Hkv,D,P", [(1, 1, 1, 1, 64, 16), (5, 4, 8, 2, 128, 64), (1, 333, 16, 4, 128, 16)])
 def test_write_into_pages(order, B, N, Hq, Hkv, D, P):
     """Keys and values of the plain call at their slots, bitwise; every other row stays."""

@@ -71,6 +71,8 @@ CASES = [
     (1, 1000, 32, 8, 128, BF, BF),       # several heads a workgroup
     (5, 131, 16, 16, 64, F32, F32),
     (2, 2500, 32, 8, 64, BF, F32),
+    (1, 4100, 7, 3, 128, BF, F32),       # runs of two heads, a last one of one
+    (3, 3000, 11, 5, 64, F32, F32),      # ... of four, a last one of three and of one
 ]
 
 
@@ -137,6 +139,36 @@ def test_layouts_give_the_same():
     got = bd.bd_qk_norm_rope_bwd(*d, q, k, *rest, c["pos"], 1e-6, *views)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert (fused[..., -64:] == 7.0).all()      # nothing past a token's heads
+
+
+@pytest.mark.parametrize("N,dt", [(9000, BF), (17500, BF), (6000, F32)])
+def test_large_calls(N, dt):
+    """Calls of more than 64 and 128 MiB (nontemporal loads, and stores), eight heads a
+    workgroup: bitwise the results of the same tokens in calls of 500, sampled
+    tokens against the oracle; the weights' gradients against sums in float64."""
+    Hq, Hkv, D = 10, 3, 128
+    c = _case(1, N, Hq, Hkv, D, dt, F32, seed=16)
+    q, k, v = _parts(c, Hq, Hkv, D)
+    w, d = (c["wq"], c["wk"], c["rope"]), (c["dq"], c["dk"], c["dv"])
+    out = bd.bd_qk_norm_rope_fwd(q, k, v, *w, c["pos"])
+    grads = bd.bd_qk_norm_rope_bwd(*d, q, k, *w, c["pos"])
+    dw = [torch.zeros(D, dtype=torch.float64, device=DEV) for _ in range(2)]
+    for n in range(0, N, 500):
+        part = slice(n, n + 500)
+        pos = c["pos"][:, part].contiguous()
+        got = bd.bd_qk_norm_rope_fwd(q[:, part], k[:, part], v[:, part], *w, pos)
+        assert all(torch.equal(a, b[:, :, part]) for a, b in zip(got, out))
+        got = bd.bd_qk_norm_rope_bwd(*(t[:, :, part].contiguous() for t in d), q[:, part], k[:, part], *w, pos)
+        assert all(torch.equal(a, b[:, part]) for a, b in zip(got[:3], grads[:3]))
+        dw = [a + b.double() for a, b in zip(dw, got[3:])]
+    pick = torch.tensor([0, 31, 32, N // 2, N - 1], device=DEV)
+    table, pos = _np(c["rope"]), c["pos"][:, pick].cpu().numpy()
+    _close(out[0][:, :, pick], oracle.norm_rope(_np(q[:, pick]), _np(c["wq"]), table, pos, 1e-6), "large q")
+    dx, _, _ = oracle.norm_rope_backward(_np(c["dk"][:, :, pick]), _np(k[:, pick]), _np(c["wk"]), table, pos, 1e-6)
+    _close(grads[1][:, pick], dx, "large dk")
+    # both sides within 2.4e-5 of the sum of the terms' absolute values, here about N H of order 1 each
+    for got, want, H in zip(grads[3:], dw, (Hq, Hkv)):
+        assert float((got.double() - want).abs().max()) <= 2 * 2.4e-5 * N * H
 
 
 def test_positions_are_clamped_and_zero_rows_finite():
