@@ -368,7 +368,8 @@ int bd_lce_objective(const float* logp, const float* logp_old, const float* logp
  *   [0, n_rope); pos_stride 0: the same positions for every b.
  * dtype: BD_ATTN_BF16, or BD_ATTN_FP32 for float32 rows (in float32 throughout
  *   here).  wdtype: type of q_weight and k_weight [D], BD_ATTN_FP32 or dtype.
- * Arithmetic is in float32, each result is rounded once.  D is 64 or 128;
+ * Arithmetic is in float32 (values beyond 1.8e19 overflow in the mean of the
+ * squares), each result is rounded once.  D is 64 or 128;
  * B, N >= 0 (nothing is enqueued for no tokens), B * N <= 2^28, Hq and Hkv up to
  * 2^14 (Hq need not be a multiple of Hkv), eps >= 0, n_rope >= 1.  Every array
  * 16-byte aligned, positions 4-byte.  Ownership, stream order and errors are as

@@ -21,6 +21,18 @@
 //   - Items have at least one tile, empty where there is no key, so that their
 //     rows are written.  Tiles without a key are not computed; 16-row pieces
 //     without one are masked.
+//
+// Roundings: P to bfloat16, the operand type of the product with V (relative
+// error of O against float64 2.3e-3, 1.7e-3 of it the result's own rounding; P as a
+// sum of two bfloat16 values leaves 1.7e-3 and took 1% more for up to 32 rows per
+// KV head, 8% for 128); scores, maxima, sums and O are float32.
+//
+// Measured (32/8 heads of 128): 64 sequences of 512 to 8192 tokens (816 MB), one
+// token each, 135 to 143 us whatever the pages (16 to 128 rows; heads or tokens
+// outermost: the latter 3% slower), 5.7 to 6.0 TB/s; blocks of 4, 142 us (over a
+// dense cache 143); 24 sequences of 200 to 4096 (184 MB), blocks of 32, 63 us (dense
+// 63): of these 17 are the partial results of 128 rows, 30 MB written and read
+// again, and the copies alone take 45.
 #include "decode.hpp"
 
 namespace bd {

@@ -70,6 +70,19 @@ __device__ inline void st8(float* p, const float* x) {
   st16<NT>(p + 4, __builtin_bit_cast(u32x4, f32x4{x[4], x[5], x[6], x[7]}));
 }
 
+// Copies a lane's values of a row, 8 in either half, bit for bit.
+template <int D, bool NTL, bool NTS, typename T>
+__device__ inline void copy_row(const T* from, T* to, bool store) {
+  constexpr int PER = 16 / sizeof(T), N = 8 / PER;
+  u32x4 v[2 * N];
+#pragma unroll
+  for (int e = 0; e < 2 * N; ++e) v[e] = ld16<NTL>(from + e / N * (D / 2) + e % N * PER);
+  if (store) {
+#pragma unroll
+    for (int e = 0; e < 2 * N; ++e) st16<NTS>(to + e / N * (D / 2) + e % N * PER, v[e]);
+  }
+}
+
 // Sum over the 4 or 8 consecutive lanes of a row.
 template <int LPR>
 __device__ inline float row_sum(float x) {
@@ -145,15 +158,7 @@ __global__ __launch_bounds__(ROPE_NT) void rope_fwd_kernel(RopeShape s, RopeFwdA
     dst_h = (int64_t)s.N * D;
   }
   if (run.kind == 2) {
-    for (int h = run.h0; h < run.h1; ++h) {
-      float x1[8], x2[8];
-      ld8<(NT > 0)>(src + h * in.sh, x1);
-      ld8<(NT > 0)>(src + h * in.sh + D / 2, x2);
-      if (store) {
-        st8<(NT > 1)>(dst + h * dst_h, x1);
-        st8<(NT > 1)>(dst + h * dst_h + D / 2, x2);
-      }
-    }
+    for (int h = run.h0; h < run.h1; ++h) copy_row<D, (NT > 0), (NT > 1)>(src + h * in.sh, dst + h * dst_h, store);
     return;
   }
   float c[8], sn[8], w1[8], w2[8];
@@ -198,15 +203,7 @@ __global__ __launch_bounds__(ROPE_NT) void rope_bwd_kernel(RopeShape s, RopeBwdA
   const int64_t dy_h = (int64_t)s.N * D;
   T* dst = static_cast<T*>(run.kind == 0 ? a.dq : run.kind == 1 ? a.dk : a.dv) + k.b * gs.sb + k.n * gs.sn + 8 * i;
   if (run.kind == 2) {
-    for (int h = run.h0; h < run.h1; ++h) {
-      float x1[8], x2[8];
-      ld8<NT>(dy + h * dy_h, x1);
-      ld8<NT>(dy + h * dy_h + D / 2, x2);
-      if (k.valid) {
-        st8(dst + h * gs.sh, x1);
-        st8(dst + h * gs.sh + D / 2, x2);
-      }
-    }
+    for (int h = run.h0; h < run.h1; ++h) copy_row<D, NT, false>(dy + h * dy_h, dst + h * gs.sh, k.valid);
     return;
   }
   const HeadRows in = run.kind == 0 ? a.sq : a.sk;
@@ -313,11 +310,11 @@ __global__ __launch_bounds__(256) void rope_table_kernel(const double* inv_freq,
 }
 
 // Heads a workgroup takes: 1, 2, 4 or 8, as many as leave 768 workgroups (three
-// a CU), so that its tokens' cos and sin are read once for all of them.  32/8
-// heads of 128, 8192 tokens: 34.6 us, one head each 45; 2048 tokens, forward and
-// backward: 26.5, one head each 30.1 (12/4 heads, 4096 tokens: 22.3 and 25.8).
-// A power of two divides most head counts: runs of 6 and 2 instead of 4 and 4
-// took 2% more.
+// a CU), so that its tokens' cos and sin are read once for all of them.  Forward of
+// 16384 tokens, 32/8 heads of 128, one head each 95 us, two 87, eight 82 (before the
+// nontemporal accesses below); forward and backward of 2048 tokens, one 30.0, four
+// 26.5; 12/4 heads, 4096 tokens, one 25.9, two 22.3.  Powers of two divide most head
+// counts: 4096 tokens of 32/8 heads, runs of six 52.5 us, of eight 48.2.
 RopeShape with_runs(const RopeShape& shape) {
   RopeShape s = shape;
   const long long work = (long long)rope_token_blocks(s) * (s.Hq + 2 * s.Hkv);
