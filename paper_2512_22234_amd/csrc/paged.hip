@@ -22,14 +22,16 @@
 //     rows are written.  Tiles without a key are not computed; 16-row pieces
 //     without one are masked.
 //
-// Roundings: P to bfloat16, the operand type of the product with V (relative
-// error of O against float64 2.3e-3, 1.7e-3 of it the result's own rounding; P as a
-// sum of two bfloat16 values leaves 1.7e-3 and took 1% more for up to 32 rows per
-// KV head, 8% for 128); scores, maxima, sums and O are float32.
+// Roundings: O to bfloat16, relative error against float64 1.7e-3.  P enters the
+// product with V in bfloat16: one wave adds a second product with what that
+// rounding left of P (1.7e-3 in all; 2.3e-3 without, and 1% faster for 64 sequences of
+// 512 to 8192 tokens, 3% for one of 1500), teams, whose products weigh more,
+// do not (2.3e-3; with it 3.5% slower for 64 rows per KV head at D = 128, 7% at D =
+// 64, 9% for 128 rows).  Scores, maxima, sums and O's sums are float32.
 //
 // Measured (32/8 heads of 128): 64 sequences of 512 to 8192 tokens (816 MB), one
-// token each, 135 to 143 us whatever the pages (16 to 128 rows; heads or tokens
-// outermost: the latter 3% slower), 5.7 to 6.0 TB/s; blocks of 4, 142 us (over a
+// token each, 136 to 144 us whatever the pages (16 to 128 rows; heads or tokens
+// outermost: the latter 3% slower), 5.7 to 6.0 TB/s; blocks of 4, 143 us (over a
 // dense cache 143); 24 sequences of 200 to 4096 (184 MB), blocks of 32, 63 us (dense
 // 63): of these 17 are the partial results of 128 rows, 30 MB written and read
 // again, and the copies alone take 45.
@@ -517,12 +519,29 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
       }
       lsum += tree_sum<KB>(sacc);
       // O^T[d][query] += sum_key V^T[d][key] P^T[key][query]
+      if constexpr (TW == 1) {
+        bf16x8 pl[2 * KB];  // what the rounding of P left
 #pragma unroll
-      for (int c = 0; c < 2 * KB; ++c)
+        for (int c = 0; c < 2 * KB; ++c)
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
-          oacc[db] = mfma32(lds_tr<D>(cur + Smem::TILE, ops.tr_rel0, ops.tr_rel1, c, db), pb[c], oacc[db]);
-      pipeline_lds_reads<2 * KB * DB, (TW == 1 || D == 128 ? 3 : 4), 2>();
+          for (int e = 0; e < 8; ++e) pl[c][e] = (bf16)(sacc[c / 2][8 * (c & 1) + e] - (float)pb[c][e]);
+#pragma unroll
+        for (int c = 0; c < 2 * KB; ++c)
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            const bf16x8 v = lds_tr<D>(cur + Smem::TILE, ops.tr_rel0, ops.tr_rel1, c, db);
+            oacc[db] = mfma32(v, pb[c], oacc[db]);
+            oacc[db] = mfma32(v, pl[c], oacc[db]);
+          }
+        pipeline_lds_reads<4 * KB * DB, 6, 1>();
+      } else {
+#pragma unroll
+        for (int c = 0; c < 2 * KB; ++c)
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+            oacc[db] = mfma32(lds_tr<D>(cur + Smem::TILE, ops.tr_rel0, ops.tr_rel1, c, db), pb[c], oacc[db]);
+        pipeline_lds_reads<2 * KB * DB, (D == 128 ? 3 : 4), 2>();
+      }
     };
 
     uint32_t bcur = 0;                           // ring offset of the tile at pc

@@ -178,6 +178,22 @@ def test_strided_table_shared_pages_and_determinism():
         assert all(torch.equal(x, y) for x, y in zip(g, want))
 
 
+@pytest.mark.parametrize("D,S,lens", [(128, 1, [1500]), (64, 4, [700, 33, 0, 2000]), (128, 8, [300, 4000])])
+def test_one_wave_rounds_the_result_only(D, S, lens):
+    """Up to 32 query rows per KV head P enters with 16 bits: O is off by the rounding of the
+    result, at most 2^-8 of each value, and by P's, 2^-17 of the sum of |p v|, with float32 sums
+    below that (at most 2^-15 of it in all)."""
+    a = _inputs(len(lens), 16, 4, D, S, 32, 130, lens, "heads", 31 + D, S > 1)
+    o, _ = bd.bd_attn_paged_decode_fwd(*a)
+    want, _ = _oracle(*a)
+    size, _ = oracle.paged_decode_forward(_np(a[0]), _np(a[1]), np.abs(_np(a[2])), a[3].cpu().numpy(), a[4].cpu().numpy(),
+                                          _np(a[5]), None if a[6] is None else np.abs(_np(a[6])))
+    err = np.abs(_np(o) - want)
+    tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -15 * size
+    print(f"[paged] one wave D{D} S{S}: largest error / tolerance {float((err / (tol + 1e-30)).max()):.3f}", flush=True)
+    assert (err <= tol).all()
+
+
 def test_many_tiles_on_shared_pages():
     """More than 2^22 key tiles (16,500 sequences of 1024 tokens on the same pages,
     8 heads): the runs' cuts in 64 bits.  Equal queries give equal results but for
