@@ -590,8 +590,9 @@ def _row_strides(name, shape, strides):
 
 # What a call derives from shapes and strides alone (checked on the way, and
 # looked up once per combination, as a size is): the dimensions, the stride
-# array of the C call and the shapes of the results.
-_RopeLayout = collections.namedtuple("_RopeLayout", "B N Hq Hkv D strides pos_stride q_shape k_shape")
+# array of the C call, the shapes of the results and the strides of contiguous
+# gradients.
+_RopeLayout = collections.namedtuple("_RopeLayout", "B N Hq Hkv D strides pos_stride q_shape k_shape dense")
 
 
 @functools.lru_cache(maxsize=1024)
@@ -609,9 +610,10 @@ def _rope_layout(q_shape, q_strides, k_shape, k_strides, v_shape, v_strides, pos
         strides += _row_strides(name, shape, st)
     if tuple(pos_shape) not in ((N,), lead + (N,)):
         raise ValueError(f"positions: expected shape {lead + (N,)} or {(N,)}, got {tuple(pos_shape)}")
+    dense = [s for H in (Hq, Hkv, Hkv) for s in (N * H * D, H * D, D)]
     return _RopeLayout(lead[0] if lead else 1, N, Hq, Hkv, D, (ctypes.c_int64 * len(strides))(*strides),
                        N if len(pos_shape) == 2 else 0,
-                       lead + (Hq, N, D), lead + (Hkv, N, D))
+                       lead + (Hq, N, D), lead + (Hkv, N, D), (ctypes.c_int64 * 9)(*dense))
 
 
 @functools.lru_cache(maxsize=1024)
@@ -669,11 +671,11 @@ def bd_rope_table(n: int, D: int, theta: float = 1e6, inv_freq=None, device="cud
     return t
 
 
-def _result(name, t, shape, dtype, device):
-    """The caller's array for a result, checked, or a new one."""
+def _result(name, t, like, shape):
+    """The caller's array for a result, checked, or a new one, of `like`'s type and device."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    _check(name, t, shape, dtype, device)
+        return like.new_empty(*shape)  # (half the time of torch.empty with a type and a device)
+    _check(name, t, shape, like.dtype, like.device)
     return t
 
 
@@ -688,15 +690,16 @@ def bd_qk_norm_rope_fwd(q, k, v, q_weight, k_weight, rope, positions, eps: float
     k, v [B,Hkv,N,D], contiguous."""
     lay = _rope_layout(q.shape, q.stride(), k.shape, k.stride(), v.shape, v.stride(), positions.shape)
     args = _rope_inputs(lay, q, (k, v), q_weight, k_weight, rope, positions)
-    return _rope_fwd(lay, (_ptr(q), _ptr(k), _ptr(v)), args, eps, q.dtype, q.device, q_out, k_out, v_out, stream)
+    return _rope_fwd(lay, q, (_ptr(q), _ptr(k), _ptr(v)), args, eps, q_out, k_out, v_out, stream)
 
 
-def _rope_fwd(lay, ptrs, args, eps, dtype, dev, q_out=None, k_out=None, v_out=None, stream=None):
-    B, N, Hq, Hkv, D, strides, _, q_shape, k_shape = lay
+def _rope_fwd(lay, x, ptrs, args, eps, q_out=None, k_out=None, v_out=None, stream=None):
+    B, N, Hq, Hkv, D, strides, _, q_shape, k_shape = lay[:9]
+    dev = x.device
     with _launch_context(dev, stream):
-        qo = _result("q_out", q_out, q_shape, dtype, dev)
-        ko = _result("k_out", k_out, k_shape, dtype, dev)
-        vo = _result("v_out", v_out, k_shape, dtype, dev)
+        qo = _result("q_out", q_out, x, q_shape)
+        ko = _result("k_out", k_out, x, k_shape)
+        vo = _result("v_out", v_out, x, k_shape)
         st = lib().bd_qk_norm_rope_fwd(*ptrs, strides, *args[0], B, N, Hq, Hkv, D, eps, *args[1], _ptr(qo), _ptr(ko),
                                        _ptr(vo), _stream_handle(dev, stream))
     if st:
@@ -717,24 +720,27 @@ def bd_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, rope, positions, e
     args = _rope_inputs(lay, q, (k,), q_weight, k_weight, rope, positions)
     dev, dt = q.device, q.dtype
     with _launch_context(dev, stream):
-        grads = []
+        grads, strides = [], lay.dense
         for name, t, like in (("grad_q", grad_q, q), ("grad_k", grad_k, k), ("grad_v", grad_v, k)):
             if t is None:
-                t = torch.empty(like.shape, dtype=dt, device=dev)
+                t = torch.empty_like(like, memory_format=torch.contiguous_format)
             elif t.shape != like.shape or t.dtype != dt or t.device != dev:
                 raise ValueError(f"{name}: expected {dt} {tuple(like.shape)} on {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+            else:
+                strides = None
             grads.append(t)
         gq, gk, gv = grads
-        strides = _rope_layout(gq.shape, gq.stride(), gk.shape, gk.stride(), gv.shape, gv.stride(), positions.shape).strides
-        gqw = _result("grad_q_weight", grad_q_weight, (lay.D,), q_weight.dtype, dev)
-        gkw = _result("grad_k_weight", grad_k_weight, (lay.D,), q_weight.dtype, dev)
+        if strides is None:
+            strides = _rope_layout(gq.shape, gq.stride(), gk.shape, gk.stride(), gv.shape, gv.stride(), positions.shape).strides
+        gqw = _result("grad_q_weight", grad_q_weight, q_weight, (lay.D,))
+        gkw = _result("grad_k_weight", grad_k_weight, q_weight, (lay.D,))
         _rope_bwd(lay, (dq, dk, dv), (_ptr(q), _ptr(k)), args, eps, dt, dev, (_ptr(gq), _ptr(gk), _ptr(gv)),
                   strides, gqw, gkw, workspace, stream)
     return (*grads, gqw, gkw)
 
 
 def _rope_bwd(lay, dy, ptrs, args, eps, dtype, dev, grad_ptrs, grad_strides, gqw, gkw, workspace=None, stream=None):
-    B, N, Hq, Hkv, D, strides, _, q_shape, k_shape = lay
+    B, N, Hq, Hkv, D, strides, _, q_shape, k_shape = lay[:9]
     dq, dk, dv = dy
     _check("dq", dq, q_shape, dtype, dev)
     _check("dk", dk, k_shape, dtype, dev)
@@ -774,7 +780,7 @@ class QkvNormRopeFunction(torch.autograd.Function):
         D = q_weight.numel()
         lay = _qkv_layout(qkv.shape, qkv.stride(), Hq, Hkv, D, positions.shape)
         args = _rope_inputs(lay, qkv, (), q_weight, k_weight, rope, positions)
-        return _rope_fwd(lay, QkvNormRopeFunction._parts(qkv, Hq, Hkv, D), args, eps, qkv.dtype, qkv.device)
+        return _rope_fwd(lay, qkv, QkvNormRopeFunction._parts(qkv, Hq, Hkv, D), args, eps)
 
     @staticmethod
     def _parts(qkv, Hq, Hkv, D):
@@ -792,7 +798,7 @@ class QkvNormRopeFunction(torch.autograd.Function):
         lay = _qkv_layout(qkv.shape, qkv.stride(), Hq, Hkv, D, positions.shape)
         args = _rope_inputs(lay, qkv, (), q_weight, k_weight, rope, positions)
         with _launch_context(dev, None):
-            grad = torch.empty(qkv.shape, dtype=dt, device=dev)
+            grad = torch.empty_like(qkv, memory_format=torch.contiguous_format)
             gqw, gkw = torch.empty_like(q_weight), torch.empty_like(k_weight)
             strides = _qkv_layout(grad.shape, grad.stride(), Hq, Hkv, D, positions.shape).strides
             _rope_bwd(lay, (dq.contiguous(), dk.contiguous(), dv.contiguous()),
@@ -864,7 +870,7 @@ def bd_qk_norm_rope_paged(q, k, v, q_weight, k_weight, rope, positions, slots, k
     """bd_qk_norm_rope_fwd for serving: returns the queries [B,Hq,N,D] and writes keys and values into
     the pages, token (b, n) at row slots[b, n] (int32 [B,N] of bd_paged_plan; outside the pages: not written)."""
     lay = _rope_layout(q.shape, q.stride(), k.shape, k.stride(), v.shape, v.stride(), positions.shape)
-    B, N, Hq, Hkv, D, strides, _, q_shape, _ = lay
+    B, N, Hq, Hkv, D, strides, _, q_shape = lay[:8]
     dev = q.device
     if q.dtype != torch.bfloat16:
         raise TypeError(f"bd_qk_norm_rope_paged supports bfloat16 tensors, got {q.dtype}")
@@ -872,7 +878,7 @@ def bd_qk_norm_rope_paged(q, k, v, q_weight, k_weight, rope, positions, slots, k
     _check("slots", slots, q.shape[:-2], torch.int32, dev)
     pages = _pages(k_pages, v_pages, Hkv, D, dev)
     with _launch_context(dev, stream):
-        o = _result("q_out", q_out, q_shape, torch.bfloat16, dev)
+        o = _result("q_out", q_out, q, q_shape)
         st = lib().bd_qk_norm_rope_paged(_ptr(q), _ptr(k), _ptr(v), strides, *head, _ptr(slots), B, N, Hq, Hkv, D, eps,
                                          *types, _ptr(o), _ptr(k_pages), _ptr(v_pages), *pages, _stream_handle(dev, stream))
     if st:
@@ -908,13 +914,12 @@ def bd_paged_plan(cache_lens, new_lens, page_table, free_pages, free_head, num_p
         raise ValueError(f"S: at least 1 expected, got {S}")
     S_, total_ = (0, int(total)) if S is None else (int(S), 0)
     shape = (B, S_) if S_ else (total_,)
-    i32 = torch.int32
     with _launch_context(dev, stream):
-        lens = _result("lens", lens, (B,), i32, dev)
-        cu = _result("cu", cu, (B + 1,), i32, dev)
-        slots = _result("slots", slots, shape, i32, dev)
-        positions = _result("positions", positions, shape, i32, dev)
-        state = _result("state", state, (2,), i32, dev)
+        lens = _result("lens", lens, cache_lens, (B,))
+        cu = _result("cu", cu, cache_lens, (B + 1,))
+        slots = _result("slots", slots, cache_lens, shape)
+        positions = _result("positions", positions, cache_lens, shape)
+        state = _result("state", state, cache_lens, (2,))
         st = lib().bd_paged_plan(_ptr(cache_lens), _ptr(new_lens), _ptr(page_table), B, page_table.shape[1], table_stride,
                                  _ptr(free_pages), free_pages.shape[0], _ptr(free_head), num_pages, page_size, S_, total_,
                                  _ptr(lens), _ptr(cu), _ptr(slots), _ptr(positions), _ptr(state),
@@ -956,8 +961,12 @@ def bd_attn_paged_decode_fwd(q, k_pages, v_pages, page_table, cache_lens, k_new=
         _check("v_new", v_new, (B, Hkv, S, D), bf16, dev)
         kn, vn = _ptr(k_new), _ptr(v_new)
     with _launch_context(dev, stream):
-        o = _result("out", out, shape, bf16, dev)
-        l_ = _result("lse", lse, (B, Hq, S), torch.float32, dev)
+        o = _result("out", out, q, shape)
+        l_ = lse
+        if l_ is None:
+            l_ = torch.empty((B, Hq, S), dtype=torch.float32, device=dev)
+        else:
+            _check("lse", l_, (B, Hq, S), torch.float32, dev)
         nbytes = _known_size("bd_attn_paged_decode_workspace_bytes", B, S, Hq, Hkv, D, P, width, BD_ATTN_BF16)
         ws, wp, wn = _workspace(nbytes, dev, workspace)
         st = lib().bd_attn_paged_decode_fwd(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(cache_lens), kn,
