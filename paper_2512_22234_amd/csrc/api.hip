@@ -163,16 +163,21 @@ int validate_lce(int N, int V, int Dm, int dtype, bd::LceShape& s) {
 
 // ---- strided arrays of head rows and of pages ----
 
-constexpr int64_t kMaxStride = (int64_t)1 << 40;  // elements: extents below stay far inside 64 bits
+// Elements that an array may span (64 TiB of float32: no memory is as large, and sums of a
+// few such spans stay far inside 64 bits).
+constexpr int64_t kMaxExtent = (int64_t)1 << 44;
 
 struct Dim {
   int64_t n, stride;
 };
 // Elements from the first to past the last one of rows of D values at the given
-// (non-negative) strides.
+// (non-negative) strides; more than kMaxExtent if a dimension spans that much.
 int64_t extent(const Dim* d, int k, int D) {
   int64_t e = D;
-  for (int i = 0; i < k; ++i) e += (d[i].n - 1) * d[i].stride;
+  for (int i = 0; i < k; ++i) {
+    if (d[i].n > 1 && d[i].stride > kMaxExtent / (d[i].n - 1)) return kMaxExtent + 1;
+    e += (d[i].n - 1) * (d[i].n > 1 ? d[i].stride : 0);
+  }
   return e;
 }
 // Do no two of those rows share an element?  (Sufficient: sorted by stride, each
@@ -203,9 +208,9 @@ struct Rows {
 };
 bool make_rows(const void* p, const int64_t* st, int B, int N, int H, int D, size_t esz, Rows& r) {
   for (int i = 0; i < 3; ++i)
-    if (st[i] < 0 || st[i] % 8 != 0 || st[i] > kMaxStride) return false;
+    if (st[i] < 0 || st[i] % 8 != 0 || st[i] > kMaxExtent) return false;
   r = Rows{p, {{B, st[0]}, {N, st[1]}, {H, st[2]}}, esz, D};
-  return p != nullptr && aligned(p, 16);
+  return p != nullptr && aligned(p, 16) && extent(r.d, 3, D) <= kMaxExtent;
 }
 bd::HeadRows head_rows(const int64_t* st) { return bd::HeadRows{st[0], st[1], st[2]}; }
 
@@ -235,10 +240,12 @@ bool make_pages(const void* K, const void* V, int num, int page_size, int64_t sp
   g = bd::PageLayout{num, page_log(page_size), sp, sh, sr};
   if (num < 1 || g.log_size < 0 || (int64_t)num << g.log_size > INT32_MAX) return false;
   for (const int64_t st : {sp, sh, sr})
-    if (st < 0 || st % 8 != 0 || st > kMaxStride) return false;
+    if (st < 0 || st % 8 != 0 || st > kMaxExtent) return false;
   if (!K || !V || !aligned(K, 16) || !aligned(V, 16)) return false;
   Dim d[4] = {{num, sp}, {Hkv, sh}, {page_size, sr}, {2, 0}};
-  const size_t n = (size_t)extent(d, 3, D) * 2;
+  const int64_t e = extent(d, 3, D);
+  if (e > kMaxExtent) return false;
+  const size_t n = (size_t)e * 2;
   k = Range{K, n};
   v = Range{V, n};
   if (!write) return true;
@@ -281,8 +288,11 @@ bool rope_inputs(const bd::RopeShape& s, const void* wq, const void* wk, Range* 
   if (!s.rope || !s.pos || !wq || !wk || !aligned(s.rope, 16) || !aligned(s.pos, 4) || !aligned(wq, 16) || !aligned(wk, 16))
     return false;
   const size_t wn = (size_t)s.D * (s.w32 ? 4 : 2);
+  const Dim seqs{s.B, s.pos_stride};
+  const int64_t n_pos = extent(&seqs, 1, s.N);
+  if (n_pos > kMaxExtent) return false;
   in[0] = Range{s.rope, (size_t)s.n_rope * s.D * 4};
-  in[1] = Range{s.pos, ((size_t)(s.B - 1) * s.pos_stride + s.N) * 4};
+  in[1] = Range{s.pos, (size_t)n_pos * 4};
   in[2] = Range{wq, wn};
   in[3] = Range{wk, wn};
   return true;
@@ -868,8 +878,11 @@ int bd_paged_plan(const int32_t* cache_lens, const int32_t* new_lens, int32_t* p
   const int lg = page_log(page_size);
   if (B < 1 || B > (1 << 16) || max_pages < 1 || lg < 0 || (int64_t)max_pages << lg > (1 << 30) || num_pages < 1 ||
       (int64_t)num_pages << lg > INT32_MAX || n_free < 0 || S < 0 || (int64_t)B * S > (1 << 30) ||
-      table_stride < max_pages || table_stride > kMaxStride)
+      table_stride < max_pages)
     return BD_ATTN_ERR_INVALID_ARGUMENT;
+  const Dim rows{B, table_stride};
+  const int64_t n_table = extent(&rows, 1, max_pages);
+  if (n_table > kMaxExtent) return BD_ATTN_ERR_INVALID_ARGUMENT;
   const int T = S > 0 ? B * S : total;
   if (T < 0 || T > (1 << 30)) return BD_ATTN_ERR_INVALID_ARGUMENT;
   if (!cache_lens || !new_lens || !page_table || (n_free > 0 && !free_pages) || !free_head || !lens || !cu || !state ||
@@ -877,7 +890,7 @@ int bd_paged_plan(const int32_t* cache_lens, const int32_t* new_lens, int32_t* p
     return BD_ATTN_ERR_INVALID_ARGUMENT;
   const Range in[] = {{cache_lens, (size_t)B * 4}, {new_lens, (size_t)B * 4}, {free_pages, (size_t)n_free * 4},
                       {free_head, 4}};
-  const Range out[] = {{page_table, ((size_t)(B - 1) * table_stride + max_pages) * 4},
+  const Range out[] = {{page_table, (size_t)n_table * 4},
                        {lens, (size_t)B * 4}, {cu, (size_t)(B + 1) * 4}, {slots, (size_t)T * 4},
                        {positions, (size_t)T * 4}, {state, 8}};
   for (const Range& i : in)
@@ -915,9 +928,11 @@ int bd_attn_paged_decode_fwd(const void* Q, const void* K_pages, const void* V_p
   if (!make_pages(K_pages, V_pages, num_pages, page_size, page_stride, head_stride, row_stride, Hkv, D, false, a.pages,
                   pages[0], pages[1]) ||
       page_stride > INT32_MAX || row_stride < D || row_stride > (1 << 20) || row_stride * page_size > (1 << 30) ||
-      table_stride < 0 || table_stride > kMaxStride ||
-      (B > 1 && table_stride != 0 && table_stride < max_pages))
+      table_stride < 0 || (B > 1 && table_stride != 0 && table_stride < max_pages))
     return BD_ATTN_ERR_INVALID_ARGUMENT;
+  const Dim rows{B, table_stride};
+  const int64_t n_table = extent(&rows, 1, max_pages);
+  if (n_table > kMaxExtent) return BD_ATTN_ERR_INVALID_ARGUMENT;
   const size_t need = bd::decode_workspace_bytes(s);
   if (!Q || !page_table || !cache_lens || !O || !LSE || !ws || (K_new == nullptr) != (V_new == nullptr))
     return BD_ATTN_ERR_INVALID_ARGUMENT;
@@ -926,7 +941,7 @@ int bd_attn_paged_decode_fwd(const void* Q, const void* K_pages, const void* V_p
     return BD_ATTN_ERR_INVALID_ARGUMENT;
   if (ws_bytes < need) return BD_ATTN_ERR_WORKSPACE_TOO_SMALL;
   const size_t nq = (size_t)B * Hq * S, nkn = K_new ? (size_t)B * Hkv * S * D * 2 : 0;
-  const Range in[] = {{Q, nq * D * 2}, pages[0], pages[1], {page_table, ((size_t)(B - 1) * table_stride + max_pages) * 4},
+  const Range in[] = {{Q, nq * D * 2}, pages[0], pages[1], {page_table, (size_t)n_table * 4},
                       {cache_lens, (size_t)B * 4}, {K_new, nkn}, {V_new, nkn}};
   const Range out[] = {{O, nq * D * 2}, {LSE, nq * 4}, {ws, need}};
   for (const Range& o : out)

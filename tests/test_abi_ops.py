@@ -277,3 +277,20 @@ def test_paged_plan_binding_refusals(change, kw, error):
     a.update(change)
     with pytest.raises(error):
         bd.bd_paged_plan(*a.values(), 16, 16, **kw)
+
+
+# Strides whose products wrap 64 bits to nothing, so that the spans would seem to fit.
+WRAPS = (0, 1 << 40, 64) * 3
+
+
+def test_strides_past_any_memory_are_refused():
+    rows = dict(B=1, N=(1 << 24) + 1, pos_stride=0)
+    assert _rope_fwd(**rows, st=WRAPS) == 1
+    assert _rope_bwd(**rows, st=WRAPS) == 1
+    assert _rope_bwd(**rows, gst=WRAPS, ws_bytes=1 << 34) == 1
+    assert _rope_paged(**rows, st=WRAPS) == 1
+    seqs = dict(B=(1 << 14) + 1, pos_stride=1 << 48)
+    assert _rope_fwd(**seqs) == 1 and _rope_bwd(**seqs, ws_bytes=1 << 30) == 1 and _rope_paged(**seqs) == 1
+    assert _rope_paged(num=(1 << 24) + 1, sp=1 << 40) == 1
+    assert _plan(B=(1 << 14) + 1, ts=1 << 48) == 1
+    assert _paged(B=(1 << 14) + 1, ts=1 << 48, ws_bytes=1 << 40) == 1
