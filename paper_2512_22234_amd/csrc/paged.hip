@@ -90,7 +90,7 @@ __device__ inline int paged_runs(int T) {
 }
 // First tile of run gw <= n (the runs cut T tiles into n near-equal pieces).
 __device__ inline int paged_run_start(int gw, int n, int T) {
-  if (T < 1 << 22) return (int)((unsigned)(gw * T) / (unsigned)n);
+  if (T < 1 << 22) return (int)((unsigned)gw * (unsigned)T / (unsigned)n);
   return (int)((unsigned)(((unsigned long long)gw * T) >> 8) / ((unsigned)n >> 8));  // (n is a multiple of 256 here)
 }
 

@@ -50,25 +50,22 @@ __device__ inline int plan_free(const PlanArgs& a, long long at) {
 __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
   // tokens and pages of the sequences before those of thread t
   __shared__ long long tok0[PLAN_NT + 1];
-  __shared__ int need0[PLAN_NT + 1];
+  __shared__ long long need0[PLAN_NT + 1];
   __shared__ long long wtok[PLAN_NT / 64];
-  __shared__ int wneed[PLAN_NT / 64];
+  __shared__ long long wneed[PLAN_NT / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int cpt = cdiv(a.B, PLAN_NT);  // consecutive sequences of a thread
   const int c0 = imin(a.B, tid * cpt), c1 = imin(a.B, c0 + cpt);
-  long long tok = 0;
-  int need = 0;
+  long long tok = 0, need = 0;
   for (int b = c0; b < c1; ++b) {
     const PlanSeq q = plan_seq(a, b);
     tok += q.fresh;
     need += q.need;
   }
-  long long itok = tok;
-  int ineed = need;
+  long long itok = tok, ineed = need;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const long long u = __shfl_up(itok, o, 64);
-    const int v = __shfl_up(ineed, o, 64);
+    const long long u = __shfl_up(itok, o, 64), v = __shfl_up(ineed, o, 64);
     if (lane >= o) {
       itok += u;
       ineed += v;
@@ -108,7 +105,7 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
   // the new head of the free list, and the tokens that have no page
   if (blockIdx.x == 0) {
     long long lost = 0;
-    int first = need0[tid];
+    long long first = need0[tid];
     for (int b = c0; b < c1; ++b) {
       const PlanSeq q = plan_seq(a, b);
       lost += q.fresh - (q.end - q.len);
@@ -142,7 +139,7 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
   for (int t = t0 + tid; t < t1; t += PLAN_NT) {
     int b, c, i;  // token i of sequence b
     PlanSeq q;
-    int first;  // pages of the sequences before b
+    long long first;  // pages of the sequences before b
     bool real = true;
     if (a.S > 0) {
       b = t / a.S;

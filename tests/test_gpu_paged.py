@@ -194,11 +194,12 @@ def test_one_wave_rounds_the_result_only(D, S, lens):
     assert (err <= tol).all()
 
 
-def test_many_tiles_on_shared_pages():
-    """More than 2^22 key tiles (16,500 sequences of 1024 tokens on the same pages,
-    8 heads): the runs' cuts in 64 bits.  Equal queries give equal results but for
-    where the runs cut them: float32 sums, P rounded to bf16."""
-    B, H, D, P, n = 16500, 8, 64, 64, 1024
+@pytest.mark.parametrize("B", [16000, 16500])
+def test_many_tiles_on_shared_pages(B):
+    """Just below and above 2^22 key tiles (sequences of 1024 tokens on the same
+    pages, 8 heads): the runs' cuts in 32 and in 64 bits.  Equal queries give equal
+    results but for where the runs cut them: float32 sums, P rounded to bf16."""
+    H, D, P, n = 8, 64, 64, 1024
     g = torch.Generator().manual_seed(4)
     kp, vp = _pages(n // P, H, P, D, "heads", g)
     q = (torch.randn((1, H, 1, D), generator=g) * 0.5).to(BF).to(DEV).repeat(B, 1, 1, 1)
@@ -320,6 +321,19 @@ def test_plan_too_small_a_total():
                             positions=buf[16:28])
     assert (buf[12:16] == 77).all() and (buf[28:] == 77).all()
     assert plan.slots.tolist() == list(range(10)) + [16, 17] and int(plan.state[1]) > 0
+
+
+def test_plan_of_more_pages_than_an_int_counts():
+    """40 sequences that would need 2^26 pages each: the list gives what it has, the head stays inside it."""
+    i32 = dict(dtype=torch.int32, device=DEV)
+    width = 1 << 26  # (rows of 2^30 tokens; a row's entries are written for the tokens below total alone)
+    table = torch.empty((40, width), **i32)
+    table[0, 0] = -1
+    plan = bd.bd_paged_plan(torch.zeros(40, **i32), torch.full((40,), 1 << 30, **i32), table, torch.arange(8, **i32),
+                            torch.tensor([3], **i32), 8, 16, total=4)
+    assert int(table[0, 0]) == 3 and plan.slots.tolist() == [48, 49, 50, 51]
+    assert plan.lens.tolist() == [1 << 30] * 40 and plan.cu.tolist() == [0, 1 << 30] + [2**31 - 1] * 39
+    assert plan.state.tolist() == [8, 2**31 - 1]
 
 
 # ---------------------------------------------------------------------------
