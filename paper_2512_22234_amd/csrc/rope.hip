@@ -16,7 +16,7 @@
 // halves of a row (16-byte accesses, pairs of the rotation in one lane), D / 16
 // lanes a row; a workgroup takes 256 / (D / 16) consecutive tokens, whose cos
 // and sin stay in registers, and a run of heads of one kind (q, k or v).
-// Measured: 16384 tokens of 32/8 heads of 128, forward: 77 us, 5.2 TB/s (a copy
+// Measured: 16384 tokens of 32/8 heads of 128, forward: 76 us, 5.4 TB/s (a copy
 // of 1 GiB: 5.1).
 #include "device.hpp"
 #include "kernels.hpp"
