@@ -23,18 +23,20 @@
 //     without one are masked.
 //
 // Roundings: O to bfloat16, relative error against float64 1.7e-3.  P enters the
-// product with V in bfloat16: one wave adds a second product with what that
-// rounding left of P (1.7e-3 in all; 2.3e-3 without, and 1% faster for 64 sequences of
-// 512 to 8192 tokens, 3% for one of 1500), teams, whose products weigh more,
-// do not (2.3e-3; with it 3.5% slower for 64 rows per KV head at D = 128, 7% at D =
-// 64, 9% for 128 rows).  Scores, maxima, sums and O's sums are float32.
+// product with V as two bfloat16 parts, the second being what the rounding of the
+// first left: 16 bits of P in all, so that O is off by its own rounding alone.  In one
+// part (2.3e-3, values that cancel by several of their steps) a call takes 1% less for
+// 64 sequences of 512 to 8192 tokens, 3% for one of 1500, 5 to 7% for 64 rows per KV head
+// (32 sequences of 128 to 2048, D = 128: 31.0 us, two parts 32.4; D = 64: 22.2, 23.7) and
+// 10% for 128 rows (24 sequences: 62.9, 69.5).  Scores, maxima, sums and O's sums are
+// float32.
 //
 // Measured (32/8 heads of 128): 64 sequences of 512 to 8192 tokens (816 MB), one
 // token each, 136 to 144 us whatever the pages (16 to 128 rows; heads or tokens
 // outermost: the latter 3% slower), 5.7 to 6.0 TB/s; blocks of 4, 143 us (over a
-// dense cache 143); 24 sequences of 200 to 4096 (184 MB), blocks of 32, 63 us (dense
-// 63): of these 17 are the partial results of 128 rows, 30 MB written and read
-// again, and the copies alone take 45.
+// dense cache 143); 24 sequences of 200 to 4096 (184 MB), blocks of 32, 69.5 us (dense,
+// with P in one part, 63): the partial results of 128 rows, 27 MB written and read
+// again, and one team of four waves a CU, which waits for each tile in turn.
 #include "decode.hpp"
 
 namespace bd {
@@ -519,29 +521,20 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
       }
       lsum += tree_sum<KB>(sacc);
       // O^T[d][query] += sum_key V^T[d][key] P^T[key][query]
-      if constexpr (TW == 1) {
-        bf16x8 pl[2 * KB];  // what the rounding of P left
+      bf16x8 pl[2 * KB];  // what the rounding of P left
 #pragma unroll
-        for (int c = 0; c < 2 * KB; ++c)
+      for (int c = 0; c < 2 * KB; ++c)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) pl[c][e] = (bf16)(sacc[c / 2][8 * (c & 1) + e] - (float)pb[c][e]);
+        for (int e = 0; e < 8; ++e) pl[c][e] = (bf16)(sacc[c / 2][8 * (c & 1) + e] - (float)pb[c][e]);
 #pragma unroll
-        for (int c = 0; c < 2 * KB; ++c)
+      for (int c = 0; c < 2 * KB; ++c)
 #pragma unroll
-          for (int db = 0; db < DB; ++db) {
-            const bf16x8 v = lds_tr<D>(cur + Smem::TILE, ops.tr_rel0, ops.tr_rel1, c, db);
-            oacc[db] = mfma32(v, pb[c], oacc[db]);
-            oacc[db] = mfma32(v, pl[c], oacc[db]);
-          }
-        pipeline_lds_reads<4 * KB * DB, 6, 1>();
-      } else {
-#pragma unroll
-        for (int c = 0; c < 2 * KB; ++c)
-#pragma unroll
-          for (int db = 0; db < DB; ++db)
-            oacc[db] = mfma32(lds_tr<D>(cur + Smem::TILE, ops.tr_rel0, ops.tr_rel1, c, db), pb[c], oacc[db]);
-        pipeline_lds_reads<2 * KB * DB, (D == 128 ? 3 : 4), 2>();
-      }
+        for (int db = 0; db < DB; ++db) {
+          const bf16x8 v = lds_tr<D>(cur + Smem::TILE, ops.tr_rel0, ops.tr_rel1, c, db);
+          oacc[db] = mfma32(v, pb[c], oacc[db]);
+          oacc[db] = mfma32(v, pl[c], oacc[db]);
+        }
+      pipeline_lds_reads<4 * KB * DB, 6, 1>();
     };
 
     uint32_t bcur = 0;                           // ring offset of the tile at pc

@@ -194,6 +194,22 @@ def test_one_wave_rounds_the_result_only(D, S, lens):
     assert (err <= tol).all()
 
 
+@pytest.mark.parametrize("D,S,lens", [(128, 16, [700, 33]), (64, 16, [1, 1000]), (128, 32, [40, 1500]), (64, 32, [600, 0, 97]),
+                                      (128, 64, [150, 900])])
+@pytest.mark.parametrize("block", [False, True])
+def test_teams_round_the_result_only(D, S, lens, block):
+    """The same with more rows per KV head (64, 128, and 256 in two groups): P has 16 bits there too."""
+    a = _inputs(len(lens), 8, 2, D, S, 32, 60, lens, "heads", 57 + D + S, block)
+    o, _ = bd.bd_attn_paged_decode_fwd(*a)
+    want, _ = _oracle(*a)
+    size, _ = oracle.paged_decode_forward(_np(a[0]), _np(a[1]), np.abs(_np(a[2])), a[3].cpu().numpy(), a[4].cpu().numpy(),
+                                          _np(a[5]), None if a[6] is None else np.abs(_np(a[6])))
+    err = np.abs(_np(o) - want)
+    tol = 2.0 ** -8 * np.abs(want) + 2.0 ** -15 * size
+    print(f"[paged] teams D{D} S{S} block={block}: largest error / tolerance {float((err / (tol + 1e-30)).max()):.3f}", flush=True)
+    assert (err <= tol).all()
+
+
 @pytest.mark.parametrize("B", [16000, 16500])
 def test_many_tiles_on_shared_pages(B):
     """Just below and above 2^22 key tiles (sequences of 1024 tokens on the same
