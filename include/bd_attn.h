@@ -445,8 +445,9 @@ int bd_rope_table(const double* inv_freq, int n, int D, float* table, hipStream_
  *   for tokens without a page; positions, len_b + i of each new token, 0 in rows
  *   that hold none; state [2], the free list's new head (at most n_free), and
  *   the number of new tokens without a slot, 0 if all is well: those past the
- *   room, in the pages that the free list could not give (entered as -1), behind
- *   cached tokens whose last page is none, or past total.
+ *   room, in the pages that the free list could not give or for which it held an id
+ *   outside the pool (both entered as -1), behind cached tokens whose last page is
+ *   none, or past total.
  * B from 1 to 2^16, max_pages >= 1, max_pages * page_size <= 2^30, page_size a
  * power of two from 16 to 2^15, num_pages * page_size <= 2^31 - 1, B * S and total at most 2^30.
  * All arrays are on the device, 4-byte aligned; outputs must not overlap

@@ -13,9 +13,9 @@
 // The work is a prefix sum over the sequences and a few integer operations a
 // token: bound by launch and load latency.  One launch: every workgroup scans
 // all lengths (8 bytes a sequence, from L2) and then takes a contiguous run of
-// tokens; a token finds its sequence by a search of the scan.  The token that
-// starts a page writes the page's table entry, the others read the same entry
-// of the free list, so no workgroup waits for another.  The kernel takes 3.8 us for
+// tokens, the first one the state; a token finds its sequence by a search of the scan.
+// The token that starts a page writes the page's table entry, the others read the
+// same entry of the free list, so no workgroup waits for another.  The kernel takes 3.8 us for
 // 64 sequences of 4 tokens and 6.4 for 82,000 tokens of 700 sequences.
 #include "device.hpp"
 #include "kernels.hpp"
@@ -45,6 +45,14 @@ __device__ inline int plan_free(const PlanArgs& a, long long at) {
   if (at >= a.n_free) return -1;
   const int id = a.free_pages[at];
   return id >= 0 && id < a.num_pages ? id : -1;
+}
+// The last thread whose sequences start at or before token (or page) x, by the sums before each thread.
+__device__ inline int plan_find(const long long* before, long long x) {
+  int c = 0;
+#pragma unroll
+  for (int step = PLAN_NT / 2; step > 0; step >>= 1)
+    if (before[c + step] <= x) c += step;
+  return c;
 }
 
 __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
@@ -91,19 +99,9 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
   const long long head = imin(imax(a.free_head[0], 0), a.n_free);
   const int P = 1 << a.log_size, cap = a.width << a.log_size;
 
-  // the sequences' own outputs: thread t's are written by workgroup t mod grid
-  if (tid % (int)gridDim.x == (int)blockIdx.x) {
-    long long t = tok0[tid];
-    for (int b = c0; b < c1; ++b) {
-      const PlanSeq q = plan_seq(a, b);
-      a.lens_out[b] = q.end;
-      a.cu[b] = (int)(t < INT32_MAX ? t : INT32_MAX);
-      t += q.fresh;
-    }
-    if (c0 < c1 && c1 == a.B) a.cu[a.B] = (int)(t < INT32_MAX ? t : INT32_MAX);
-  }
-  // the new head of the free list, and the tokens that have no page
-  if (blockIdx.x == 0) {
+  // The first workgroup: the new head of the free list, and the tokens that have no page.
+  const int workers = (int)gridDim.x - 1, worker = (int)blockIdx.x - 1;
+  if (worker < 0) {
     long long lost = 0;
     long long first = need0[tid];
     for (int b = c0; b < c1; ++b) {
@@ -120,6 +118,30 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
       }
       first += q.need;
     }
+    // tokens in pages whose entry of the list is no page: every entry taken is looked at, eight loads at a time; a
+    // sequence is sought for the bad ones alone
+    const long long pages = need0[PLAN_NT];
+    const long long given = pages < a.n_free - head ? pages : a.n_free - head;
+    for (long long u0 = tid; u0 < given; u0 += 8 * PLAN_NT) {
+      int id[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) id[e] = u0 + e * PLAN_NT < given ? a.free_pages[head + u0 + e * PLAN_NT] : 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (id[e] >= 0 && id[e] < a.num_pages) continue;
+        const long long u = u0 + e * PLAN_NT;
+        const int c = plan_find(need0, u);
+        int b = c * cpt;
+        long long at = u - need0[c];  // page among those of the sequences of thread c
+        PlanSeq q = plan_seq(a, b);
+        while (at >= q.need) {  // (ends: thread c's sequences need need0[c + 1] - need0[c] > u - need0[c] pages)
+          at -= q.need;
+          q = plan_seq(a, ++b);
+        }
+        const int begin = (q.p0 + (int)at) << a.log_size;
+        lost += imin(q.end - begin, P);
+      }
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) lost += __shfl_xor(lost, o);
     if (lane == 0) wtok[wave] = lost;
@@ -128,14 +150,27 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
       long long sum = 0;
       for (int v = 0; v < PLAN_NT / 64; ++v) sum += wtok[v];
       if (a.S == 0 && total > a.T) sum += total - a.T;
-      const long long used = head + need0[PLAN_NT];
+      const long long used = head + pages;
       a.state[0] = (int)(used < a.n_free ? used : a.n_free);
       a.state[1] = (int)(sum < INT32_MAX ? sum : INT32_MAX);
     }
+    return;
+  }
+
+  // the sequences' own outputs: thread t's are written by worker t mod workers
+  if (tid % workers == worker) {
+    long long t = tok0[tid];
+    for (int b = c0; b < c1; ++b) {
+      const PlanSeq q = plan_seq(a, b);
+      a.lens_out[b] = q.end;
+      a.cu[b] = (int)(t < INT32_MAX ? t : INT32_MAX);
+      t += q.fresh;
+    }
+    if (c0 < c1 && c1 == a.B) a.cu[a.B] = (int)(t < INT32_MAX ? t : INT32_MAX);
   }
 
   // tokens: a contiguous run for each workgroup
-  const int t0 = (int)((long long)a.T * blockIdx.x / gridDim.x), t1 = (int)((long long)a.T * (blockIdx.x + 1) / gridDim.x);
+  const int t0 = (int)((long long)a.T * worker / workers), t1 = (int)((long long)a.T * (worker + 1) / workers);
   for (int t = t0 + tid; t < t1; t += PLAN_NT) {
     int b, c, i;  // token i of sequence b
     PlanSeq q;
@@ -150,10 +185,7 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
       q = plan_seq(a, b);
       real = i < q.fresh;
     } else if (t < total) {
-      c = 0;  // the last thread whose sequences start at or before t
-#pragma unroll
-      for (int step = PLAN_NT / 2; step > 0; step >>= 1)
-        if (tok0[c + step] <= t) c += step;
+      c = plan_find(tok0, t);
       i = t - (int)tok0[c];
       first = need0[c];
       b = c * cpt;
@@ -190,10 +222,10 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
 }  // namespace
 
 hipError_t launch_plan(const PlanArgs& a, hipStream_t st) {
-  // a workgroup for each 256 tokens (one a thread) and 256 sequences: 82,000 tokens of 700 sequences 7.4 us a call,
-  // with 1024 tokens a workgroup 9.7
+  // a workgroup for each 256 tokens (one a thread) and 256 sequences, and one for the state: 82,000 tokens of 700
+  // sequences 7.4 us a call, with 1024 tokens a workgroup 9.7
   const int work = imax(a.T / PLAN_NT, a.B / PLAN_NT);
-  hipLaunchKernelGGL(plan_kernel, dim3(imin(imax(work, 1), 2048)), dim3(PLAN_NT), 0, st, a);
+  hipLaunchKernelGGL(plan_kernel, dim3(imin(imax(work, 1), 2048) + 1), dim3(PLAN_NT), 0, st, a);
   return hipGetLastError();
 }
 

@@ -339,6 +339,30 @@ def test_plan_too_small_a_total():
     assert plan.slots.tolist() == list(range(10)) + [16, 17] and int(plan.state[1]) > 0
 
 
+def _damaged(B, P, width, pages, seed, bad):
+    """Lengths, new lengths, a table of stale ids and a free list with a share of ids outside the pool."""
+    rng = np.random.default_rng(seed)
+    lens = rng.integers(0, width * P + 1, B)
+    new = rng.integers(0, 3 * P, B) * (rng.random(B) < 0.8)
+    table = rng.integers(0, pages, (B, width))
+    free = np.where(rng.random(2 * B) < bad, rng.choice([-1, -(1 << 31), pages, (1 << 31) - 1], 2 * B), rng.permutation(2 * B) % pages)
+    return lens, new, table, free
+
+
+@pytest.mark.parametrize("S", [20, None])
+def test_plan_counts_the_tokens_of_ids_outside_the_pool(S):
+    """state[1] is exact where the free list holds ids outside the pool: in a whole page, the
+    last one of a sequence, several in a row, and behind a list that runs out."""
+    total = None if S else 70
+    _plan_check([0, 0], [20, 4], np.full((2, 3), -1), [1, 50, -4, 2], 0, 8, 16, S, total)
+    table = np.array([[4, 5, 6], [7, 3, 3], [3, 3, 3], [3, 9, 3]])
+    _plan_check([0, 3, 0, 32], [17, 20, 0, 7], table, [8, 8, 1, 99], 0, 8, 16, S, total)
+    _plan_check([0, 3, 0, 32], [17, 20, 0, 7], table, [0, -9, 8], 1, 8, 16, S, total)
+    for B in (40, 700):
+        lens, new, table, free = _damaged(B, 16, 5, 900, B, 0.3)
+        _plan_check(lens, new, table, free, 3, 900, 16, S, None if S else int(new.sum()) + 5)
+
+
 def test_plan_of_more_pages_than_an_int_counts():
     """40 sequences that would need 2^26 pages each: the list gives what it has, the head stays inside it."""
     i32 = dict(dtype=torch.int32, device=DEV)
