@@ -438,7 +438,8 @@ int bd_rope_table(const double* inv_freq, int n, int D, float* table, hipStream_
  *   is entered as -1 and gives its tokens no slot.  free_head: int32 [1].
  * S >= 1: slots and positions are [B, S], row b those of the (up to S) new
  *   tokens of sequence b; total is ignored.  S = 0: they are [total], the new
- *   tokens of all sequences in order; new_lens must sum to at most total.
+ *   tokens of all sequences in order; new_lens should sum to at most total (tokens
+ *   past it get no slot, but count in lens and cu, and their pages are taken and entered).
  * Results (int32): lens [B], cache_lens[b] + new_lens[b], at most the room; cu
  *   [B + 1], the sums of the new lengths before each sequence; slots, the row
  *   page * page_size + position mod page_size of each new token, -1 for rows that hold none and
@@ -447,7 +448,7 @@ int bd_rope_table(const double* inv_freq, int n, int D, float* table, hipStream_
  *   the number of new tokens without a slot, 0 if all is well: those past the
  *   room, in the pages that the free list could not give or for which it held an id
  *   outside the pool (both entered as -1), behind cached tokens whose last page is
- *   none, or past total.
+ *   none, or past total (each counted once).
  * B from 1 to 2^16, max_pages >= 1, max_pages * page_size <= 2^30, page_size a
  * power of two from 16 to 2^15, num_pages * page_size <= 2^31 - 1, B * S and total at most 2^30.
  * All arrays are on the device, 4-byte aligned; outputs must not overlap

@@ -57,7 +57,7 @@ def paged_plan(lens, new, table, free, head, num_pages, P, S=0, total=0):
             t = b * S + i if S else at + i
             page = table[b, (n + i) // P] if n + i < cap else -1
             ok = 0 <= page < num_pages
-            lost += not ok
+            lost += not (ok and t < count)
             if t < count:
                 positions[t] = n + i
                 slots[t] = page * P + (n + i) % P if ok else -1

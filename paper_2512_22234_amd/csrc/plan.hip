@@ -46,6 +46,11 @@ __device__ inline int plan_free(const PlanArgs& a, long long at) {
   const int id = a.free_pages[at];
   return id >= 0 && id < a.num_pages ? id : -1;
 }
+// New tokens of a sequence that have a row in the results; t: tokens before it.
+__device__ inline int plan_seen(const PlanArgs& a, const PlanSeq& q, long long t) {
+  if (a.S > 0 || t + q.fresh <= a.T) return q.fresh;
+  return t < a.T ? (int)(a.T - t) : 0;
+}
 // The last thread whose sequences start at or before token (or page) x, by the sums before each thread.
 __device__ inline int plan_find(const long long* before, long long x) {
   int c = 0;
@@ -102,20 +107,24 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
   // The first workgroup: the new head of the free list, and the tokens that have no page.
   const int workers = (int)gridDim.x - 1, worker = (int)blockIdx.x - 1;
   if (worker < 0) {
+    // (packed tokens past T are lost once, wherever else they would be)
     long long lost = 0;
-    long long first = need0[tid];
+    long long first = need0[tid], t = tok0[tid];
     for (int b = c0; b < c1; ++b) {
       const PlanSeq q = plan_seq(a, b);
-      lost += q.fresh - (q.end - q.len);
+      const int seen = plan_seen(a, q, t);
+      const int end = q.len + imin(seen, cap - q.len);  // of the tokens below T
+      lost += q.fresh - (end - q.len);
       const long long left = a.n_free - head - first;  // entries of the free list for this sequence
       const int given = left <= 0 ? 0 : (int)(left < q.need ? left : q.need);
-      if (given < q.need) lost += q.end - imax(q.len, (q.p0 + given) << a.log_size);
+      if (given < q.need) lost += imax(end - imax(q.len, (q.p0 + given) << a.log_size), 0);
       // tokens behind the cached ones in a page that is none
-      const int tail = imin(q.end, q.p0 << a.log_size) - q.len;
+      const int tail = imin(end, q.p0 << a.log_size) - q.len;
       if (tail > 0) {
         const int id = a.table[b * a.table_stride + (q.len >> a.log_size)];
         if (id < 0 || id >= a.num_pages) lost += tail;
       }
+      t += q.fresh;
       first += q.need;
     }
     // tokens in pages whose entry of the list is no page: every entry taken is looked at, eight loads at a time; a
@@ -132,14 +141,15 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
         const long long u = u0 + e * PLAN_NT;
         const int c = plan_find(need0, u);
         int b = c * cpt;
-        long long at = u - need0[c];  // page among those of the sequences of thread c
+        long long at = u - need0[c], t = tok0[c];  // page, and token, among those of the sequences of thread c
         PlanSeq q = plan_seq(a, b);
         while (at >= q.need) {  // (ends: thread c's sequences need need0[c + 1] - need0[c] > u - need0[c] pages)
           at -= q.need;
+          t += q.fresh;
           q = plan_seq(a, ++b);
         }
-        const int begin = (q.p0 + (int)at) << a.log_size;
-        lost += imin(q.end - begin, P);
+        const int begin = (q.p0 + (int)at) << a.log_size, end = q.len + imin(plan_seen(a, q, t), cap - q.len);
+        lost += imax(imin(end - begin, P), 0);
       }
     }
 #pragma unroll
@@ -149,7 +159,6 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
     if (tid == 0) {
       long long sum = 0;
       for (int v = 0; v < PLAN_NT / 64; ++v) sum += wtok[v];
-      if (a.S == 0 && total > a.T) sum += total - a.T;
       const long long used = head + pages;
       a.state[0] = (int)(used < a.n_free ? used : a.n_free);
       a.state[1] = (int)(sum < INT32_MAX ? sum : INT32_MAX);
@@ -216,6 +225,25 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
     }
     a.slots[t] = slot;
     a.positions[t] = position;
+  }
+
+  // Packed tokens past T: the pages that they begin are taken from the list like the others, and are entered too (a row
+  // may hold ids of an earlier sequence there).  A sequence at a time for each workgroup.
+  if (a.S == 0 && total > a.T) {
+    for (int b = worker; b < a.B; b += workers) {
+      const int c = b / cpt;
+      long long t = tok0[c], first = need0[c];
+      for (int u = c * cpt; u < b; ++u) {
+        const PlanSeq q = plan_seq(a, u);
+        t += q.fresh;
+        first += q.need;
+      }
+      const PlanSeq q = plan_seq(a, b);
+      // entered above: pages that begin with one of the tokens below T
+      const int seen = plan_seen(a, q, t), begun = (q.len + imin(seen, cap - q.len) + P - 1) >> a.log_size;
+      for (int j = imax(begun, q.p0) + tid; j < q.p0 + q.need; j += PLAN_NT)
+        a.table[b * a.table_stride + j] = plan_free(a, head + first + (j - q.p0));
+    }
   }
 }
 

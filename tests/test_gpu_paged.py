@@ -363,6 +363,20 @@ def test_plan_counts_the_tokens_of_ids_outside_the_pool(S):
         _plan_check(lens, new, table, free, 3, 900, 16, S, None if S else int(new.sum()) + 5)
 
 
+@pytest.mark.parametrize("B", [3, 40, 700])
+@pytest.mark.parametrize("share", [0.0, 0.01, 0.4, 0.97])
+def test_plan_enters_the_pages_of_tokens_past_total(B, share):
+    """Packed tokens that sum to more than total: those past it get no slot and are counted once,
+    and every page that is taken from the list is entered, over the stale ids of the table."""
+    for bad in (0.0, 0.3):
+        lens, new, table, free = _damaged(B, 16, 5, 900, B, bad)
+        new[:2] = [40, 90]
+        lens[:2] = [3, 0]
+        for total in (int(new.sum() * share), int(new[0]) + 37):
+            _plan_check(lens, new, table, free, 1, 900, 16, None, total)
+        _plan_check(lens, new, table, free, len(free) - 5, 900, 16, None, int(new.sum() * share))
+
+
 def test_plan_of_more_pages_than_an_int_counts():
     """40 sequences that would need 2^26 pages each: the list gives what it has, the head stays inside it."""
     i32 = dict(dtype=torch.int32, device=DEV)

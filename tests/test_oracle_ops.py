@@ -92,3 +92,12 @@ def test_paged_plan_places_every_token_once(S):
     assert all(len({owner[s] for s in owner if s // P == p}) <= 1 for p in range(pages))
     used = sorted(int(p) for p in table[table >= 0])
     assert used == sorted(int(p) for p in free[:head])
+
+
+def test_paged_plan_past_total_by_hand():
+    """12 of 10 + 64 packed tokens have a row: two of the second sequence; its four pages are taken and entered."""
+    table, lens, cu, slots, pos, state = oracle.paged_plan([0, 0], [10, 64], [[7, 7, 7, 7], [7, 7, 7, 7]], [3, 0, 9, 5, 1], 0, 6, 16,
+                                                           0, 12)
+    assert table.tolist() == [[3, 7, 7, 7], [0, -1, 5, 1]]          # (9 is no page)
+    assert lens.tolist() == [10, 64] and cu.tolist() == [0, 10, 74] and state.tolist() == [5, 62]
+    assert slots.tolist() == [*range(48, 58), 0, 1] and pos.tolist() == [*range(10), 0, 1]
