@@ -182,7 +182,7 @@ int64_t extent(const Dim* d, int k, int D) {
 }
 // Do no two of those rows share an element?  (Sufficient: sorted by stride, each
 // stride spans all that lies below it.)
-bool rows_apart(const Dim* dims, int k, int D) {
+bool rows_apart(const Dim* dims, int k, int64_t D) {
   Dim d[4];
   for (int i = 0; i < k; ++i) {
     int at = i;
@@ -215,16 +215,16 @@ bool make_rows(const void* p, const int64_t* st, int B, int N, int H, int D, siz
 bd::HeadRows head_rows(const int64_t* st) { return bd::HeadRows{st[0], st[1], st[2]}; }
 
 // Two outputs apart: their ranges do not meet, or they are interleaved token by
-// token (views of one fused array).
+// token (views of one fused array): a token's heads of one behind those of the
+// other, and the rows of both together apart.
 bool outputs_apart(const Rows& a, const Rows& b) {
   if (!overlap(a.range(), b.range())) return true;
   if ((uintptr_t)a.p > (uintptr_t)b.p) return outputs_apart(b, a);
   const int64_t off = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p) / (int64_t)a.esz;
-  const int64_t wa = (a.d[2].n - 1) * a.d[2].stride + a.D, wb = (b.d[2].n - 1) * b.d[2].stride + b.D;
-  if (off < wa) return false;
-  for (int i = 0; i < 2; ++i)  // the same outer strides, each past both
-    if (a.d[i].n > 1 && (a.d[i].stride != b.d[i].stride || a.d[i].stride < off + wb)) return false;
-  return true;
+  if (off < extent(a.d + 2, 1, a.D)) return false;
+  for (int i = 0; i < 2; ++i)
+    if (a.d[i].n > 1 && a.d[i].stride != b.d[i].stride) return false;
+  return rows_apart(a.d, 2, off + extent(b.d + 2, 1, b.D));
 }
 
 // log2 of a page size, or -1 if it is none.

@@ -294,3 +294,21 @@ def test_strides_past_any_memory_are_refused():
     assert _rope_paged(num=(1 << 24) + 1, sp=1 << 40) == 1
     assert _plan(B=(1 << 14) + 1, ts=1 << 48) == 1
     assert _paged(B=(1 << 14) + 1, ts=1 << 48, ws_bytes=1 << 40) == 1
+
+
+E = A + 11 * SZ  # the queries' gradient
+
+
+@pytest.mark.parametrize("kw", [
+    # one head of 64, the keys' gradient 64 behind the queries' in every token: two sequences a token and a half apart,
+    dict(gst=(192, 128, 64) * 3, dv=A + 15 * SZ),
+    # ... and less than a sequence's span apart, which puts (1, 0) of one on (0, 9) of the other
+    dict(N=10, gst=(9064, 1000, 64) * 3, dv=A + 15 * SZ),
+    dict(B=10, gst=(1000, 9064, 64) * 3, dv=A + 15 * SZ),
+    # the values' gradient, behind both
+    dict(gst=(256, 192, 64, 256, 192, 64, 256, 192, 64), dk=A + 15 * SZ, dv=E + 128),
+])
+def test_interleaved_gradients_that_meet_are_refused(kw):
+    a = dict(Hq=1, Hkv=1, dq=E, dk=E + 128, pos_stride=0)
+    a.update(kw)
+    assert _rope_bwd(**a) == 1
