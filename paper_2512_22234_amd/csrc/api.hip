@@ -214,17 +214,26 @@ bool make_rows(const void* p, const int64_t* st, int B, int N, int H, int D, siz
 }
 bd::HeadRows head_rows(const int64_t* st) { return bd::HeadRows{st[0], st[1], st[2]}; }
 
-// Two outputs apart: their ranges do not meet, or they are interleaved token by
-// token (views of one fused array): a token's heads of one behind those of the
-// other, and the rows of both together apart.
+// Two outputs, each with rows apart, apart from each other: their ranges do not
+// meet, or they are interleaved (views of one fused array, token by token or head by
+// head).  Dimensions that both have alike and whose stride passes the distance of
+// the two have to pass all of both that lies below; the others lie within one's part.
 bool outputs_apart(const Rows& a, const Rows& b) {
   if (!overlap(a.range(), b.range())) return true;
   if ((uintptr_t)a.p > (uintptr_t)b.p) return outputs_apart(b, a);
   const int64_t off = (int64_t)((uintptr_t)b.p - (uintptr_t)a.p) / (int64_t)a.esz;
-  if (off < extent(a.d + 2, 1, a.D)) return false;
-  for (int i = 0; i < 2; ++i)
-    if (a.d[i].n > 1 && a.d[i].stride != b.d[i].stride) return false;
-  return rows_apart(a.d, 2, off + extent(b.d + 2, 1, b.D));
+  Dim outer[3];
+  int k = 0;
+  int64_t wa = a.D, wb = b.D;
+  for (int i = 0; i < 3; ++i) {
+    if (a.d[i].n == b.d[i].n && a.d[i].stride == b.d[i].stride && a.d[i].stride > off) {
+      outer[k++] = a.d[i];
+    } else {
+      wa += (a.d[i].n - 1) * a.d[i].stride;
+      wb += (b.d[i].n - 1) * b.d[i].stride;
+    }
+  }
+  return off >= wa && rows_apart(outer, k, off + wb);
 }
 
 // log2 of a page size, or -1 if it is none.

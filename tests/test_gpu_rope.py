@@ -141,6 +141,33 @@ def test_layouts_give_the_same():
     assert (fused[..., -64:] == 7.0).all()      # nothing past a token's heads
 
 
+@pytest.mark.parametrize("order", ["head by head", "keys and values", "by sequence", "tokens inside", "heads inside"])
+def test_gradients_into_interleaved_arrays(order):
+    """The three gradients as views of one array that holds them head by head, sequence by
+    sequence, or with tokens or heads innermost: bitwise those of separate arrays."""
+    B, N, H, D = 2, 70, 3, 64
+    c = _case(B, N, H, H, D, BF, F32, seed=21)
+    q, k, v = _parts(c, H, H, D)
+    args = (c["dq"], c["dk"], c["dv"], q, k, c["wq"], c["wk"], c["rope"], c["pos"], 1e-6)
+
+    def fused(*shape):
+        return torch.full(shape, 7.0, dtype=BF, device=DEV)
+
+    if order == "head by head":
+        views = fused(B, N, H, 3, D).unbind(3)
+    elif order == "keys and values":
+        views = (fused(B, N, H, D), *fused(B, N, H, 2, D).unbind(3))
+    elif order == "by sequence":
+        views = fused(B, 3, N, H, D).unbind(1)
+    elif order == "tokens inside":
+        views = [t.transpose(1, 2) for t in fused(B, H, 3, N, D).unbind(2)]
+    else:
+        views = [t.transpose(0, 1) for t in fused(N, 3, B, H, D).unbind(1)]
+    want = bd.bd_qk_norm_rope_bwd(*args)
+    got = bd.bd_qk_norm_rope_bwd(*args, *views)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 @pytest.mark.parametrize("N,dt", [(9000, BF), (17500, BF), (6000, F32)])
 def test_large_calls(N, dt):
     """Calls of more than 64 and 128 MiB (nontemporal loads, and stores), eight heads a
