@@ -16,6 +16,7 @@ import collections
 import contextlib
 import ctypes
 import functools
+import operator
 
 import numpy as np
 import torch
@@ -776,6 +777,7 @@ class QkvNormRopeFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, qkv, Hq, Hkv, q_weight, k_weight, rope, positions, eps):
         ctx.save_for_backward(qkv, q_weight, k_weight, rope, positions)
+        Hq, Hkv = operator.index(Hq), operator.index(Hkv)  # (only plain integers are looked up and kept)
         ctx.heads, ctx.eps = (Hq, Hkv), eps
         D = q_weight.numel()
         lay = _qkv_layout(qkv.shape, qkv.stride(), Hq, Hkv, D, positions.shape)

@@ -6,6 +6,7 @@ import ctypes
 import os
 import re
 
+import numpy as np
 import pytest
 import torch
 
@@ -312,3 +313,21 @@ def test_interleaved_gradients_that_meet_are_refused(kw):
     a = dict(Hq=1, Hkv=1, dq=E, dk=E + 128, pos_stride=0)
     a.update(kw)
     assert _rope_bwd(**a) == 1
+
+
+def _fused_call(Hq, Hkv, qkv=_t(2, 3, 8 * 64)):
+    bd.qkv_norm_rope(qkv, Hq, Hkv, _t(64), _t(64), _t(9, 64, dtype=torch.float32), _i(2, 3))
+
+
+def test_fused_heads_are_taken_at_their_present_value():
+    """A scalar that changed between two calls is checked again (the first call gets as far as the device)."""
+    for Hq, change in ((torch.tensor(6), lambda x: x.fill_(60)), (np.array(6), lambda x: x.fill(60))):
+        for _ in range(2):
+            with pytest.raises(Exception) as e:
+                _fused_call(Hq, 1)
+            assert "heads" not in str(e.value)
+        change(Hq)
+        with pytest.raises(ValueError, match="60/1 heads"):
+            _fused_call(Hq, 1)
+    with pytest.raises(TypeError):
+        _fused_call(6.0, 1)
