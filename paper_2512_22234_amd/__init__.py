@@ -578,6 +578,16 @@ def _launch_context(device: torch.device, stream):
 _HERE = contextlib.nullcontext()
 
 
+def _fit(*sizes) -> bool:
+    """Do these sizes reach the library, which takes them as C ints, as they are?"""
+    return max(sizes) < 1 << 31 and min(sizes) >= -1 << 31
+
+
+def _check_fit(*sizes):
+    if not _fit(*sizes):
+        raise ValueError(f"sizes of at most 32 bits expected, got {sizes}")
+
+
 def _row_strides(name, shape, strides):
     """Element strides (batch, token, head) of rows [.., N, H, D] of D contiguous values."""
     if strides[-1] != 1 and 0 not in shape:
@@ -611,6 +621,7 @@ def _rope_layout(q_shape, q_strides, k_shape, k_strides, v_shape, v_strides, pos
         strides += _row_strides(name, shape, st)
     if tuple(pos_shape) not in ((N,), lead + (N,)):
         raise ValueError(f"positions: expected shape {lead + (N,)} or {(N,)}, got {tuple(pos_shape)}")
+    _check_fit(*lead, N, Hq, Hkv, D)
     dense = [s for H in (Hq, Hkv, Hkv) for s in (N * H * D, H * D, D)]
     return _RopeLayout(lead[0] if lead else 1, N, Hq, Hkv, D, (ctypes.c_int64 * len(strides))(*strides),
                        N if len(pos_shape) == 2 else 0,
@@ -657,6 +668,7 @@ def bd_rope_table(n: int, D: int, theta: float = 1e6, inv_freq=None, device="cud
         device = out.device
     elif inv_freq is not None:
         device = inv_freq.device
+    _check_fit(n, D)
     device = torch.device(device)
     if device.type == "cuda" and device.index is None:
         device = torch.device("cuda", torch.cuda.current_device())
@@ -709,7 +721,7 @@ def _rope_fwd(lay, x, ptrs, args, eps, q_out=None, k_out=None, v_out=None, strea
 
 
 def bd_qk_norm_rope_workspace_bytes(B, N, Hq, Hkv, D, dtype=BD_ATTN_BF16) -> int:
-    return int(lib().bd_qk_norm_rope_workspace_bytes(B, N, Hq, Hkv, D, int(dtype)))
+    return int(lib().bd_qk_norm_rope_workspace_bytes(B, N, Hq, Hkv, D, int(dtype))) if _fit(B, N, Hq, Hkv, D) else 0
 
 
 def bd_qk_norm_rope_bwd(dq, dk, dv, q, k, q_weight, k_weight, rope, positions, eps: float = 1e-6, grad_q=None,
@@ -838,6 +850,7 @@ def _page_layout(k_shape, k_strides, v_shape, v_strides, Hkv, D):
             raise ValueError(f"{name}: expected shape {(n, Hkv, P, D)}, got {tuple(shape)}")
     if k_strides != v_strides or k_strides[3] != 1:
         raise ValueError("k_pages and v_pages: equal strides with the last dimension contiguous expected")
+    _check_fit(n, P)
     # (a dimension of one page or head has no stride of its own)
     st = tuple(s if m > 1 else 0 for m, s in zip(k_shape[:3], k_strides[:3]))
     if any(s % 8 for s in st):
@@ -862,6 +875,8 @@ def _table_stride(page_table, B, device):
     if page_table.dtype is not torch.int32:
         raise TypeError(f"page_table: expected {torch.int32}, got {page_table.dtype}")
     width, (rows, cols) = page_table.shape[1], page_table.stride()
+    if width >= 1 << 31:
+        _check_fit(width)
     if page_table.device != device or (cols != 1 and width > 1):
         raise ValueError(f"page_table: contiguous rows on {device} expected")
     return rows if B > 1 else width
@@ -915,6 +930,7 @@ def bd_paged_plan(cache_lens, new_lens, page_table, free_pages, free_head, num_p
     if S is not None and S < 1:
         raise ValueError(f"S: at least 1 expected, got {S}")
     S_, total_ = (0, int(total)) if S is None else (int(S), 0)
+    _check_fit(S_, total_, num_pages, page_size, free_pages.shape[0])
     shape = (B, S_) if S_ else (total_,)
     with _launch_context(dev, stream):
         lens = _result("lens", lens, cache_lens, (B,))
@@ -932,6 +948,8 @@ def bd_paged_plan(cache_lens, new_lens, page_table, free_pages, free_head, num_p
 
 
 def bd_attn_paged_decode_workspace_bytes(B, S, Hq, Hkv, D, page_size, max_pages, dtype=BD_ATTN_BF16) -> int:
+    if not _fit(B, S, Hq, Hkv, D, page_size, max_pages):
+        return 0
     return int(lib().bd_attn_paged_decode_workspace_bytes(B, S, Hq, Hkv, D, page_size, max_pages, int(dtype)))
 
 

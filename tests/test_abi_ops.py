@@ -331,3 +331,43 @@ def test_fused_heads_are_taken_at_their_present_value():
             _fused_call(Hq, 1)
     with pytest.raises(TypeError):
         _fused_call(6.0, 1)
+
+
+@pytest.mark.parametrize("change,kw", [
+    ({}, dict(S=4, page_size=(1 << 32) + 16)), ({}, dict(S=4, num_pages=(1 << 32) + 16)), ({}, dict(S=4, num_pages=16 - (1 << 32))),
+    ({}, dict(total=(1 << 32) + 8, slots=_i(1).expand((1 << 32) + 8))), ({}, dict(S=(1 << 32) + 4, slots=_i(1, 1).expand(2, (1 << 32) + 4))),
+    (dict(table=torch.empty((2, (1 << 32) + 4), dtype=torch.int32, device="meta")), dict(S=4)),
+    (dict(free=torch.empty((1 << 32) + 4, dtype=torch.int32, device="meta")), dict(S=4)),
+])
+def test_paged_plan_sizes_past_32_bits_are_refused(change, kw):
+    """They reach the library as C ints, where they would count as what is left of them."""
+    a = dict(old=_i(2), new=_i(2), table=_i(2, 4), free=_i(8), head=_i(1))
+    if change:
+        a = {n: t.to("meta") for n, t in a.items()}
+    a.update(change)
+    kw = dict(dict(num_pages=16, page_size=16), **kw)
+    with pytest.raises(ValueError, match="32 bits"):
+        bd.bd_paged_plan(*a.values(), **kw)
+
+
+def test_other_sizes_past_32_bits_are_refused():
+    big = 1 << 32
+    with pytest.raises(ValueError, match="32 bits"):
+        bd.bd_rope_table(big + 4, 64, device="cpu")
+    with pytest.raises(ValueError, match="32 bits"):
+        bd.bd_rope_table(4, big + 64, device="cpu")
+    pages = _t(1, 2, 16, 64).expand(big + 5, 2, 16, 64)
+    with pytest.raises(ValueError, match="32 bits"):
+        bd.bd_attn_paged_decode_fwd(_t(2, 4, 1, 64), pages, pages, _i(2, 3), _i(2))
+    q, pages, lens, table = (torch.empty(x, dtype=t, device="meta") for x, t in (
+        ((2, 4, 1, 64), torch.bfloat16), ((5, 2, 16, 64), torch.bfloat16), ((2,), torch.int32), ((2, big + 3), torch.int32)))
+    with pytest.raises(ValueError, match="32 bits"):
+        bd.bd_attn_paged_decode_fwd(q, pages, pages, table, lens)
+    for i in range(7):
+        sizes = [2, 1, 4, 2, 64, 16, 8]
+        sizes[i] += big
+        assert bd.bd_attn_paged_decode_workspace_bytes(*sizes) == 0
+    for i in range(5):
+        sizes = [1, 33, 3, 2, 128]
+        sizes[i] += big
+        assert bd.bd_qk_norm_rope_workspace_bytes(*sizes) == 0
