@@ -848,11 +848,11 @@ def _page_layout(k_shape, k_strides, v_shape, v_strides, Hkv, D):
     for name, shape in (("k_pages", k_shape), ("v_pages", v_shape)):
         if tuple(shape) != (n, Hkv, P, D):
             raise ValueError(f"{name}: expected shape {(n, Hkv, P, D)}, got {tuple(shape)}")
-    if k_strides != v_strides or k_strides[3] != 1:
+    # (a dimension of one page or head has no stride of its own)
+    st, sv = (tuple(s if m > 1 else 0 for m, s in zip(k_shape[:3], strides[:3])) for strides in (k_strides, v_strides))
+    if st != sv or k_strides[3] != 1 or v_strides[3] != 1:
         raise ValueError("k_pages and v_pages: equal strides with the last dimension contiguous expected")
     _check_fit(n, P)
-    # (a dimension of one page or head has no stride of its own)
-    st = tuple(s if m > 1 else 0 for m, s in zip(k_shape[:3], k_strides[:3]))
     if any(s % 8 for s in st):
         raise ValueError(f"k_pages: strides must be multiples of 8 elements, got {k_strides}")
     return (n, P) + st

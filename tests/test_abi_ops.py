@@ -371,3 +371,14 @@ def test_other_sizes_past_32_bits_are_refused():
         sizes = [1, 33, 3, 2, 128]
         sizes[i] += big
         assert bd.bd_qk_norm_rope_workspace_bytes(*sizes) == 0
+
+
+@pytest.mark.parametrize("k,v", [
+    (_t(1, 2, 16, 64), _t(1, 2, 2, 16, 64)[:, 0]),                          # one page
+    (_t(5, 1, 16, 64), _t(5, 16, 1, 64).permute(0, 2, 1, 3)),               # one head
+])
+def test_pages_alike_but_for_strides_without_a_step(k, v):
+    """A dimension of one has no stride of its own: such K and V pages lie alike (the call gets as far as the device)."""
+    with pytest.raises(Exception) as e:
+        bd.bd_attn_paged_decode_fwd(_t(2, 4, 1, 64), k, v, _i(2, 3), _i(2))
+    assert "strides" not in str(e.value)
