@@ -68,27 +68,34 @@ __device__ inline int paged_tiles(const PagedParams& p, int len) {
   return imax(tiles_of<KT>(len) + tiles_of<KT>(p.Sn), 1);
 }
 
-// Runs that T tiles are cut into.  Every run that holds part of an item leaves
-// partial results, for one wave up to 32 rows of D floats (as many bytes as a
-// tile of keys and values), which are written, read and merged, so a call is cut
-// no finer than its reading needs.  One wave: single tiles for up to 256 runs (one
-// a CU), then three tiles a run; where these come to two runs on most CUs, two on
-// all; three a CU from 24,576 tiles on, and at D = 64, with half the bytes a tile.
-// Measured, us (32/8 heads; * no more than one tile a run):
+// Runs that the T tiles of all items are cut into.  Every run that holds part of an
+// item leaves partial results, for one wave up to 32 rows of D floats (as many bytes
+// as a tile of keys and values), which are written, read and merged, so a call is cut
+// no finer than its reading needs.  One wave: single tiles for up to 256 runs (one a
+// CU), then three tiles a run; where these come to two runs on most CUs, two on all.
+// Items of at most eight tiles on average end a run's chain of copies so often that
+// three runs a CU are needed to fill the gaps; so are they at D = 64, with half the
+// bytes a tile.  Measured, us (32/8 heads; * no more than one tile a run):
 //                                               256   cdiv(T, 3)  512   768   1024 runs
 //   one sequence of 1500, S = 8 (384 tiles)     11.3     -        13.7* 13.6* 14.1*
 //   ... of 3000 (760)                           13.6    13.6      16.0  20.1  20.7*
 //   ... of 6000 (1512)                          16.5    17.9      16.8  18.4  20.0
 //   8 sequences of 3000, S = 8 (6080)           34.5     -        27.3  29.9  31.0
-//   64 of 512 to 8192, S = 1 (25,000)             -      -       143.4 138.2 140.5
 //   D = 64: 2 of 3000, S = 4 (1520)               -     12.8       -    13.5    -
-//   D = 64: 64 of 512 to 8192, S = 1              -      -        84.8  70.7  75.6
+//   D = 64: 64 of 512 to 8192, S = 1 (50,072)     -      -        84.8  70.7  75.6
+// and by the tiles of an item, S = 1, 512 / 768 runs:
+//   tiles an item       2            4            8           16           32           64
+//    4,000 tiles   26.1  22.7   22.9  20.3   21.9  20.7   22.0  21.5   21.1  21.9   22.6  21.9
+//   15,000         72.0  64.8   61.3  59.5   56.8  56.8   55.1  56.1   55.2  55.5   58.0  57.7
+//   30,000        132.6 109.2  107.3  96.7   91.7  91.1   84.8  87.9   83.2  86.9   84.8  86.7
+//   60,000        254.3 211.0  204.3 184.9  175.8 174.5  162.3 166.2  159.2 164.2  157.7 162.3
+// (64 sequences of 512 to 8192, 98 tiles an item: heads outermost 137.8 and 138.5, tokens 133.4 and 139.8).
 // Teams take two tiles at least (dec_runs).
 template <int D, int TW>
-__device__ inline int paged_runs(int T) {
+__device__ inline int paged_runs(int T, int items) {
   if (TW > 1) return dec_runs<TW>(DEC_WAVES / TW, T);
   const int three = imax(256, cdiv(T, 3));
-  return imin(T, D == 64 ? imin(three, 768) : T < 1152 ? three : T < 24576 ? 512 : 768);
+  return imin(T, D == 64 ? imin(three, 768) : T < 1152 ? three : T >> 3 <= items ? 768 : 512);
 }
 // First tile of run gw <= n (the runs cut T tiles into n near-equal pieces).
 __device__ inline int paged_run_start(int gw, int n, int T) {
@@ -154,7 +161,7 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
   const int excl = before + incl - csum;  // tiles per item of the sequences before c0
   total = __builtin_amdgcn_readfirstlane(total);
   const int T = total * I;  // checked on the host to fit in 31 bits
-  const int n = paged_runs<D, TW>(T);
+  const int n = paged_runs<D, TW>(T, p.d.B * I);
   const bool stream = total * p.d.Hkv > (int)(DEC_STREAM_BYTES / (2 * Smem::TILE));
   auto run_of = [&](int v) { return v * (int)gridDim.x + (int)blockIdx.x; };  // run of a workgroup's team v
 #pragma unroll
