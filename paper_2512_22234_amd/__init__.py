@@ -72,6 +72,8 @@ def _stream_handle(device: torch.device, stream) -> int:
 def _workspace(nbytes: int, device: torch.device, workspace):
     """The caller's workspace or a new one, and its pointer and size (none for 0 bytes)."""
     if workspace is not None:
+        if workspace.device != device or not workspace.is_contiguous():
+            raise ValueError(f"workspace: a contiguous tensor on {device} expected, got one on {workspace.device}")
         return workspace, workspace.data_ptr(), workspace.numel()
     if nbytes == 0:
         return None, None, 0

@@ -382,3 +382,13 @@ def test_pages_alike_but_for_strides_without_a_step(k, v):
     with pytest.raises(Exception) as e:
         bd.bd_attn_paged_decode_fwd(_t(2, 4, 1, 64), k, v, _i(2, 3), _i(2))
     assert "strides" not in str(e.value)
+
+
+@pytest.mark.parametrize("ws", [torch.empty(1 << 28, dtype=torch.uint8, device="meta"),
+                                torch.empty((1 << 28, 2), dtype=torch.uint8, device="meta")[:, 0]])
+def test_workspace_elsewhere_or_with_gaps_is_refused(ws):
+    dev = "cpu" if ws.is_contiguous() else "meta"
+    q, pages, lens, table = (torch.empty(x, dtype=t, device=dev) for x, t in (
+        ((2, 4, 1, 64), torch.bfloat16), ((5, 2, 16, 64), torch.bfloat16), ((2,), torch.int32), ((2, 3), torch.int32)))
+    with pytest.raises(ValueError, match="workspace"):
+        bd.bd_attn_paged_decode_fwd(q, pages, pages, table, lens, workspace=ws)
