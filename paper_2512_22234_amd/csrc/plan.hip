@@ -127,18 +127,21 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
       t += q.fresh;
       first += q.need;
     }
-    // tokens in pages whose entry of the list is no page: every entry taken is looked at, eight loads at a time; a
-    // sequence is sought for the bad ones alone
+    // tokens in pages whose entry of the list is no page: every entry taken is looked at, 32 loads at a time (four prompts
+    // of 62,500 tokens in pages of 16: PLACE us a call, eight at a time 8.2); a sequence is sought for the bad ones alone
     const long long pages = need0[PLAN_NT];
     const long long given = pages < a.n_free - head ? pages : a.n_free - head;
-    for (long long u0 = tid; u0 < given; u0 += 8 * PLAN_NT) {
-      int id[8];
+    for (long long u0 = tid; u0 < given; u0 += 32 * PLAN_NT) {
+      bool bad = false;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) id[e] = u0 + e * PLAN_NT < given ? a.free_pages[head + u0 + e * PLAN_NT] : 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (id[e] >= 0 && id[e] < a.num_pages) continue;
+      for (int e = 0; e < 32; ++e) {
         const long long u = u0 + e * PLAN_NT;
+        bad |= (unsigned)a.free_pages[head + (u < given ? u : given - 1)] >= (unsigned)a.num_pages;
+      }
+      if (!bad) continue;
+      const long long end_u = given < u0 + 32 * PLAN_NT ? given : u0 + 32 * PLAN_NT;
+      for (long long u = u0; u < end_u; u += PLAN_NT) {
+        if (plan_free(a, head + u) >= 0) continue;
         const int c = plan_find(need0, u);
         int b = c * cpt;
         long long at = u - need0[c], t = tok0[c];  // page, and token, among those of the sequences of thread c
