@@ -32,11 +32,11 @@
 // float32.
 //
 // Measured (32/8 heads of 128): 64 sequences of 512 to 8192 tokens (816 MB), one
-// token each, 136 to 144 us whatever the pages (16 to 128 rows; heads or tokens
-// outermost: the latter 3% slower), 5.7 to 6.0 TB/s; blocks of 4, 143 us (over a
-// dense cache 143); 24 sequences of 200 to 4096 (184 MB), blocks of 32, 69.5 us (dense,
-// with P in one part, 63): the partial results of 128 rows, 27 MB written and read
-// again, and one team of four waves a CU, which waits for each tile in turn.
+// token each, 133 to 143 us whatever the pages (16 to 128 rows; heads or tokens
+// outermost), 5.7 to 6.1 TB/s; blocks of 4, 139 to 141 us (over a dense cache 143);
+// 24 sequences of 200 to 4096 (184 MB), blocks of 32, 66 to 71 us (dense, with P in one
+// part, 63 to 66): 7 are the merge of 27 MB of partial results, and without any product the
+// call takes 56, one team of four waves a CU waiting for each tile in turn.
 #include "decode.hpp"
 
 namespace bd {

@@ -15,8 +15,10 @@
 // all lengths (8 bytes a sequence, from L2) and then takes a contiguous run of
 // tokens, the first one the state; a token finds its sequence by a search of the scan.
 // The token that starts a page writes the page's table entry, the others read the
-// same entry of the free list, so no workgroup waits for another.  The kernel takes 3.8 us for
-// 64 sequences of 4 tokens and 6.4 for 82,000 tokens of 700 sequences.
+// same entry of the free list, so no workgroup waits for another.  The kernel takes 3.7 us for
+// 64 sequences of 4 tokens and 6.1 for 82,000 tokens of 700 sequences; a call 30 to
+// 33 us for 8192 sequences and 300 to 390 for 65,536, whose lengths a thread walks
+// 256 at a time.
 #include "device.hpp"
 #include "kernels.hpp"
 
@@ -128,7 +130,7 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
       first += q.need;
     }
     // tokens in pages whose entry of the list is no page: every entry taken is looked at, 32 loads at a time (four prompts
-    // of 62,500 tokens in pages of 16: PLACE us a call, eight at a time 8.2); a sequence is sought for the bad ones alone
+    // of 62,500 tokens in pages of 16: 5.9 us a call, eight at a time 8.2); a sequence is sought for the bad ones alone
     const long long pages = need0[PLAN_NT];
     const long long given = pages < a.n_free - head ? pages : a.n_free - head;
     for (long long u0 = tid; u0 < given; u0 += 32 * PLAN_NT) {
@@ -254,7 +256,7 @@ __global__ __launch_bounds__(PLAN_NT) void plan_kernel(PlanArgs a) {
 
 hipError_t launch_plan(const PlanArgs& a, hipStream_t st) {
   // a workgroup for each 256 tokens (one a thread) and 256 sequences, and one for the state: 82,000 tokens of 700
-  // sequences 7.4 us a call, with 1024 tokens a workgroup 9.7
+  // sequences 5.9 us a call, with 1024 tokens a workgroup 8.5
   const int work = imax(a.T / PLAN_NT, a.B / PLAN_NT);
   hipLaunchKernelGGL(plan_kernel, dim3(imin(imax(work, 1), 2048) + 1), dim3(PLAN_NT), 0, st, a);
   return hipGetLastError();
