@@ -488,6 +488,105 @@ int bd_attn_paged_decode_fwd(const void* Q, const void* K_pages, const void* V_p
 size_t bd_attn_paged_decode_workspace_bytes(int B, int S, int Hq, int Hkv, int D, int page_size, int max_pages,
                                             int dtype);
 
+/*
+ * Decoding over a paged cache for sequences that share a prefix, as several
+ * samples of one prompt do: bd_attn_paged_decode_fwd where the queries of
+ * sequence b also see the prefix of its group, ahead of its own cached keys.
+ * The prefix's keys and values are read once for a group's sequences.
+ *
+ * group_sizes: int32 [groups].  Group g is the max(group_sizes[g], 0) sequences
+ *   behind those of the groups before it, as far as there are B; sequences behind
+ *   the last group have no prefix.
+ * prefix_table: [groups] rows of max_prefix_pages int32, prefix_stride elements
+ *   apart: the pages that hold the prefixes; prefix_lens: int32 [groups], their
+ *   keys (clamped to [0, max_prefix_pages * page_size]).
+ * page_table, cache_lens, K_new, V_new: the sequences' own keys, behind the
+ *   prefix, as for bd_attn_paged_decode_fwd (max_pages >= 1; cache_lens may be 0).
+ * A prefix takes whole pages of its own: the last one need not be full.  Pages
+ * may be shared freely, nothing is written to them.
+ * groups from 1 to 2^16, max_prefix_pages >= 1 and max_prefix_pages * page_size
+ * <= 2^22; all else as for bd_attn_paged_decode_fwd.
+ */
+int bd_attn_paged_shared_decode_fwd(const void* Q, const void* K_pages, const void* V_pages, const int32_t* group_sizes,
+                                    int groups, const int32_t* prefix_table, int max_prefix_pages,
+                                    int64_t prefix_stride, const int32_t* prefix_lens, const int32_t* page_table,
+                                    const int32_t* cache_lens, const void* K_new, const void* V_new, int B, int S,
+                                    int Hq, int Hkv, int D, int num_pages, int page_size, int max_pages,
+                                    int64_t table_stride, int64_t page_stride, int64_t head_stride, int64_t row_stride,
+                                    float scale, int dtype, void* O, float* LSE, void* ws, size_t ws_bytes,
+                                    hipStream_t stream);
+/* Workspace bytes for bd_attn_paged_shared_decode_fwd; 0 for arguments it would reject. */
+size_t bd_attn_paged_shared_decode_workspace_bytes(int B, int groups, int S, int Hq, int Hkv, int D, int page_size,
+                                                   int max_prefix_pages, int max_pages, int dtype);
+
+/*
+ * Summaries of pages, from which bd_paged_select tells which of them a query may
+ * attend to: for every page g of the pool and KV head h
+ *   summaries[g][h][0][d] = min over the page's keys of k_d,
+ *   summaries[g][h][1][d] = max over the page's keys of k_d.
+ * For each sequence those of the pages that hold positions from_lens[b] up to
+ * cache_lens[b] (both clamped, to [0, max_pages * page_size] and to at most
+ * cache_lens[b]) are written, each over the page's positions below
+ * cache_lens[b]; the other summaries are left as they are.  So with from_lens
+ * the lengths before some tokens were added and cache_lens those after, the
+ * summaries follow the cache.  A table entry outside [0, num_pages) is passed over.
+ *
+ * K_pages and page_table as for bd_attn_paged_decode_fwd (no bound on
+ * row_stride); summaries: bfloat16 [num_pages, Hkv, 2, D].  B * Hkv at most
+ * 2^22, max_pages * page_size at most 2^30.  Keys must be finite.  A page that
+ * two sequences hold is written by both; it should be full, or hold as many keys for both.
+ */
+int bd_paged_summarize(const void* K_pages, const int32_t* page_table, const int32_t* from_lens,
+                       const int32_t* cache_lens, int B, int Hkv, int D, int num_pages, int page_size, int max_pages,
+                       int64_t table_stride, int64_t page_stride, int64_t head_stride, int64_t row_stride, int dtype,
+                       void* summaries, hipStream_t stream);
+
+/*
+ * The pages that the queries of each sequence and KV head should attend to.  A
+ * page's score is the sum over the G * S query rows q of the KV head of
+ *   sum_d max(q_d lo_d, q_d hi_d),
+ * (lo, hi) being the page's summary: an upper bound of q . k over its keys.  Of
+ * the ceil(cache_lens[b] / page_size) pages of sequence b (those outside
+ * [0, num_pages) left out) the `first` first and `last` last by position are
+ * chosen, then those with the highest scores, the earlier of equal ones, up to
+ * `budget` in all.  Scores are formed in float64.
+ *
+ * Results, as bd_attn_paged_sparse_decode_fwd takes them: lists, int32
+ *   [B, Hkv, budget], the chosen pages in the order of their positions, -1 behind
+ *   them; list_lens, int32 [B, Hkv], the keys in them (whole pages but for the
+ *   sequence's last one).
+ * Q bfloat16 [B, Hq, S, D]; page_table, cache_lens as for
+ * bd_attn_paged_decode_fwd; budget >= 1 and budget * page_size at most 2^22,
+ * first, last >= 0 and first + last <= budget; B * Hkv * max_pages at most 2^30.
+ * Queries and the summaries of the sequences' pages must be finite.
+ * ws/ws_bytes: at least bd_paged_select_workspace_bytes bytes (16-byte aligned).
+ */
+int bd_paged_select(const void* Q, const void* summaries, const int32_t* page_table, const int32_t* cache_lens, int B,
+                    int S, int Hq, int Hkv, int D, int num_pages, int page_size, int max_pages, int64_t table_stride,
+                    int budget, int first, int last, int dtype, int32_t* lists, int32_t* list_lens, void* ws,
+                    size_t ws_bytes, hipStream_t stream);
+/* Workspace bytes for bd_paged_select; 0 for arguments it would reject. */
+size_t bd_paged_select_workspace_bytes(int B, int S, int Hq, int Hkv, int D, int page_size, int max_pages, int budget,
+                                       int dtype);
+
+/*
+ * Decoding over a paged cache with a list of pages for each KV head:
+ * bd_attn_paged_decode_fwd where the query rows of KV head h of sequence b see
+ * the first list_lens[b * Hkv + h] keys (clamped to [0, max_pages * page_size])
+ * of the pages lists[(b * Hkv + h) * max_pages + ...], and the block's own keys if
+ * K_new, V_new are given.  lists: int32 [B, Hkv, max_pages], in any order; an entry
+ * outside [0, num_pages) stands for a page without keys.  All else as for
+ * bd_attn_paged_decode_fwd.
+ */
+int bd_attn_paged_sparse_decode_fwd(const void* Q, const void* K_pages, const void* V_pages, const int32_t* lists,
+                                    const int32_t* list_lens, const void* K_new, const void* V_new, int B, int S,
+                                    int Hq, int Hkv, int D, int num_pages, int page_size, int max_pages,
+                                    int64_t page_stride, int64_t head_stride, int64_t row_stride, float scale,
+                                    int dtype, void* O, float* LSE, void* ws, size_t ws_bytes, hipStream_t stream);
+/* Workspace bytes for bd_attn_paged_sparse_decode_fwd; 0 for arguments it would reject. */
+size_t bd_attn_paged_sparse_decode_workspace_bytes(int B, int S, int Hq, int Hkv, int D, int page_size, int max_pages,
+                                                   int dtype);
+
 /* Comma-separated names of the kernels bd_attn_fwd (for_bwd = 0) or
  * bd_attn_bwd (for_bwd = 1) launch for `dtype`, in launch order (static). */
 const char* bd_attn_stage_names(int for_bwd, int dtype);

@@ -40,6 +40,9 @@ __all__ = [
     "bd_rope_table", "bd_qk_norm_rope_fwd", "bd_qk_norm_rope_bwd", "bd_qk_norm_rope_workspace_bytes",
     "QkNormRopeFunction", "QkvNormRopeFunction", "qk_norm_rope", "qkv_norm_rope", "bd_qk_norm_rope_paged",
     "bd_paged_plan", "PagedPlan", "bd_attn_paged_decode_fwd", "bd_attn_paged_decode_workspace_bytes",
+    "bd_attn_paged_shared_decode_fwd", "bd_attn_paged_shared_decode_workspace_bytes", "bd_paged_summarize",
+    "bd_paged_select", "bd_paged_select_workspace_bytes", "PagedLists", "bd_attn_paged_sparse_decode_fwd",
+    "bd_attn_paged_sparse_decode_workspace_bytes",
 ]
 
 
@@ -870,17 +873,17 @@ def _pages(k_pages, v_pages, Hkv, D, device):
     return lay
 
 
-def _table_stride(page_table, B, device):
+def _table_stride(page_table, B, device, name="page_table"):
     """Checks a page table [B, max_pages] (rows contiguous) and returns the distance of its rows."""
     if page_table.dim() != 2 or page_table.shape[0] != B:
-        raise ValueError(f"page_table: expected shape ({B}, max_pages), got {tuple(page_table.shape)}")
+        raise ValueError(f"{name}: expected shape ({B}, max_pages), got {tuple(page_table.shape)}")
     if page_table.dtype is not torch.int32:
-        raise TypeError(f"page_table: expected {torch.int32}, got {page_table.dtype}")
+        raise TypeError(f"{name}: expected {torch.int32}, got {page_table.dtype}")
     width, (rows, cols) = page_table.shape[1], page_table.stride()
     if width >= 1 << 31:
         _check_fit(width)
     if page_table.device != device or (cols != 1 and width > 1):
-        raise ValueError(f"page_table: contiguous rows on {device} expected")
+        raise ValueError(f"{name}: contiguous rows on {device} expected")
     return rows if B > 1 else width
 
 
@@ -955,6 +958,36 @@ def bd_attn_paged_decode_workspace_bytes(B, S, Hq, Hkv, D, page_size, max_pages,
     return int(lib().bd_attn_paged_decode_workspace_bytes(B, S, Hq, Hkv, D, page_size, max_pages, int(dtype)))
 
 
+def _paged_inputs(call, q, k_pages, v_pages, k_new, v_new):
+    """Checks the arrays that the decode calls over pages share: (B, Hq, S, Hkv, D, page arguments, addresses
+    of the block's keys and values)."""
+    if q.dim() != 4 or k_pages.dim() != 4:
+        raise ValueError("q [B,Hq,S,D] and k_pages/v_pages [pages,Hkv,page_size,D] expected")
+    B, Hq, S, D = shape = q.shape
+    Hkv, dev, bf16 = k_pages.shape[1], q.device, torch.bfloat16
+    if q.dtype is not bf16:
+        raise TypeError(f"{call} supports bfloat16 tensors, got {q.dtype}")
+    _check("q", q, shape, bf16, dev)
+    pages = _pages(k_pages, v_pages, Hkv, D, dev)
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new: both or neither expected")
+    kn = vn = None
+    if k_new is not None:
+        _check("k_new", k_new, (B, Hkv, S, D), bf16, dev)
+        _check("v_new", v_new, (B, Hkv, S, D), bf16, dev)
+        kn, vn = _ptr(k_new), _ptr(v_new)
+    return B, Hq, S, Hkv, D, pages, kn, vn
+
+
+def _paged_outputs(q, out, lse):
+    o = _result("out", out, q, q.shape)
+    shape = q.shape[:3]
+    if lse is None:
+        return o, torch.empty(shape, dtype=torch.float32, device=q.device)
+    _check("lse", lse, shape, torch.float32, q.device)
+    return o, lse
+
+
 def bd_attn_paged_decode_fwd(q, k_pages, v_pages, page_table, cache_lens, k_new=None, v_new=None, scale=None, out=None,
                              lse=None, workspace=None, stream=None):
     """bd_attn_decode_fwd over a paged cache; returns (O [B,Hq,S,D], LSE [B,Hq,S] float32).
@@ -964,31 +997,14 @@ def bd_attn_paged_decode_fwd(q, k_pages, v_pages, page_table, cache_lens, k_new=
     strided); cache_lens int32 [B], clamped to [0, max_pages * page_size];
     k_new, v_new [B,Hkv,S,D]: the block's own keys, or None where the queries
     see the cache alone.  Rows that see no key: O = 0, LSE = -inf."""
-    if q.dim() != 4 or k_pages.dim() != 4:
-        raise ValueError("q [B,Hq,S,D] and k_pages/v_pages [pages,Hkv,page_size,D] expected")
-    B, Hq, S, D = shape = q.shape
-    Hkv, dev, bf16 = k_pages.shape[1], q.device, torch.bfloat16
-    if q.dtype is not bf16:
-        raise TypeError(f"bd_attn_paged_decode_fwd supports bfloat16 tensors, got {q.dtype}")
-    _check("q", q, shape, bf16, dev)
-    n, P, sp, sh, sr = _pages(k_pages, v_pages, Hkv, D, dev)
+    B, Hq, S, Hkv, D, pages, kn, vn = _paged_inputs("bd_attn_paged_decode_fwd", q, k_pages, v_pages, k_new, v_new)
+    n, P, sp, sh, sr = pages
+    dev = q.device
     table_stride = _table_stride(page_table, B, dev)
     width = page_table.shape[1]
     _check("cache_lens", cache_lens, (B,), torch.int32, dev)
-    if (k_new is None) != (v_new is None):
-        raise ValueError("k_new and v_new: both or neither expected")
-    kn = vn = None
-    if k_new is not None:
-        _check("k_new", k_new, (B, Hkv, S, D), bf16, dev)
-        _check("v_new", v_new, (B, Hkv, S, D), bf16, dev)
-        kn, vn = _ptr(k_new), _ptr(v_new)
     with _launch_context(dev, stream):
-        o = _result("out", out, q, shape)
-        l_ = lse
-        if l_ is None:
-            l_ = torch.empty((B, Hq, S), dtype=torch.float32, device=dev)
-        else:
-            _check("lse", l_, (B, Hq, S), torch.float32, dev)
+        o, l_ = _paged_outputs(q, out, lse)
         nbytes = _known_size("bd_attn_paged_decode_workspace_bytes", B, S, Hq, Hkv, D, P, width, BD_ATTN_BF16)
         ws, wp, wn = _workspace(nbytes, dev, workspace)
         st = lib().bd_attn_paged_decode_fwd(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(cache_lens), kn,
@@ -996,4 +1012,153 @@ def bd_attn_paged_decode_fwd(q, k_pages, v_pages, page_table, cache_lens, k_new=
                                             BD_ATTN_BF16, _ptr(o), _ptr(l_), wp, wn, _stream_handle(dev, stream))
     if st:
         raise BdAttnError(st, "bd_attn_paged_decode_fwd")
+    return o, l_
+
+
+def bd_attn_paged_shared_decode_workspace_bytes(B, groups, S, Hq, Hkv, D, page_size, max_prefix_pages, max_pages,
+                                                dtype=BD_ATTN_BF16) -> int:
+    if not _fit(B, groups, S, Hq, Hkv, D, page_size, max_prefix_pages, max_pages):
+        return 0
+    return int(lib().bd_attn_paged_shared_decode_workspace_bytes(B, groups, S, Hq, Hkv, D, page_size, max_prefix_pages,
+                                                                 max_pages, int(dtype)))
+
+
+def bd_attn_paged_shared_decode_fwd(q, k_pages, v_pages, group_sizes, prefix_table, prefix_lens, page_table, cache_lens,
+                                    k_new=None, v_new=None, scale=None, out=None, lse=None, workspace=None, stream=None):
+    """bd_attn_paged_decode_fwd for consecutive sequences that share a prefix, read once for the group.
+
+    group_sizes int32 [groups]: sequences of each group, in order (sequences
+    behind the last group have no prefix); prefix_table int32 [groups,
+    max_prefix_pages] (rows may be strided) and prefix_lens int32 [groups]: the
+    pages and keys of the prefixes; page_table, cache_lens and all else: the
+    sequences' own keys, behind the prefix, as for bd_attn_paged_decode_fwd."""
+    B, Hq, S, Hkv, D, pages, kn, vn = _paged_inputs("bd_attn_paged_shared_decode_fwd", q, k_pages, v_pages, k_new, v_new)
+    n, P, sp, sh, sr = pages
+    dev = q.device
+    if group_sizes.dim() != 1:
+        raise ValueError("group_sizes: 1-D expected")
+    groups = group_sizes.shape[0]
+    _check_fit(groups)
+    _check("group_sizes", group_sizes, (groups,), torch.int32, dev)
+    prefix_stride = _table_stride(prefix_table, groups, dev, "prefix_table")
+    _check("prefix_lens", prefix_lens, (groups,), torch.int32, dev)
+    table_stride = _table_stride(page_table, B, dev)
+    prefix_width, width = prefix_table.shape[1], page_table.shape[1]
+    _check("cache_lens", cache_lens, (B,), torch.int32, dev)
+    with _launch_context(dev, stream):
+        o, l_ = _paged_outputs(q, out, lse)
+        nbytes = _known_size("bd_attn_paged_shared_decode_workspace_bytes", B, groups, S, Hq, Hkv, D, P, prefix_width, width,
+                             BD_ATTN_BF16)
+        ws, wp, wn = _workspace(nbytes, dev, workspace)
+        st = lib().bd_attn_paged_shared_decode_fwd(
+            _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(group_sizes), groups, _ptr(prefix_table), prefix_width,
+            prefix_stride, _ptr(prefix_lens), _ptr(page_table), _ptr(cache_lens), kn, vn, B, S, Hq, Hkv, D, n, P, width,
+            table_stride, sp, sh, sr, _scale_arg(scale), BD_ATTN_BF16, _ptr(o), _ptr(l_), wp, wn,
+            _stream_handle(dev, stream))
+    if st:
+        raise BdAttnError(st, "bd_attn_paged_shared_decode_fwd")
+    return o, l_
+
+
+# ---------------------------------------------------------------------------
+# Attention over chosen pages: summaries [pages, Hkv, 2, D] bfloat16 (smallest and
+# largest keys of each page), lists of pages for each sequence and KV head.
+
+def bd_paged_summarize(k_pages, page_table, from_lens, cache_lens, summaries, stream=None):
+    """Updates the summaries of the pages that hold positions from_lens[b] up to cache_lens[b] (int32 [B]).
+
+    k_pages [pages,Hkv,page_size,D] (any strides as for the other paged calls),
+    page_table int32 [B,max_pages]; summaries [pages,Hkv,2,D] bfloat16, updated
+    in place (the other pages' are left as they are) and returned."""
+    if k_pages.dim() != 4:
+        raise ValueError("k_pages [pages,Hkv,page_size,D] expected")
+    Hkv, D, dev = k_pages.shape[1], k_pages.shape[3], k_pages.device
+    n, P, sp, sh, sr = _pages(k_pages, k_pages, Hkv, D, dev)
+    _check_fit(Hkv, D)
+    B = cache_lens.numel()
+    _check("from_lens", from_lens, (B,), torch.int32, dev)
+    _check("cache_lens", cache_lens, (B,), torch.int32, dev)
+    table_stride = _table_stride(page_table, B, dev)
+    _check("summaries", summaries, (n, Hkv, 2, D), torch.bfloat16, dev)
+    with _launch_context(dev, stream):
+        st = lib().bd_paged_summarize(_ptr(k_pages), _ptr(page_table), _ptr(from_lens), _ptr(cache_lens), B, Hkv, D, n, P,
+                                      page_table.shape[1], table_stride, sp, sh, sr, BD_ATTN_BF16, _ptr(summaries),
+                                      _stream_handle(dev, stream))
+    if st:
+        raise BdAttnError(st, "bd_paged_summarize")
+    return summaries
+
+
+PagedLists = collections.namedtuple("PagedLists", "lists lens")
+
+
+def bd_paged_select_workspace_bytes(B, S, Hq, Hkv, D, page_size, max_pages, budget, dtype=BD_ATTN_BF16) -> int:
+    if not _fit(B, S, Hq, Hkv, D, page_size, max_pages, budget):
+        return 0
+    return int(lib().bd_paged_select_workspace_bytes(B, S, Hq, Hkv, D, page_size, max_pages, budget, int(dtype)))
+
+
+def bd_paged_select(q, summaries, page_table, cache_lens, page_size: int, budget: int, first: int = 1, last: int = 1,
+                    lists=None, lens=None, workspace=None, stream=None):
+    """The pages that the queries of each sequence and KV head should attend to: the `first` first and `last`
+    last of the sequence and those of the highest scores, `budget` in all (bounds of q . k by the summaries).
+
+    q [B,Hq,S,D]; summaries [pages,Hkv,2,D] (bd_paged_summarize); page_table
+    int32 [B,max_pages], cache_lens int32 [B].  Returns PagedLists(lists
+    [B,Hkv,budget] in the order of positions, -1 behind them; lens [B,Hkv], the
+    keys in them) for bd_attn_paged_sparse_decode_fwd."""
+    if q.dim() != 4 or summaries.dim() != 4:
+        raise ValueError("q [B,Hq,S,D] and summaries [pages,Hkv,2,D] expected")
+    B, Hq, S, D = q.shape
+    n, Hkv, dev, bf16 = summaries.shape[0], summaries.shape[1], q.device, torch.bfloat16
+    _check("q", q, (B, Hq, S, D), bf16, dev)
+    _check("summaries", summaries, (n, Hkv, 2, D), bf16, dev)
+    page_size, budget, first, last = (operator.index(x) for x in (page_size, budget, first, last))
+    table_stride = _table_stride(page_table, B, dev)
+    width = page_table.shape[1]
+    _check("cache_lens", cache_lens, (B,), torch.int32, dev)
+    _check_fit(B, Hq, S, D, n, page_size, budget, first, last)
+    if budget < 1:
+        raise ValueError(f"budget: at least 1 expected, got {budget}")
+    with _launch_context(dev, stream):
+        lists = _result("lists", lists, cache_lens, (B, Hkv, budget))
+        lens = _result("lens", lens, cache_lens, (B, Hkv))
+        nbytes = _known_size("bd_paged_select_workspace_bytes", B, S, Hq, Hkv, D, page_size, width, budget, BD_ATTN_BF16)
+        ws, wp, wn = _workspace(nbytes, dev, workspace)
+        st = lib().bd_paged_select(_ptr(q), _ptr(summaries), _ptr(page_table), _ptr(cache_lens), B, S, Hq, Hkv, D, n,
+                                   page_size, width, table_stride, budget, first, last, BD_ATTN_BF16, _ptr(lists), _ptr(lens),
+                                   wp, wn, _stream_handle(dev, stream))
+    if st:
+        raise BdAttnError(st, "bd_paged_select")
+    return PagedLists(lists, lens)
+
+
+def bd_attn_paged_sparse_decode_workspace_bytes(B, S, Hq, Hkv, D, page_size, max_pages, dtype=BD_ATTN_BF16) -> int:
+    if not _fit(B, S, Hq, Hkv, D, page_size, max_pages):
+        return 0
+    return int(lib().bd_attn_paged_sparse_decode_workspace_bytes(B, S, Hq, Hkv, D, page_size, max_pages, int(dtype)))
+
+
+def bd_attn_paged_sparse_decode_fwd(q, k_pages, v_pages, lists, list_lens, k_new=None, v_new=None, scale=None, out=None,
+                                    lse=None, workspace=None, stream=None):
+    """bd_attn_paged_decode_fwd with pages of its own for each KV head: lists int32 [B,Hkv,max_pages]
+    (contiguous), of which the first list_lens int32 [B,Hkv] keys are seen (bd_paged_select)."""
+    B, Hq, S, Hkv, D, pages, kn, vn = _paged_inputs("bd_attn_paged_sparse_decode_fwd", q, k_pages, v_pages, k_new, v_new)
+    n, P, sp, sh, sr = pages
+    dev = q.device
+    if lists.dim() != 3:
+        raise ValueError("lists [B,Hkv,max_pages] expected")
+    width = lists.shape[2]
+    _check_fit(width)
+    _check("lists", lists, (B, Hkv, width), torch.int32, dev)
+    _check("list_lens", list_lens, (B, Hkv), torch.int32, dev)
+    with _launch_context(dev, stream):
+        o, l_ = _paged_outputs(q, out, lse)
+        nbytes = _known_size("bd_attn_paged_sparse_decode_workspace_bytes", B, S, Hq, Hkv, D, P, width, BD_ATTN_BF16)
+        ws, wp, wn = _workspace(nbytes, dev, workspace)
+        st = lib().bd_attn_paged_sparse_decode_fwd(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(lists), _ptr(list_lens), kn,
+                                                   vn, B, S, Hq, Hkv, D, n, P, width, sp, sh, sr, _scale_arg(scale),
+                                                   BD_ATTN_BF16, _ptr(o), _ptr(l_), wp, wn, _stream_handle(dev, stream))
+    if st:
+        raise BdAttnError(st, "bd_attn_paged_sparse_decode_fwd")
     return o, l_

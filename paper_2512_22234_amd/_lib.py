@@ -82,6 +82,21 @@ def lib() -> ctypes.CDLL:
     L.bd_attn_paged_decode_fwd.argtypes = [vp] * 7 + [ci] * 8 + [i64] * 4 + [cf, ci, vp, vp, vp, sz, vp]
     L.bd_attn_paged_decode_workspace_bytes.restype = sz
     L.bd_attn_paged_decode_workspace_bytes.argtypes = [ci] * 8
+    L.bd_attn_paged_shared_decode_fwd.restype = ci
+    L.bd_attn_paged_shared_decode_fwd.argtypes = ([vp] * 4 + [ci, vp, ci, i64] + [vp] * 5 + [ci] * 8 + [i64] * 4
+                                                  + [cf, ci, vp, vp, vp, sz, vp])
+    L.bd_attn_paged_shared_decode_workspace_bytes.restype = sz
+    L.bd_attn_paged_shared_decode_workspace_bytes.argtypes = [ci] * 10
+    L.bd_paged_summarize.restype = ci
+    L.bd_paged_summarize.argtypes = [vp] * 4 + [ci] * 6 + [i64] * 4 + [ci, vp, vp]
+    L.bd_paged_select.restype = ci
+    L.bd_paged_select.argtypes = [vp] * 4 + [ci] * 8 + [i64] + [ci] * 4 + [vp, vp, vp, sz, vp]
+    L.bd_paged_select_workspace_bytes.restype = sz
+    L.bd_paged_select_workspace_bytes.argtypes = [ci] * 9
+    L.bd_attn_paged_sparse_decode_fwd.restype = ci
+    L.bd_attn_paged_sparse_decode_fwd.argtypes = [vp] * 7 + [ci] * 8 + [i64] * 3 + [cf, ci, vp, vp, vp, sz, vp]
+    L.bd_attn_paged_sparse_decode_workspace_bytes.restype = sz
+    L.bd_attn_paged_sparse_decode_workspace_bytes.argtypes = [ci] * 8
     L.bd_attn_stage_names.restype = ctypes.c_char_p
     L.bd_attn_stage_names.argtypes = [ci, ci]
     L.bd_attn_workspace_bytes.restype = sz

@@ -317,6 +317,101 @@ int validate_paged(int B, int S, int Hq, int Hkv, int D, int page_size, int max_
   return validate_decode(B, S, Hq, Hkv, D, max_pages << lg, scale, dtype, s);
 }
 
+// A decode call over pages as its caller gives it.
+struct PagedCall {
+  const void *Q, *K_pages, *V_pages;
+  const int32_t *page_table, *cache_lens;
+  const void *K_new, *V_new;
+  int num_pages, page_size, max_pages;
+  int64_t table_stride, page_stride, head_stride, row_stride;
+  void* O;
+  float* LSE;
+  void* ws;
+  size_t ws_bytes;
+};
+// Checks the arrays of a decode call (s: its validated shape; rows: those of the page
+// table and of cache_lens; Hkv: heads of the pages; need: workspace bytes; more: other
+// inputs, 4-byte aligned) and fills the kernel's arguments.
+int paged_arrays(const PagedCall& c, const bd::DecodeShape& s, int rows, int Hkv, size_t need, const Range* more, int n_more,
+                 bd::PagedArgs& a) {
+  Range pages[2];
+  if (!make_pages(c.K_pages, c.V_pages, c.num_pages, c.page_size, c.page_stride, c.head_stride, c.row_stride, Hkv, s.D, false,
+                  a.pages, pages[0], pages[1]) ||
+      c.page_stride > INT32_MAX || c.row_stride < s.D || c.row_stride > (1 << 20) || c.row_stride * c.page_size > (1 << 30) ||
+      c.table_stride < 0 || (rows > 1 && c.table_stride != 0 && c.table_stride < c.max_pages))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  const Dim table{rows, c.table_stride};
+  const int64_t n_table = extent(&table, 1, c.max_pages);
+  if (n_table > kMaxExtent) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (!c.Q || !c.page_table || !c.cache_lens || !c.O || !c.LSE || !c.ws || (c.K_new == nullptr) != (c.V_new == nullptr))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (!aligned(c.Q, 16) || !aligned(c.page_table, 4) || !aligned(c.cache_lens, 4) || !aligned(c.K_new, 16) ||
+      !aligned(c.V_new, 16) || !aligned(c.O, 16) || !aligned(c.LSE, 4) || !aligned(c.ws, 16))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  for (int i = 0; i < n_more; ++i)
+    if (!more[i].p || !aligned(more[i].p, 4)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (c.ws_bytes < need) return BD_ATTN_ERR_WORKSPACE_TOO_SMALL;
+  const size_t nq = (size_t)s.B * s.Hq * s.S, nkn = c.K_new ? (size_t)s.B * s.Hkv * s.S * s.D * 2 : 0;
+  const Range in[] = {{c.Q, nq * s.D * 2}, pages[0], pages[1], {c.page_table, (size_t)n_table * 4},
+                      {c.cache_lens, (size_t)rows * 4}, {c.K_new, nkn}, {c.V_new, nkn}};
+  const Range out[] = {{c.O, nq * s.D * 2}, {c.LSE, nq * 4}, {c.ws, need}};
+  for (const Range& o : out) {
+    for (const Range& i : in)
+      if (i.p && overlap(o, i)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+    for (int i = 0; i < n_more; ++i)
+      if (overlap(o, more[i])) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  }
+  if (overlap(out[0], out[1]) || overlap(out[0], out[2]) || overlap(out[1], out[2]))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  a.Q = c.Q;
+  a.Kp = c.K_pages;
+  a.Vp = c.V_pages;
+  a.table = c.page_table;
+  a.width = c.max_pages;
+  a.table_stride = c.table_stride;
+  a.cache_lens = c.cache_lens;
+  a.Kn = c.K_new;
+  a.Vn = c.V_new;
+  a.O = c.O;
+  a.LSE = c.LSE;
+  return BD_ATTN_OK;
+}
+
+// Validation of a decode call whose sequences share prefixes; fills the resolved shape.
+int validate_shared(int B, int groups, int S, int Hq, int Hkv, int D, int page_size, int max_prefix_pages, int max_pages,
+                    float scale, int dtype, bd::DecodeShape& s) {
+  const int st = validate_paged(B, S, Hq, Hkv, D, page_size, max_pages, scale, dtype, s);
+  if (st != BD_ATTN_OK) return st;
+  const int lg = page_log(page_size);
+  if (groups < 1 || groups > (1 << 16) || max_prefix_pages < 1 || (int64_t)max_prefix_pages << lg > (1 << 22))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  // the tiles of the prefixes are counted in int32, as those of the sequences' own keys
+  if (bd::shared_items(s, groups) * (size_t)bd::cdiv(max_prefix_pages << lg, bd::DEC_KT) > (size_t)INT32_MAX / 2)
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  return BD_ATTN_OK;
+}
+// Validation of a decode call with a list of pages for each KV head; fills the shape
+// of its B * Hkv lists.
+int validate_sparse(int B, int S, int Hq, int Hkv, int D, int page_size, int max_pages, float scale, int dtype,
+                    bd::DecodeShape& s) {
+  const int st = validate_paged(B, S, Hq, Hkv, D, page_size, max_pages, scale, dtype, s);
+  if (st != BD_ATTN_OK) return st;
+  return validate_decode(B * Hkv, S, Hq / Hkv, 1, D, s.C, scale, dtype, s);
+}
+
+// Validation of a choice of pages.
+int validate_select(int B, int S, int Hq, int Hkv, int D, int page_size, int max_pages, int budget, int dtype) {
+  const int lg = page_log(page_size);
+  if (B < 1 || S < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || lg < 0 || max_pages < 1 || budget < 1 ||
+      (int64_t)max_pages << lg > (1 << 22) || (int64_t)budget << lg > (1 << 22))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  // (launches count their threads in 32 bits)
+  if ((int64_t)B * Hq > (1 << 26) / S || (int64_t)B * Hkv > (1 << 22) || (int64_t)B * Hkv * max_pages > (1 << 30))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if ((D != 64 && D != 128) || dtype != BD_ATTN_BF16) return BD_ATTN_ERR_UNSUPPORTED;
+  return BD_ATTN_OK;
+}
+
 #define BD_TRY(expr)                                    \
   do {                                                  \
     if ((expr) != hipSuccess) return BD_ATTN_ERR_HIP;   \
@@ -930,47 +1025,158 @@ int bd_attn_paged_decode_fwd(const void* Q, const void* K_pages, const void* V_p
                              int64_t page_stride, int64_t head_stride, int64_t row_stride, float scale, int dtype,
                              void* O, float* LSE, void* ws, size_t ws_bytes, hipStream_t stream) {
   bd::DecodeShape s;
-  const int st = validate_paged(B, S, Hq, Hkv, D, page_size, max_pages, scale, dtype, s);
+  int st = validate_paged(B, S, Hq, Hkv, D, page_size, max_pages, scale, dtype, s);
   if (st != BD_ATTN_OK) return st;
+  const PagedCall c{Q,           K_pages,    V_pages, page_table, cache_lens, K_new, V_new, num_pages, page_size, max_pages, table_stride,
+                    page_stride, head_stride, row_stride, O, LSE, ws, ws_bytes};
   bd::PagedArgs a{};
+  st = paged_arrays(c, s, s.B, Hkv, bd::decode_workspace_bytes(s), nullptr, 0, a);
+  if (st != BD_ATTN_OK) return st;
+  (void)hipGetLastError();
+  return bd::launch_paged_decode(s, a, ws, stream) == hipSuccess ? BD_ATTN_OK : BD_ATTN_ERR_HIP;
+}
+
+size_t bd_attn_paged_shared_decode_workspace_bytes(int B, int groups, int S, int Hq, int Hkv, int D, int page_size,
+                                                   int max_prefix_pages, int max_pages, int dtype) {
+  bd::DecodeShape s;
+  if (validate_shared(B, groups, S, Hq, Hkv, D, page_size, max_prefix_pages, max_pages, 0.f, dtype, s) != BD_ATTN_OK) return 0;
+  return bd::shared_workspace_bytes(s, groups);
+}
+
+int bd_attn_paged_shared_decode_fwd(const void* Q, const void* K_pages, const void* V_pages, const int32_t* group_sizes,
+                                    int groups, const int32_t* prefix_table, int max_prefix_pages,
+                                    int64_t prefix_stride, const int32_t* prefix_lens, const int32_t* page_table,
+                                    const int32_t* cache_lens, const void* K_new, const void* V_new, int B, int S,
+                                    int Hq, int Hkv, int D, int num_pages, int page_size, int max_pages,
+                                    int64_t table_stride, int64_t page_stride, int64_t head_stride, int64_t row_stride,
+                                    float scale, int dtype, void* O, float* LSE, void* ws, size_t ws_bytes,
+                                    hipStream_t stream) {
+  bd::DecodeShape s;
+  int st = validate_shared(B, groups, S, Hq, Hkv, D, page_size, max_prefix_pages, max_pages, scale, dtype, s);
+  if (st != BD_ATTN_OK) return st;
+  if (prefix_stride < 0 || (groups > 1 && prefix_stride != 0 && prefix_stride < max_prefix_pages))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  const Dim rows{groups, prefix_stride};
+  const int64_t n_table = extent(&rows, 1, max_prefix_pages);
+  if (n_table > kMaxExtent) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  const Range more[] = {{group_sizes, (size_t)groups * 4}, {prefix_table, (size_t)n_table * 4}, {prefix_lens, (size_t)groups * 4}};
+  const PagedCall c{Q,           K_pages,    V_pages, page_table, cache_lens, K_new, V_new, num_pages, page_size, max_pages, table_stride,
+                    page_stride, head_stride, row_stride, O, LSE, ws, ws_bytes};
+  bd::SharedArgs a{};
+  st = paged_arrays(c, s, s.B, Hkv, bd::shared_workspace_bytes(s, groups), more, 3, a.own);
+  if (st != BD_ATTN_OK) return st;
+  a.sizes = group_sizes;
+  a.groups = groups;
+  a.table = prefix_table;
+  a.width = max_prefix_pages;
+  a.table_stride = prefix_stride;
+  a.lens = prefix_lens;
+  (void)hipGetLastError();
+  return bd::launch_shared_decode(s, a, ws, stream) == hipSuccess ? BD_ATTN_OK : BD_ATTN_ERR_HIP;
+}
+
+int bd_paged_summarize(const void* K_pages, const int32_t* page_table, const int32_t* from_lens,
+                       const int32_t* cache_lens, int B, int Hkv, int D, int num_pages, int page_size, int max_pages,
+                       int64_t table_stride, int64_t page_stride, int64_t head_stride, int64_t row_stride, int dtype,
+                       void* summaries, hipStream_t stream) {
+  const int lg = page_log(page_size);
+  if (B < 1 || Hkv < 1 || lg < 0 || max_pages < 1 || (int64_t)max_pages << lg > (1 << 30) || (int64_t)B * Hkv > (1 << 22))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if ((D != 64 && D != 128) || dtype != BD_ATTN_BF16) return BD_ATTN_ERR_UNSUPPORTED;
+  bd::SummaryArgs a{};
   Range pages[2];
-  if (!make_pages(K_pages, V_pages, num_pages, page_size, page_stride, head_stride, row_stride, Hkv, D, false, a.pages,
-                  pages[0], pages[1]) ||
-      page_stride > INT32_MAX || row_stride < D || row_stride > (1 << 20) || row_stride * page_size > (1 << 30) ||
+  if (!make_pages(K_pages, K_pages, num_pages, page_size, page_stride, head_stride, row_stride, Hkv, D, false, a.pages, pages[0],
+                  pages[1]) ||
       table_stride < 0 || (B > 1 && table_stride != 0 && table_stride < max_pages))
     return BD_ATTN_ERR_INVALID_ARGUMENT;
   const Dim rows{B, table_stride};
   const int64_t n_table = extent(&rows, 1, max_pages);
-  if (n_table > kMaxExtent) return BD_ATTN_ERR_INVALID_ARGUMENT;
-  const size_t need = bd::decode_workspace_bytes(s);
-  if (!Q || !page_table || !cache_lens || !O || !LSE || !ws || (K_new == nullptr) != (V_new == nullptr))
-    return BD_ATTN_ERR_INVALID_ARGUMENT;
-  if (!aligned(Q, 16) || !aligned(page_table, 4) || !aligned(cache_lens, 4) || !aligned(K_new, 16) ||
-      !aligned(V_new, 16) || !aligned(O, 16) || !aligned(LSE, 4) || !aligned(ws, 16))
-    return BD_ATTN_ERR_INVALID_ARGUMENT;
-  if (ws_bytes < need) return BD_ATTN_ERR_WORKSPACE_TOO_SMALL;
-  const size_t nq = (size_t)B * Hq * S, nkn = K_new ? (size_t)B * Hkv * S * D * 2 : 0;
-  const Range in[] = {{Q, nq * D * 2}, pages[0], pages[1], {page_table, (size_t)n_table * 4},
-                      {cache_lens, (size_t)B * 4}, {K_new, nkn}, {V_new, nkn}};
-  const Range out[] = {{O, nq * D * 2}, {LSE, nq * 4}, {ws, need}};
-  for (const Range& o : out)
-    for (const Range& i : in)
-      if (i.p && overlap(o, i)) return BD_ATTN_ERR_INVALID_ARGUMENT;
-  if (overlap(out[0], out[1]) || overlap(out[0], out[2]) || overlap(out[1], out[2]))
-    return BD_ATTN_ERR_INVALID_ARGUMENT;
-  a.Q = Q;
-  a.Kp = K_pages;
-  a.Vp = V_pages;
+  const Dim sums[] = {{num_pages, (int64_t)Hkv * 2 * D}};
+  const int64_t n_sums = extent(sums, 1, Hkv * 2 * D);
+  if (n_table > kMaxExtent || n_sums > kMaxExtent) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  const Range out = {summaries, (size_t)n_sums * 2};
+  const Range in[] = {pages[0], {page_table, (size_t)n_table * 4}, {from_lens, (size_t)B * 4}, {cache_lens, (size_t)B * 4}};
+  if (!summaries || !aligned(summaries, 16)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  for (const Range& i : in)
+    if (!i.p || !aligned(i.p, 4) || overlap(out, i)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  a.K = static_cast<const __bf16*>(K_pages);
   a.table = page_table;
+  a.B = B;
+  a.Hkv = Hkv;
   a.width = max_pages;
   a.table_stride = table_stride;
-  a.cache_lens = cache_lens;
-  a.Kn = K_new;
-  a.Vn = V_new;
-  a.O = O;
-  a.LSE = LSE;
+  a.from = from_lens;
+  a.lens = cache_lens;
+  a.summaries = static_cast<__bf16*>(summaries);
   (void)hipGetLastError();
-  return bd::launch_paged_decode(s, a, ws, stream) == hipSuccess ? BD_ATTN_OK : BD_ATTN_ERR_HIP;
+  return bd::launch_summarize(a, D, stream) == hipSuccess ? BD_ATTN_OK : BD_ATTN_ERR_HIP;
+}
+
+size_t bd_paged_select_workspace_bytes(int B, int S, int Hq, int Hkv, int D, int page_size, int max_pages, int budget,
+                                       int dtype) {
+  if (validate_select(B, S, Hq, Hkv, D, page_size, max_pages, budget, dtype) != BD_ATTN_OK) return 0;
+  return bd::select_workspace_bytes(B, Hkv, max_pages);
+}
+
+int bd_paged_select(const void* Q, const void* summaries, const int32_t* page_table, const int32_t* cache_lens, int B,
+                    int S, int Hq, int Hkv, int D, int num_pages, int page_size, int max_pages, int64_t table_stride,
+                    int budget, int first, int last, int dtype, int32_t* lists, int32_t* list_lens, void* ws,
+                    size_t ws_bytes, hipStream_t stream) {
+  const int st = validate_select(B, S, Hq, Hkv, D, page_size, max_pages, budget, dtype);
+  if (st != BD_ATTN_OK) return st;
+  const int lg = page_log(page_size);
+  if (num_pages < 1 || (int64_t)num_pages << lg > INT32_MAX || first < 0 || last < 0 || (int64_t)first + last > budget ||
+      table_stride < 0 || (B > 1 && table_stride != 0 && table_stride < max_pages))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  const Dim rows{B, table_stride};
+  const int64_t n_table = extent(&rows, 1, max_pages);
+  const Dim sums[] = {{num_pages, (int64_t)Hkv * 2 * D}};
+  const int64_t n_sums = extent(sums, 1, Hkv * 2 * D);
+  if (n_table > kMaxExtent || n_sums > kMaxExtent) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  const size_t need = bd::select_workspace_bytes(B, Hkv, max_pages);
+  if (!Q || !summaries || !page_table || !cache_lens || !lists || !list_lens || !ws || !aligned(Q, 16) ||
+      !aligned(summaries, 16) || !aligned(page_table, 4) || !aligned(cache_lens, 4) || !aligned(lists, 4) ||
+      !aligned(list_lens, 4) || !aligned(ws, 16))
+    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  if (ws_bytes < need) return BD_ATTN_ERR_WORKSPACE_TOO_SMALL;
+  const Range in[] = {{Q, (size_t)B * Hq * S * D * 2}, {summaries, (size_t)n_sums * 2}, {page_table, (size_t)n_table * 4},
+                      {cache_lens, (size_t)B * 4}};
+  const Range out[] = {{lists, (size_t)B * Hkv * budget * 4}, {list_lens, (size_t)B * Hkv * 4}, {ws, need}};
+  for (int u = 0; u < 3; ++u) {
+    for (const Range& i : in)
+      if (overlap(out[u], i)) return BD_ATTN_ERR_INVALID_ARGUMENT;
+    for (int v = u + 1; v < 3; ++v)
+      if (overlap(out[u], out[v])) return BD_ATTN_ERR_INVALID_ARGUMENT;
+  }
+  const bd::SelectArgs a{static_cast<const __bf16*>(Q), static_cast<const __bf16*>(summaries), page_table, B, Hkv, Hq / Hkv * S,
+                         max_pages, table_stride, cache_lens, num_pages, lg, budget, first, last, lists, list_lens,
+                         static_cast<uint64_t*>(ws)};
+  (void)hipGetLastError();
+  return bd::launch_select(a, D, stream) == hipSuccess ? BD_ATTN_OK : BD_ATTN_ERR_HIP;
+}
+
+size_t bd_attn_paged_sparse_decode_workspace_bytes(int B, int S, int Hq, int Hkv, int D, int page_size, int max_pages,
+                                                   int dtype) {
+  bd::DecodeShape s;
+  if (validate_sparse(B, S, Hq, Hkv, D, page_size, max_pages, 0.f, dtype, s) != BD_ATTN_OK) return 0;
+  return bd::decode_workspace_bytes(s);
+}
+
+int bd_attn_paged_sparse_decode_fwd(const void* Q, const void* K_pages, const void* V_pages, const int32_t* lists,
+                                    const int32_t* list_lens, const void* K_new, const void* V_new, int B, int S,
+                                    int Hq, int Hkv, int D, int num_pages, int page_size, int max_pages,
+                                    int64_t page_stride, int64_t head_stride, int64_t row_stride, float scale,
+                                    int dtype, void* O, float* LSE, void* ws, size_t ws_bytes, hipStream_t stream) {
+  bd::DecodeShape s;
+  int st = validate_sparse(B, S, Hq, Hkv, D, page_size, max_pages, scale, dtype, s);
+  if (st != BD_ATTN_OK) return st;
+  const PagedCall c{Q,           K_pages,    V_pages, lists, list_lens, K_new, V_new, num_pages, page_size, max_pages, max_pages,
+                    page_stride, head_stride, row_stride, O, LSE, ws, ws_bytes};
+  bd::PagedArgs a{};
+  st = paged_arrays(c, s, s.B, Hkv, bd::decode_workspace_bytes(s), nullptr, 0, a);
+  if (st != BD_ATTN_OK) return st;
+  (void)hipGetLastError();
+  return bd::launch_sparse_decode(s, a, Hkv, ws, stream) == hipSuccess ? BD_ATTN_OK : BD_ATTN_ERR_HIP;
 }
 
 const char* bd_attn_stage_names(int for_bwd, int dtype) {

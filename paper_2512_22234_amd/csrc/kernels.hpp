@@ -355,4 +355,75 @@ struct PagedArgs {
 };
 hipError_t launch_paged_decode(const DecodeShape& s, const PagedArgs& a, void* ws, hipStream_t st);
 
+// The same with a list of pages for each KV head: DecodeShape of B * Hkv sequences
+// of G query heads and one KV head, row b * Hkv + h of the table holding pages of
+// KV head h of `heads`.
+hipError_t launch_sparse_decode(const DecodeShape& s, const PagedArgs& a, int heads, void* ws, hipStream_t st);
+
+// Decoding of sequences that share a prefix in groups of consecutive sequences:
+// PagedArgs for the sequences' own keys, and the prefixes' pages and lengths.
+struct SharedArgs {
+  PagedArgs own;
+  const int* sizes;  // [groups]
+  int groups;
+  const int* table;  // [groups][width], rows table_stride apart
+  int width;
+  int64_t table_stride;
+  const int* lens;  // [groups]
+};
+// The prefix's items: a KV head's G * S rows of all members, in row groups of 32
+// rows for each wave of a team; a team as large as the average group needs.
+inline int shared_waves(const DecodeShape& s, int groups) {
+  const long long rows = ((long long)s.B * (s.Hq / s.Hkv) * s.S + groups - 1) / groups;
+  return rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+}
+inline size_t shared_items(const DecodeShape& s, int groups) {
+  const size_t rows = (size_t)s.B * (s.Hq / s.Hkv) * s.S;
+  return (size_t)s.Hkv * (rows / (DEC_QT * shared_waves(s, groups)) + (groups < s.B ? groups : s.B));
+}
+// Workspace: the sequences' own (decode_workspace_bytes), then for the prefixes a
+// descriptor for each item and a reference for each sequence, and the partial
+// results of every (team, item) run.
+inline size_t shared_desc_bytes(const DecodeShape& s, int groups) {
+  return ((shared_items(s, groups) + s.B + 1) * 16 + 255) & ~(size_t)255;
+}
+inline size_t shared_part_bytes(const DecodeShape& s, int groups) {
+  const int waves = shared_waves(s, groups);
+  return (DEC_WAVES / waves + shared_items(s, groups)) * DEC_QT * waves * decode_part_stride(s.D) * 4;
+}
+inline size_t shared_own_bytes(const DecodeShape& s) { return (decode_workspace_bytes(s) + 255) & ~(size_t)255; }
+inline size_t shared_workspace_bytes(const DecodeShape& s, int groups) {
+  return shared_own_bytes(s) + shared_desc_bytes(s, groups) + shared_part_bytes(s, groups);
+}
+hipError_t launch_shared_decode(const DecodeShape& s, const SharedArgs& a, void* ws, hipStream_t st);
+
+// Smallest and largest keys of the pages that hold positions from[b] to lens[b].
+struct SummaryArgs {
+  const __bf16* K;
+  PageLayout pages;
+  const int* table;  // [B][width], rows table_stride apart
+  int B, Hkv, width;
+  int64_t table_stride;
+  const int *from, *lens;
+  __bf16* summaries;  // [pages][Hkv][2][D]
+  int split;          // workgroups a sequence and KV head (set by the launcher)
+};
+hipError_t launch_summarize(const SummaryArgs& a, int D, hipStream_t st);
+
+// The pages that each sequence and KV head attends to.
+struct SelectArgs {
+  const __bf16* Q;          // [B][Hkv][rows][D]
+  const __bf16* summaries;  // [num_pages][Hkv][2][D]
+  const int* table;         // [B][width], rows table_stride apart
+  int B, Hkv, rows, width;
+  int64_t table_stride;
+  const int* lens;
+  int num_pages, log_size, budget, first, last;
+  int* lists;      // [B][Hkv][budget]
+  int* rows_out;   // [B][Hkv]
+  uint64_t* keys;  // workspace: [B][Hkv][width]
+};
+inline size_t select_workspace_bytes(int B, int Hkv, int width) { return (size_t)B * Hkv * width * 8; }
+hipError_t launch_select(const SelectArgs& a, int D, hipStream_t st);
+
 }  // namespace bd
