@@ -313,6 +313,15 @@ __device__ inline bf16x8 pack8(const f32x16& acc, int base) {
   return r;
 }
 
+// Two values as bf16 (round to nearest even), the first in the low half.
+__device__ inline uint32_t pack2(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  bf16x2 r;
+  r[0] = (bf16)a;
+  r[1] = (bf16)b;
+  return __builtin_bit_cast(uint32_t, r);
+}
+
 // Store four consecutive bf16 values (8 bytes).
 __device__ inline void st_bf16x4(bf16* p, float a, float b, float c, float d) {
   bf16x4 v;
@@ -354,6 +363,12 @@ __device__ inline float tree_max(const float* v) {
   } else {
     return fmaxf(tree_max<N / 2>(v), tree_max<N - N / 2>(v + N / 2));
   }
+}
+// Sum of N values (a power of two) as a balanced tree.
+template <int N>
+__device__ inline float tree_add(const float* v) {
+  if constexpr (N == 1) return v[0];
+  else return tree_add<N / 2>(v) + tree_add<N / 2>(v + N / 2);
 }
 // Sum of the 16 K entries of K accumulators as a balanced tree.
 template <int K>

@@ -375,8 +375,10 @@ struct SharedArgs {
 // rows for each wave of a team; a team as large as the average group needs.
 inline int shared_waves(const DecodeShape& s, int groups) {
   const long long rows = ((long long)s.B * (s.Hq / s.Hkv) * s.S + groups - 1) / groups;
-  return rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+  return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
 }
+// Teams that work on the prefixes, at most (four waves: two a CU, eight: one).
+inline int shared_runs(int waves) { return waves >= 4 ? 2 * DEC_WAVES / waves : DEC_WAVES / waves; }
 inline size_t shared_items(const DecodeShape& s, int groups) {
   const size_t rows = (size_t)s.B * (s.Hq / s.Hkv) * s.S;
   return (size_t)s.Hkv * (rows / (DEC_QT * shared_waves(s, groups)) + (groups < s.B ? groups : s.B));
@@ -389,7 +391,7 @@ inline size_t shared_desc_bytes(const DecodeShape& s, int groups) {
 }
 inline size_t shared_part_bytes(const DecodeShape& s, int groups) {
   const int waves = shared_waves(s, groups);
-  return (DEC_WAVES / waves + shared_items(s, groups)) * DEC_QT * waves * decode_part_stride(s.D) * 4;
+  return (shared_runs(waves) + shared_items(s, groups)) * DEC_QT * waves * decode_part_stride(s.D) * 4;
 }
 inline size_t shared_own_bytes(const DecodeShape& s) { return (decode_workspace_bytes(s) + 255) & ~(size_t)255; }
 inline size_t shared_workspace_bytes(const DecodeShape& s, int groups) {

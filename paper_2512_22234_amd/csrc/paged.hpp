@@ -81,34 +81,19 @@ __device__ inline int paged_tiles(const PagedParams& p, int len) {
 //   60,000        254.3 211.0  204.3 184.9  175.8 174.5  162.3 166.2  159.2 164.2  157.7 162.3
 // (64 sequences of 512 to 8192, 98 tiles an item: heads outermost 137.8 and 138.5, tokens 133.4 and 139.8).
 // Teams take two tiles at least (dec_runs).
-template <int D, int TW>
+// Where every item leaves partial results, its run waits for its stores: three runs a CU (16 groups of
+// 6 to 8 sequences, one token: 92.8 us a call, with the rule above 96.0).
+template <int D, int TW, bool PARTS>
 __device__ inline int paged_runs(int T, int items) {
   if (TW > 1) return dec_runs<TW>(DEC_WAVES / TW, T);
   const int three = imax(256, cdiv(T, 3));
-  return imin(T, D == 64 ? imin(three, 768) : T < 1152 ? three : T >> 3 <= items ? 768 : 512);
+  return imin(T, D == 64 || PARTS ? imin(three, 768) : T < 1152 ? three : T >> 3 <= items ? 768 : 512);
 }
 // First tile of run gw <= n (the runs cut T tiles into n near-equal pieces).
 __device__ inline int paged_run_start(int gw, int n, int T) {
   if (T < 1 << 22) return (int)((unsigned)gw * (unsigned)T / (unsigned)n);
   return (int)((unsigned)(((unsigned long long)gw * T) >> 8) / ((unsigned)n >> 8));  // (n is a multiple of 256 here)
 }
-
-template <int D, int TW, int KT, int NST>
-struct PagedSmem {
-  static constexpr int TEAMS = TW == 1 ? 3 : 1;  // teams per workgroup (paged_runs: at most 768 runs)
-  static constexpr int NW = TW * TEAMS;          // waves per workgroup
-  static constexpr uint32_t TILE = KT * D * 2;   // bytes of one swizzled K or V tile
-  alignas(256) char buf[TEAMS][NST * 2 * TILE];  // per team: a ring of K and V tiles
-  int wsum[NW];                                  // prologue: per-wave sums of the scan
-  int start_b[TEAMS], start_off[TEAMS];          // where each team's run starts
-};
-// Prefix: per-wave sums of members and of row groups, and each team's first group.
-template <int NW, int TEAMS>
-struct PrefixSmem {
-  int wmem[NW], wrow[NW];
-  int first[TEAMS], n[TEAMS], row[TEAMS];
-};
-struct Nothing {};
 
 // Position of a tile: sequence b (cache length len, nt tiles per item), KV head
 // h and row group g of the item, tile j of it.
@@ -121,37 +106,29 @@ struct PrefixPos : PagedPos {
   int ng, first, n, row;
 };
 
-// `lens` is the parameters' array as a restrict kernel argument, read through the
-// scalar cache where the index is uniform.
-template <int D, int TW, int KT, int NST, PagedMode MODE>
-__global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(PagedParams p, const int* __restrict__ lens) {
-  constexpr bool LISTS = MODE == PagedMode::Lists, PREFIX = MODE == PagedMode::Prefix;
-  constexpr bool PARTS = MODE == PagedMode::Own || PREFIX;  // every item leaves partial results
-  using Pos = std::conditional_t<PREFIX, PrefixPos, PagedPos>;
-  constexpr int DS = D / 16, DB = D / 32, PST = D + 4, KB = KT / 32;
-  using Smem = PagedSmem<D, TW, KT, NST>;
-  constexpr int TEAMS = Smem::TEAMS, NW = Smem::NW, NT = 64 * NW;
-  constexpr int NP = KT / 16;  // 16-row pieces of a tile
-  static_assert(NP * NST <= 32, "pieces of the tiles in flight fit a word");
-  __shared__ Smem sm;
-  __shared__ std::conditional_t<PREFIX, PrefixSmem<NW, TEAMS>, Nothing> sp;
+// The tiles of all prefixes in order of (group, KV head, row group): how many there
+// are, where a run starts, and what follows a tile.  NW waves scan the groups.
+template <int KT, int TW, int NW, int TEAMS>
+struct PrefixWork {
+  struct Smem {
+    int wmem[NW], wrow[NW], wsum[NW];  // per-wave sums: members, row groups, tiles of a KV head
+    int b[TEAMS], off[TEAMS], first[TEAMS], n[TEAMS], row[TEAMS];  // where each team's run starts
+  };
+  const PagedParams& p;
+  const int* __restrict__ lens;
+  int c0, c1, before_members, before_rows, before_tiles, tiles;  // this thread's groups, what lies before them, their tiles
 
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l32 = lane & 31, g2 = lane >> 5;
-  const int tm = TW == 1 ? w : 0, tw = TW == 1 ? 0 : w;  // team of the workgroup, wave of the team
-  const int ng = TW < 4 || PREFIX ? 1 : p.d.ng;          // (decode_groups: smaller teams hold all rows of a KV head)
-  const int I = p.d.Hkv * ng;                            // items per sequence (Prefix: and row group)
-  // Prefix: members of group b, whose first is sequence `first` (sizes that pass the sequences end there), and their row groups
-  auto members = [&](int b, int first) { return imin(imax(p.sizes[b], 0), p.seqs - first); };
-  auto row_groups = [&](int n) { return tiles_of<32 * TW>(n * p.d.G * p.d.S); };
+  // Members of group b, whose first is sequence `first` (sizes that pass the sequences end there).
+  __device__ int members(int b, int first) const { return imin(imax(p.sizes[b], 0), p.seqs - first); }
+  __device__ int row_groups(int n) const { return tiles_of<32 * TW>(n * p.d.G * p.d.S); }
+  __device__ int tiles_at(int b) const { return imax(tiles_of<KT>(dec_len(p.d, lens, b)), 1); }
 
-  // ---- prologue: T, and the position of each team's first tile (as over a dense cache) ----
-  const int cpt = cdiv(p.d.B, NT);
-  const int c0 = imin(p.d.B, tid * cpt), c1 = imin(p.d.B, c0 + cpt);
-  int csum = 0;
-  int cfirst = 0, cgroups = 0;  // Prefix: members and row groups of the groups before c0
-  if constexpr (PREFIX) {
+  // Tiles of a KV head in all groups; the first workgroup notes the sequences that are in one.
+  __device__ int scan(Smem& sm, int tid) {
+    const int lane = tid & 63, w = tid >> 6;
+    const int cpt = cdiv(p.d.B, 64 * NW);
+    c0 = imin(p.d.B, tid * cpt);
+    c1 = imin(p.d.B, c0 + cpt);
     int mem = 0;
     for (int b = c0; b < c1; ++b) mem += members(b, mem);
     int imem = mem;
@@ -160,35 +137,154 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
       const int u = __shfl_up(imem, o, 64);
       if (lane >= o) imem = imin(imem + u, p.seqs);
     }
-    if (lane == 63) sp.wmem[w] = imem;
+    if (lane == 63) sm.wmem[w] = imem;
     __syncthreads();
-    int last = __shfl_up(imem, 1, 64);
-    cfirst = lane == 0 ? 0 : last;
+    const int last = __shfl_up(imem, 1, 64);
+    before_members = lane == 0 ? 0 : last;
     int all = 0;
     for (int v = 0; v < NW; ++v) {
-      if (v < w) cfirst = imin(cfirst + sp.wmem[v], p.seqs);
-      all = imin(all + sp.wmem[v], p.seqs);
+      if (v < w) before_members = imin(before_members + sm.wmem[v], p.seqs);
+      all = imin(all + sm.wmem[v], p.seqs);
     }
     if (blockIdx.x == 0 && tid == 0) *p.members = all;
     int rows = 0;
-    for (int b = c0, first = cfirst; b < c1; ++b) {
+    tiles = 0;
+    for (int b = c0, first = before_members; b < c1; ++b) {
       const int n = members(b, first), r = row_groups(n);
       first += n;
       rows += r;
-      csum += paged_tiles<KT>(p, dec_len(p.d, lens, b)) * r;
+      tiles += tiles_at(b) * r;
     }
-    int irow = rows;
+    int irow = rows, itile = tiles;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-      const int u = __shfl_up(irow, o, 64);
-      if (lane >= o) irow += u;
+      const int u = __shfl_up(irow, o, 64), t = __shfl_up(itile, o, 64);
+      if (lane >= o) {
+        irow += u;
+        itile += t;
+      }
     }
-    if (lane == 63) sp.wrow[w] = irow;
-    cgroups = irow - rows;
-  } else {
-#pragma unroll 4
-    for (int b = c0; b < c1; ++b) csum += paged_tiles<KT>(p, dec_len(p.d, lens, b));
+    if (lane == 63) {
+      sm.wrow[w] = irow;
+      sm.wsum[w] = itile;
+    }
+    __syncthreads();
+    before_rows = irow - rows;
+    before_tiles = itile - tiles;
+    int total = 0;
+    for (int v = 0; v < NW; ++v) {
+      before_rows += v < w ? sm.wrow[v] : 0;
+      before_tiles += v < w ? sm.wsum[v] : 0;
+      total += sm.wsum[v];
+    }
+    return __builtin_amdgcn_readfirstlane(total);
   }
+  // Notes where team v's run starts, at tile x0 of all.  (A barrier before start().)
+  __device__ void find(Smem& sm, int v, int x0) const {
+    const int I = p.d.Hkv;
+    if (tiles == 0 || x0 < before_tiles * I || x0 >= (before_tiles + tiles) * I) return;
+    int pb = before_tiles, first = before_members, row = before_rows;
+    for (int b = c0; b < c1; ++b) {
+      const int n = members(b, first), r = row_groups(n), t = tiles_at(b) * r;
+      if (x0 < (pb + t) * I) {
+        sm.b[v] = b;
+        sm.off[v] = x0 - pb * I;
+        sm.first[v] = first;
+        sm.n[v] = n;
+        sm.row[v] = row;
+        return;
+      }
+      pb += t;
+      first += n;
+      row += r;
+    }
+  }
+  __device__ PrefixPos start(const Smem& sm, int v) const {
+    PrefixPos q;
+    q.b = __builtin_amdgcn_readfirstlane(sm.b[v]);
+    const int off = __builtin_amdgcn_readfirstlane(sm.off[v]);
+    q.first = __builtin_amdgcn_readfirstlane(sm.first[v]);
+    q.n = __builtin_amdgcn_readfirstlane(sm.n[v]);
+    q.row = __builtin_amdgcn_readfirstlane(sm.row[v]);
+    q.len = __builtin_amdgcn_readfirstlane(dec_len(p.d, lens, q.b));
+    q.nt = imax(tiles_of<KT>(q.len), 1);
+    q.ng = row_groups(q.n);
+    const int item = off / q.nt;
+    q.j = off - item * q.nt;
+    q.h = item / q.ng;
+    q.g = item - q.h * q.ng;
+    return q;
+  }
+  // The first tile of the item behind that of q.
+  __device__ __attribute__((always_inline)) void next_item(PrefixPos& q) const {
+    q.j = 0;
+    if (++q.g < q.ng) return;
+    q.g = 0;
+    if (++q.h < p.d.Hkv) return;
+    q.h = 0;
+    // (scalar loads: nothing writes these arrays while the kernel runs)
+    typedef const __attribute__((address_space(4))) int* Uniform;
+    const Uniform sizes = (Uniform)(uintptr_t)p.sizes, all = (Uniform)(uintptr_t)p.d.cache_lens;
+    do {  // (to the next group that has members)
+      q.first += q.n;
+      q.row += q.ng;
+      if (++q.b >= p.d.B) return;
+      q.n = imin(imax(sizes[q.b], 0), p.seqs - q.first);
+      q.ng = row_groups(q.n);
+    } while (q.n == 0);
+    q.len = imin(imax(all[q.b], 0), p.d.C);
+    q.nt = imax(tiles_of<KT>(q.len), 1);
+  }
+  // Query row R of the group's rows of a KV head (rows past the last: the last).
+  __device__ __attribute__((always_inline)) size_t query_row(const DecParams& a, const PrefixPos& q, int R, bool& valid) const {
+    const unsigned rows = (unsigned)(a.G * a.S);  // of a member
+    valid = R < q.n * (int)rows;
+    const unsigned Rc = valid ? R : q.n * rows - 1, m = Rc / rows;
+    return ((size_t)(q.first + m) * a.Hkv + q.h) * rows + (Rc - m * rows);
+  }
+};
+struct Nothing {};
+template <int D, int TW, int KT, int NST, PagedMode MODE>
+struct PagedSmem {
+  static constexpr int TEAMS = TW == 1 ? 3 : 1;  // teams per workgroup (paged_runs: at most 768 runs)
+  static constexpr int NW = TW * TEAMS;          // waves per workgroup
+  static constexpr uint32_t TILE = KT * D * 2;   // bytes of one swizzled K or V tile
+  alignas(256) char buf[TEAMS][NST * 2 * TILE];  // per team: a ring of K and V tiles
+  int wsum[NW];                                  // prologue: per-wave sums of the scan
+  int start_b[TEAMS], start_off[TEAMS];          // where each team's run starts
+  using Work = PrefixWork<KT, TW, NW, TEAMS>;
+  // (in here: with a second object the compiler tells their accesses apart in a way that has it wait for all copies in
+  // flight before the next read of a tile)
+  std::conditional_t<MODE == PagedMode::Prefix, typename Work::Smem, Nothing> work;
+};
+
+// `lens` is the parameters' array as a restrict kernel argument, read through the
+// scalar cache where the index is uniform.
+template <int D, int TW, int KT, int NST, PagedMode MODE>
+__global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(PagedParams p, const int* __restrict__ lens) {
+  constexpr bool LISTS = MODE == PagedMode::Lists, PREFIX = MODE == PagedMode::Prefix;
+  constexpr bool PARTS = MODE == PagedMode::Own || PREFIX;  // every item leaves partial results
+  using Pos = std::conditional_t<PREFIX, PrefixPos, PagedPos>;
+  constexpr int DS = D / 16, DB = D / 32, PST = D + 4, KB = KT / 32;
+  using Smem = PagedSmem<D, TW, KT, NST, MODE>;
+  constexpr int TEAMS = Smem::TEAMS, NW = Smem::NW, NT = 64 * NW;
+  constexpr int NP = KT / 16;  // 16-row pieces of a tile
+  static_assert(NP * NST <= 32, "pieces of the tiles in flight fit a word");
+  __shared__ Smem sm;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, g2 = lane >> 5;
+  const int tm = TW == 1 ? w : 0, tw = TW == 1 ? 0 : w;  // team of the workgroup, wave of the team
+  const int ng = TW < 4 || PREFIX ? 1 : p.d.ng;          // (decode_groups: smaller teams hold all rows of a KV head)
+  const int I = p.d.Hkv * ng;                            // items per sequence (Prefix: and row group)
+  typename Smem::Work work{p, lens};
+  // ---- prologue: T, and the position of each team's first tile (as over a dense cache) ----
+  const int cpt = cdiv(p.d.B, NT);
+  const int c0 = imin(p.d.B, tid * cpt), c1 = imin(p.d.B, c0 + cpt);
+  int csum = 0;
+#pragma unroll 4
+  for (int b = c0; b < c1; ++b) csum += PREFIX ? 0 : paged_tiles<KT>(p, dec_len(p.d, lens, b));
   int incl = csum;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -203,45 +299,28 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
     const int s = sm.wsum[v];
     before += v < w ? s : 0;
     total += s;
-    if constexpr (PREFIX) cgroups += v < w ? sp.wrow[v] : 0;
   }
   const int excl = before + incl - csum;  // tiles per item of the sequences before c0
   total = __builtin_amdgcn_readfirstlane(total);
+  if constexpr (PREFIX) total = work.scan(sm.work, tid);
   const int T = total * I;  // checked on the host to fit in 31 bits
-  const int n = paged_runs<D, TW>(T, p.d.B * I);
+  const int n = paged_runs<D, TW, PARTS>(T, p.d.B * I);
   const bool stream = total * p.d.Hkv > (int)(DEC_STREAM_BYTES / (2 * Smem::TILE));
   auto run_of = [&](int v) { return v * (int)gridDim.x + (int)blockIdx.x; };  // run of a workgroup's team v
 #pragma unroll
   for (int v = 0; v < TEAMS; ++v) {
     const int x0 = run_of(v) < n ? paged_run_start(run_of(v), n, T) : T;
-    if (csum > 0 && excl * I <= x0 && x0 < (excl + csum) * I) {
+    if constexpr (PREFIX) work.find(sm.work, v, x0);
+    else if (csum > 0 && excl * I <= x0 && x0 < (excl + csum) * I) {
       int pb = excl;
-      if constexpr (PREFIX) {
-        int first = cfirst, row = cgroups;
-        for (int b = c0; b < c1; ++b) {
-          const int m = members(b, first), r = row_groups(m), nt = paged_tiles<KT>(p, dec_len(p.d, lens, b)) * r;
-          if (x0 < (pb + nt) * I) {
-            sm.start_b[v] = b;
-            sm.start_off[v] = x0 - pb * I;
-            sp.first[v] = first;
-            sp.n[v] = m;
-            sp.row[v] = row;
-            break;
-          }
-          pb += nt;
-          first += m;
-          row += r;
+      for (int b = c0; b < c1; ++b) {
+        const int nt = paged_tiles<KT>(p, dec_len(p.d, lens, b));
+        if (x0 < (pb + nt) * I) {
+          sm.start_b[v] = b;
+          sm.start_off[v] = x0 - pb * I;
+          break;
         }
-      } else {
-        for (int b = c0; b < c1; ++b) {
-          const int nt = paged_tiles<KT>(p, dec_len(p.d, lens, b));
-          if (x0 < (pb + nt) * I) {
-            sm.start_b[v] = b;
-            sm.start_off[v] = x0 - pb * I;
-            break;
-          }
-          pb += nt;
-        }
+        pb += nt;
       }
     }
   }
@@ -252,48 +331,24 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
   if (gw >= n) return;
   const int x0 = paged_run_start(gw, n, T), x1 = paged_run_start(gw + 1, n, T);
   Pos pc;
-  pc.b = __builtin_amdgcn_readfirstlane(sm.start_b[tm]);
-  const int off = __builtin_amdgcn_readfirstlane(sm.start_off[tm]);
-  pc.len = __builtin_amdgcn_readfirstlane(dec_len(p.d, lens, pc.b));
-  pc.nt = paged_tiles<KT>(p, pc.len);
-  const int item0 = off / pc.nt;  // of the sequence's items
-  pc.j = off - item0 * pc.nt;
   if constexpr (PREFIX) {
-    pc.first = __builtin_amdgcn_readfirstlane(sp.first[tm]);
-    pc.n = __builtin_amdgcn_readfirstlane(sp.n[tm]);
-    pc.row = __builtin_amdgcn_readfirstlane(sp.row[tm]);
-    pc.ng = row_groups(pc.n);
-    pc.h = item0 / pc.ng;
-    pc.g = item0 - pc.h * pc.ng;
-  } else if constexpr (LISTS) {
-    pc.h = pc.b % p.heads;
-    pc.g = item0;
+    pc = work.start(sm.work, tm);
   } else {
-    pc.h = item0 / ng;
-    pc.g = item0 - pc.h * ng;
+    pc.b = __builtin_amdgcn_readfirstlane(sm.start_b[tm]);
+    const int off = __builtin_amdgcn_readfirstlane(sm.start_off[tm]);
+    pc.len = __builtin_amdgcn_readfirstlane(dec_len(p.d, lens, pc.b));
+    pc.nt = paged_tiles<KT>(p, pc.len);
+    const int item0 = off / pc.nt;  // of the sequence's items
+    pc.j = off - item0 * pc.nt;
+    pc.h = LISTS ? pc.b % p.heads : item0 / ng;
+    pc.g = LISTS ? item0 : item0 - pc.h * ng;
   }
 
   auto advance = [&](Pos q) __attribute__((always_inline)) {
     if (++q.j == q.nt) {
       q.j = 0;
       if constexpr (PREFIX) {
-        if (++q.g == q.ng) {
-          q.g = 0;
-          if (++q.h == p.d.Hkv) {
-            q.h = 0;
-            do {  // (to the next group that has members)
-              q.first += q.n;
-              q.row += q.ng;
-              if (++q.b >= p.d.B) break;
-              q.n = __builtin_amdgcn_readfirstlane(members(q.b, q.first));
-              q.ng = row_groups(q.n);
-            } while (q.n == 0);
-            if (q.b < p.d.B) {
-              q.len = __builtin_amdgcn_readfirstlane(dec_len(p.d, lens, q.b));
-              q.nt = paged_tiles<KT>(p, q.len);
-            }
-          }
-        }
+        work.next_item(q);
       } else if constexpr (LISTS) {
         if (++q.g == ng) {
           q.g = 0;
@@ -337,10 +392,7 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
   auto query_row = [&](const DecParams& p, Pos q, bool& valid) __attribute__((always_inline)) -> size_t {
     const int rl = 32 * tw + l32, R = q.g * p.grows + rl;
     if constexpr (PREFIX) {
-      const unsigned rows = (unsigned)(p.G * p.S);  // of a member
-      valid = R < q.n * (int)rows;
-      const unsigned Rc = valid ? R : q.n * rows - 1, m = Rc / rows;
-      return ((size_t)(q.first + m) * p.Hkv + q.h) * rows + (Rc - m * rows);
+      return work.query_row(p, q, R, valid);
     } else {
       valid = R < p.G * p.S && (TW == 1 || rl < p.grows);
       return ((size_t)q.b * p.Hq + (LISTS ? 0 : (size_t)q.h * p.G)) * p.S + (R < p.G * p.S ? R : p.G * p.S - 1);
@@ -544,7 +596,7 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
       }
       if (ends && lane == 0 && tw == 0) {
         // the runs holding this item: from the one holding its first tile to this one
-        const int first = (int)((((long long)item_start + 1) * n - 1) / T);
+        const int first = PARTS && item_start >= x0 ? gw : (int)((((long long)item_start + 1) * n - 1) / T);
         p.desc[item] = DecRuns{first, gw};
       }
       if constexpr (PREFIX) {
@@ -691,7 +743,7 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
 
 template <int D, int TW, int KT, int NST, PagedMode MODE>
 void launch_paged_kernel(const PagedParams& p, hipStream_t st) {
-  using Smem = PagedSmem<D, TW, KT, NST>;
+  using Smem = PagedSmem<D, TW, KT, NST, MODE>;
   hipLaunchKernelGGL((paged_kernel<D, TW, KT, NST, MODE>), dim3(TW == 1 ? 256 : DEC_WAVES / TW), dim3(64 * Smem::NW), 0, st, p,
                      p.d.cache_lens);
 }
@@ -738,7 +790,7 @@ template <int D, PagedMode MODE>
 hipError_t launch_paged_runs(const DecodeGroups& g, const PagedParams& p, hipStream_t st) {
   if (g.waves == 1) launch_paged_kernel<D, 1, 32, 2, MODE>(p, st);
   else if (g.waves == 2) launch_paged_kernel<D, 2, (D == 64 ? 64 : 32), 4, MODE>(p, st);
-  else launch_paged_kernel<D, 4, 64, 512 / D, MODE>(p, st);
+  else if constexpr (MODE != PagedMode::Prefix) launch_paged_kernel<D, 4, 64, 512 / D, MODE>(p, st);
   return hipGetLastError();
 }
 
