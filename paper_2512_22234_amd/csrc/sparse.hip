@@ -81,113 +81,181 @@ __device__ inline uint64_t score_key(double x) {
   return u >> 63 ? ~u : u | 1ull << 63;
 }
 
-constexpr int SCORE_PAGES = 256;  // of a workgroup
+// Pages of a sequence that hold its tokens, and the tokens.
+struct SelectSeq {
+  int len, used;
+};
+__device__ inline SelectSeq select_seq(const SelectArgs& a, int b) {
+  SelectSeq q;
+  q.len = imin(imax(a.lens[b], 0), a.width << a.log_size);
+  q.used = (q.len + (1 << a.log_size) - 1) >> a.log_size;
+  return q;
+}
 
-// Keys of SCORE_PAGES pages of one sequence and KV head.
-template <int D>
-__global__ __launch_bounds__(256) void score_kernel(SelectArgs a) {
-  constexpr int CPP = D / 4, PPI = 64 / CPP, U = 8;  // 16-byte chunks of a summary, summaries a load, loads in flight
-  __shared__ double sums[2][256];
-  const int chunks = cdiv(a.width, SCORE_PAGES);
-  const int c = blockIdx.x % chunks, bh = blockIdx.x / chunks, h = bh % a.Hkv, b = bh / a.Hkv;
+// Keys of the pages j0 <= j < j1 of KV head h of sequence b, by NW waves, to put(j, key); ids: room
+// for the j1 - j0 entries of the table, which are left there.
+//   A load covers 1 KiB, PPI summaries of CPP lanes each: half of the lanes of a page hold
+//   smallest values, half largest ones, eight features a lane.  U loads are in flight while
+//   the U before them are summed, and the first while the query rows are.  A page's lanes are
+//   summed U pages at a time: at each step a lane keeps half of its pages and sends the others,
+//   so that 1 + 2 + 4 numbers go instead of 8 a step, in the same order for every page.
+template <int D, int NW>
+struct ScoreSmem {
+  double part[NW][2 * D], sum[2 * D];  // at e * CPP + (lane of a page): feature e of eight (no two lanes in one bank)
+};
+template <int D, int NW, class Put>
+__device__ inline void score_pages(const SelectArgs& a, ScoreSmem<D, NW>& sm, int* ids, int b, int h, int used, int j0, int j1,
+                                   Put put) {
+  constexpr int CPP = D / 4, PPI = 64 / CPP, U = 8, UQ = 4;
+  static_assert(2 * D <= 64 * NW, "a thread a sum");
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int P = 1 << a.log_size;
-  const int len = imin(imax(a.lens[b], 0), a.width << a.log_size), used = (len + P - 1) >> a.log_size;
-  if (c * SCORE_PAGES >= used) return;
-
-  // Q+ and Q-
+  const int in_page = lane % CPP, side = in_page / (CPP / 2), d0 = in_page % (CPP / 2) * 8;
+  // query rows r0, r0 + NW * PPI, ...: UQ in flight
+  const bf16* q = a.Q + ((int64_t)b * a.Hkv + h) * a.rows * D + d0;
+  int r0 = w * PPI + lane / CPP;
+  u32x4 v[UQ];
+  auto load_rows = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < UQ; ++u) v[u] = ld16(q + (int64_t)imin(r0 + u * NW * PPI, a.rows - 1) * D);
+  };
+  load_rows();
   {
-    const int d = tid % D;
-    double up = 0, down = 0;
-    for (int r = tid / D; r < a.rows; r += 256 / D) {
-      const double q = (double)(float)a.Q[((int64_t)bh * a.rows + r) * D + d];
-      up += fmax(q, 0.0);
-      down += fmin(q, 0.0);
-    }
-    sums[1][tid] = up;
-    sums[0][tid] = down;
-    __syncthreads();
-    if (tid < D) {
-#pragma unroll
-      for (int u = 1; u < 256 / D; ++u) {
-        up += sums[1][tid + u * D];
-        down += sums[0][tid + u * D];
-      }
-      sums[1][tid] = up;
-      sums[0][tid] = down;
-    }
-    __syncthreads();
+    const int* row = a.table + (int64_t)b * a.table_stride;
+    for (int j = j0 + tid; j < j1; j += 64 * NW) ids[j - j0] = row[j];
   }
-  const int part = lane % CPP, side = part / (CPP / 2), d0 = part % (CPP / 2) * 8;  // side: of the smallest, of the largest values
-  double weight[8];
+  __syncthreads();
+  int id[U];
+  u32x4 x[U];
+  auto load = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) weight[e] = sums[side][d0 + e];
-
-  const int* row = a.table + (int64_t)b * a.table_stride;
-  const int end = imin(used, (c + 1) * SCORE_PAGES);
-  for (int j0 = c * SCORE_PAGES + w * U * PPI; j0 < end; j0 += 4 * U * PPI) {
-    int id[U];
-    u32x4 x[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) id[u] = row[imin(j0 + u * PPI + lane / CPP, used - 1)];
+    for (int u = 0; u < U; ++u) id[u] = ids[imin(j + u * PPI + lane / CPP, j1 - 1) - j0];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int some = (unsigned)id[u] < (unsigned)a.num_pages ? id[u] : 0;
       x[u] = ld16(a.summaries + (((int64_t)some * a.Hkv + h) * 2 + side) * D + d0);
     }
-    double s[U];
+  };
+  int j = j0 + w * U * PPI;
+  if (j < j1) load(j);
+
+  // Q- and Q+: every lane the features and the side that it weighs, of its rows
+  double weight[8];
+  {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      double t[8];
+    for (int e = 0; e < 8; ++e) weight[e] = 0;
+    while (r0 < a.rows) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) t[e] = weight[e] * (double)(e & 1 ? bf16_hi(x[u][e / 2]) : bf16_lo(x[u][e / 2]));
-      s[u] = ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+      for (int u = 0; u < UQ; ++u) {
+        if (r0 + u * NW * PPI >= a.rows) break;
 #pragma unroll
-      for (int o = CPP / 2; o > 0; o >>= 1) s[u] += __shfl_xor(s[u], o);
+        for (int e = 0; e < 8; ++e) {
+          const float y = e & 1 ? bf16_hi(v[u][e / 2]) : bf16_lo(v[u][e / 2]);
+          weight[e] += (double)(side ? fmaxf(y, 0.f) : fminf(y, 0.f));
+        }
+      }
+      r0 += UQ * NW * PPI;
+      if (r0 < a.rows) load_rows();
     }
 #pragma unroll
+    for (int o = CPP; o < 64; o <<= 1)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) weight[e] += __shfl_xor(weight[e], o);
+    if (lane < CPP) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sm.part[w][e * CPP + lane] = weight[e];
+    }
+    __syncthreads();
+    if (tid < 2 * D) {
+      double y = sm.part[0][tid];
+#pragma unroll
+      for (int p = 1; p < NW; ++p) y += sm.part[p][tid];
+      sm.sum[tid] = y;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) weight[e] = sm.sum[e * CPP + in_page];
+  }
+
+  for (; j < j1; j += NW * U * PPI) {
+    double s[U];
+    unsigned bad = 0;  // pages that are none
+#pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int j = j0 + u * PPI + lane / CPP;
-      if (part == u && j < end) {
-        uint64_t key = score_key(s[u]);
-        if (j < a.first || j >= used - a.last) key = ~0ull;
-        if ((unsigned)id[u] >= (unsigned)a.num_pages) key = 0;
-        a.keys[(int64_t)bh * a.width + j] = key;
+      double t[2] = {0, 0};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e & 1] = fma(weight[e], (double)(e & 1 ? bf16_hi(x[u][e / 2]) : bf16_lo(x[u][e / 2])), t[e & 1]);
+      s[u] = t[0] + t[1];
+      bad |= (unsigned)id[u] < (unsigned)a.num_pages ? 0u : 1u << u;
+    }
+    if (j + NW * U * PPI < j1) load(j + NW * U * PPI);
+    int mine = 0;  // the load whose page this lane ends with
+#pragma unroll
+    for (int o = CPP / 2, n = U; o > 0; o >>= 1) {
+      if (n > 1) {
+        const bool high = lane & o;
+        n /= 2;
+#pragma unroll
+        for (int u = 0; u < U / 2; ++u)
+          if (u < n) {
+            const double send = high ? s[u] : s[u + n];
+            s[u] = (high ? s[u + n] : s[u]) + __shfl_xor(send, o);
+          }
+        mine = 2 * mine + (high ? 1 : 0);
+      } else {
+        s[0] += __shfl_xor(s[0], o);
       }
     }
+    const int at = j + mine * PPI + lane / CPP;
+    uint64_t key = score_key(s[0]);
+    if (at < a.first || at >= used - a.last) key = ~0ull;
+    if (bad >> mine & 1) key = 0;
+    if (in_page % (CPP / U) == 0 && at < j1) put(at, key);
   }
 }
 
 // ---- the choice ----
 
-constexpr int SELECT_NT = 512;
+constexpr int CHOOSE_NT = 512, SCORE_NT = 512, SELECT_NT = 1024;  // threads of the kernels below
+constexpr int SELECT_KEYS = 4096;   // of a sequence and KV head, in LDS
+constexpr int SCORE_PAGES = 256;    // of a workgroup, where several share a sequence and KV head
 
-// One workgroup a sequence and KV head: the highest `budget` keys, equal ones by
-// position.  The lowest of them is found eight bits at a time, from counts of the
+// Inclusive sum over the wave's lanes, in registers.
+__device__ inline int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);   // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);   // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);   // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15, into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31, into rows 2 and 3
+  return x;
+}
+
+template <int NT>
+struct SelectSmem {
+  int bins[2][256];
+  int found[3];  // digit, keys above it, keys in it
+  int above[NT / 64], equal[NT / 64];
+};
+
+// The list of sequence and KV head bh, of the keys key_of(0 .. used - 1) of the pages id_of(...): the highest `budget`,
+// equal ones by position.  The lowest of them is found eight bits at a time, from counts of the
 // keys that agree with it so far; then a pass in order of positions writes the list.
-__global__ __launch_bounds__(SELECT_NT) void select_kernel(SelectArgs a) {
-  constexpr int NW = SELECT_NT / 64;
-  __shared__ int bins[256];
-  __shared__ int found[3];  // digit, keys above it, keys in it
-  __shared__ int wabove[NW], wequal[NW];
-  const int bh = blockIdx.x, b = bh / a.Hkv;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int P = 1 << a.log_size;
-  const int len = imin(imax(a.lens[b], 0), a.width << a.log_size), used = (len + P - 1) >> a.log_size;
-  const uint64_t* keys = a.keys + (int64_t)bh * a.width;
-
-  // the threshold: keys above it are chosen, and the first `equal` of those that are it
+template <int NT, class Key, class Id>
+__device__ inline void select_pages(const SelectArgs& a, SelectSmem<NT>& sm, int bh, const SelectSeq& seq, Key key_of, Id id_of) {
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, used = seq.used;
+  // the threshold: keys from `low` on are chosen, of those that are `low` the first `equal`
   uint64_t low = 1;
   int equal = INT32_MAX;
   if (used > a.budget) {
     uint64_t prefix = 0;
     int need = a.budget;
+    if (tid < 256) sm.bins[0][tid] = 0;
+    __syncthreads();
     for (int shift = 56; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += SELECT_NT) bins[i] = 0;
-      __syncthreads();
-      for (int j0 = 0; j0 < used; j0 += SELECT_NT) {
+      int* const bins = sm.bins[shift >> 3 & 1 ? 0 : 1];
+      for (int j0 = 0; j0 < used; j0 += NT) {
         const int j = j0 + tid;
-        const uint64_t key = j < used ? keys[j] : 0;
+        const uint64_t key = j < used ? key_of(j) : 0;
         const bool in = j < used && (shift == 56 || key >> (shift + 8) == prefix);
         const int digit = (int)(key >> shift) & 255;
         const uint64_t all = __ballot(in);
@@ -206,72 +274,128 @@ __global__ __launch_bounds__(SELECT_NT) void select_kernel(SelectArgs a) {
         int n[4], sum = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum += n[e] = bins[255 - 4 * lane - e];
-        int incl = sum;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-          const int u = __shfl_up(incl, o);
-          if (lane >= o) incl += u;
-        }
-        int above = incl - sum;
+        int above = wave_scan(sum) - sum;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           if (above < need && above + n[e] >= need) {
-            found[0] = 255 - 4 * lane - e;
-            found[1] = above;
-            found[2] = n[e];
+            sm.found[0] = 255 - 4 * lane - e;
+            sm.found[1] = above;
+            sm.found[2] = n[e];
           }
           above += n[e];
         }
+      } else if (tid >= NT - 256) {  // (the next digit's counts)
+        sm.bins[shift >> 3 & 1][tid - (NT - 256)] = 0;
       }
       __syncthreads();
-      prefix = prefix << 8 | (uint64_t)found[0];
-      need -= found[1];
-      const bool all = found[2] == need;  // all keys with these digits are chosen
+      prefix = prefix << 8 | (uint64_t)sm.found[0];
+      need -= sm.found[1];
       low = prefix << shift;
-      equal = shift == 0 ? need : INT32_MAX;
-      if (all) break;
-      __syncthreads();
+      if (sm.found[2] == need) break;  // all keys that begin so are chosen
+      if (shift == 0) equal = need;
     }
-    // (keys are counted from `low` on; without the last digits' count, all that begin with it are chosen)
-    if (low == 0) low = 1, equal = INT32_MAX;  // fewer pages than the budget can be chosen
+    if (low == 0) {  // fewer pages than the budget can be chosen
+      low = 1;
+      equal = INT32_MAX;
+    }
   }
   int* out = a.lists + (int64_t)bh * a.budget;
-  const int* row = a.table + (int64_t)b * a.table_stride;
-  int count = 0, met = 0;
-  bool tail = false;
+  int count = 0, met = 0, tail = -1;  // tail: keys up to the sequence's last page, if that is chosen (its own thread)
   const bool ties = equal != INT32_MAX;
-  for (int j0 = 0; j0 < used; j0 += SELECT_NT) {
+  for (int j0 = 0; j0 < used; j0 += NT) {
     const int j = j0 + tid;
-    const uint64_t key = j < used ? keys[j] : 0;
+    const uint64_t key = j < used ? key_of(j) : 0;
     const bool same = ties && key == low;
-    const uint64_t eq = __ballot(same);
-    const uint64_t gt = __ballot(!same && key >= low);
-    const uint64_t below = (1ull << lane) - 1;
-    if (lane == 0) wequal[w] = __builtin_popcountll(eq);
-    if (lane == 0) wabove[w] = __builtin_popcountll(gt);
+    const uint64_t eq = __ballot(same), gt = __ballot(!same && key >= low), below = (1ull << lane) - 1;
+    if (lane == 0) {
+      sm.equal[w] = __builtin_popcountll(eq);
+      sm.above[w] = __builtin_popcountll(gt);
+    }
     __syncthreads();
     int e0 = met, g0 = 0, all_e = 0, all_g = 0;  // equal keys and others chosen before this wave's
 #pragma unroll
-    for (int v = 0; v < NW; ++v) {
-      e0 += v < w ? wequal[v] : 0;
-      g0 += v < w ? wabove[v] : 0;
-      all_e += wequal[v];
-      all_g += wabove[v];
+    for (int v = 0; v < NT / 64; ++v) {
+      e0 += v < w ? sm.equal[v] : 0;
+      g0 += v < w ? sm.above[v] : 0;
+      all_e += sm.equal[v];
+      all_g += sm.above[v];
     }
     const int er = e0 + __builtin_popcountll(eq & below);  // rank among equal keys
     const bool chosen = (gt >> lane & 1) || (same && er < equal);
     const int at = count + g0 + __builtin_popcountll(gt & below) + imin(er, equal) - imin(met, equal);
     if (chosen) {
-      out[at] = row[j];
-      if (j == used - 1) a.rows_out[bh] = ((at + 1) << a.log_size) - ((used << a.log_size) - len);
-      tail |= j == used - 1;
+      out[at] = id_of(j);
+      if (j == used - 1) tail = ((at + 1) << a.log_size) - ((used << a.log_size) - seq.len);
     }
     count += all_g + imin(met + all_e, equal) - imin(met, equal);
     met += all_e;
     __syncthreads();
   }
-  for (int i = count + tid; i < a.budget; i += SELECT_NT) out[i] = -1;
-  if (!__syncthreads_or(tail) && tid == 0) a.rows_out[bh] = count << a.log_size;
+  for (int i = count + tid; i < a.budget; i += NT) out[i] = -1;
+  if (tid == (used > 0 ? (used - 1) % NT : 0)) a.rows_out[bh] = tail >= 0 ? tail : count << a.log_size;
+}
+
+// One workgroup a sequence and KV head, its pages and keys in LDS.
+// (four waves a SIMD: two workgroups a CU)
+template <int D, int KEYS>
+__global__ __launch_bounds__(CHOOSE_NT, 4) void choose_kernel(SelectArgs a) {
+  __shared__ struct {
+    uint64_t keys[KEYS];
+    int ids[KEYS];
+    ScoreSmem<D, CHOOSE_NT / 64> score;
+    SelectSmem<CHOOSE_NT> select;
+  } sm;
+  const int bh = blockIdx.x, h = bh % a.Hkv, b = bh / a.Hkv;
+  const SelectSeq seq = select_seq(a, b);
+  if (seq.used > a.budget) {
+    score_pages<D, CHOOSE_NT / 64>(a, sm.score, sm.ids, b, h, seq.used, 0, seq.used, [&](int j, uint64_t key) { sm.keys[j] = key; });
+    __syncthreads();
+    select_pages(a, sm.select, bh, seq, [&](int j) { return sm.keys[j]; }, [&](int j) { return sm.ids[j]; });
+  } else {  // every page that there is
+    const int* row = a.table + (int64_t)b * a.table_stride;
+    select_pages(a, sm.select, bh, seq, [&](int j) -> uint64_t { return (unsigned)row[j] < (unsigned)a.num_pages; },
+                 [&](int j) { return row[j]; });
+  }
+}
+
+// Several workgroups a sequence and KV head: keys of SCORE_PAGES pages each, in the workspace ...
+template <int D>
+__global__ __launch_bounds__(SCORE_NT) void score_kernel(SelectArgs a) {
+  __shared__ struct {
+    ScoreSmem<D, SCORE_NT / 64> score;
+    int ids[SCORE_PAGES];
+  } sm;
+  const int chunks = cdiv(a.width, SCORE_PAGES);
+  const int c = blockIdx.x % chunks, bh = blockIdx.x / chunks, h = bh % a.Hkv, b = bh / a.Hkv;
+  const SelectSeq seq = select_seq(a, b);
+  if (c * SCORE_PAGES >= seq.used) return;
+  uint64_t* keys = a.keys + (int64_t)bh * a.width;
+  score_pages<D, SCORE_NT / 64>(a, sm.score, sm.ids, b, h, seq.used, c * SCORE_PAGES, imin(seq.used, (c + 1) * SCORE_PAGES),
+                    [&](int j, uint64_t key) { keys[j] = key; });
+}
+// ... and the choice among them.
+__global__ __launch_bounds__(SELECT_NT) void select_kernel(SelectArgs a) {
+  __shared__ struct {
+    uint64_t keys[SELECT_KEYS];
+    SelectSmem<SELECT_NT> select;
+  } sm;
+  const int bh = blockIdx.x;
+  const SelectSeq seq = select_seq(a, bh / a.Hkv);
+  const uint64_t* keys = a.keys + (int64_t)bh * a.width;
+  const int* row = a.table + (int64_t)(bh / a.Hkv) * a.table_stride;
+  auto id_of = [&](int j) { return row[j]; };
+  if (seq.used <= SELECT_KEYS) {
+    for (int j = threadIdx.x; j < seq.used; j += SELECT_NT) sm.keys[j] = keys[j];
+    __syncthreads();
+    select_pages(a, sm.select, bh, seq, [&](int j) { return sm.keys[j]; }, id_of);
+  } else {
+    select_pages(a, sm.select, bh, seq, [&](int j) { return keys[j]; }, id_of);
+  }
+}
+
+// Whether one workgroup takes a sequence and KV head on its own.
+bool select_fused(const SelectArgs& a) {
+  return a.width <= SELECT_KEYS && (a.width <= 1024 || a.B * a.Hkv >= 256);
 }
 
 }  // namespace
@@ -287,12 +411,21 @@ hipError_t launch_summarize(const SummaryArgs& in, int D, hipStream_t st) {
 }
 
 hipError_t launch_select(const SelectArgs& a, int D, hipStream_t st) {
-  const dim3 grid((unsigned)a.B * a.Hkv * cdiv(a.width, SCORE_PAGES));
-  if (D == 128) hipLaunchKernelGGL(score_kernel<128>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(score_kernel<64>, grid, dim3(256), 0, st, a);
+  const unsigned items = (unsigned)a.B * a.Hkv;
+  if (select_fused(a)) {
+    const bool few = a.width <= 1024;
+    if (D == 128 && few) hipLaunchKernelGGL((choose_kernel<128, 1024>), dim3(items), dim3(CHOOSE_NT), 0, st, a);
+    else if (D == 128) hipLaunchKernelGGL((choose_kernel<128, SELECT_KEYS>), dim3(items), dim3(CHOOSE_NT), 0, st, a);
+    else if (few) hipLaunchKernelGGL((choose_kernel<64, 1024>), dim3(items), dim3(CHOOSE_NT), 0, st, a);
+    else hipLaunchKernelGGL((choose_kernel<64, SELECT_KEYS>), dim3(items), dim3(CHOOSE_NT), 0, st, a);
+    return hipGetLastError();
+  }
+  const dim3 grid(items * cdiv(a.width, SCORE_PAGES));
+  if (D == 128) hipLaunchKernelGGL(score_kernel<128>, grid, dim3(SCORE_NT), 0, st, a);
+  else hipLaunchKernelGGL(score_kernel<64>, grid, dim3(SCORE_NT), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(select_kernel, dim3((unsigned)a.B * a.Hkv), dim3(SELECT_NT), 0, st, a);
+  hipLaunchKernelGGL(select_kernel, dim3(items), dim3(SELECT_NT), 0, st, a);
   return hipGetLastError();
 }
 
