@@ -379,15 +379,17 @@ int paged_arrays(const PagedCall& c, const bd::DecodeShape& s, int rows, int Hkv
 
 // Validation of a decode call whose sequences share prefixes; fills the resolved shape.
 int validate_shared(int B, int groups, int S, int Hq, int Hkv, int D, int page_size, int max_prefix_pages, int max_pages,
-                    float scale, int dtype, bd::DecodeShape& s) {
-  const int st = validate_paged(B, S, Hq, Hkv, D, page_size, max_pages, scale, dtype, s);
+                    float scale, int dtype, bd::SharedShape& a) {
+  const int st = validate_paged(B, S, Hq, Hkv, D, page_size, max_pages, scale, dtype, a.s);
   if (st != BD_ATTN_OK) return st;
   const int lg = page_log(page_size);
   if (groups < 1 || groups > (1 << 16) || max_prefix_pages < 1 || (int64_t)max_prefix_pages << lg > (1 << 22))
     return BD_ATTN_ERR_INVALID_ARGUMENT;
   // the tiles of the prefixes are counted in int32, as those of the sequences' own keys
-  if (bd::shared_items(s, groups) * (size_t)bd::cdiv(max_prefix_pages << lg, bd::DEC_KT) > (size_t)INT32_MAX / 2)
-    return BD_ATTN_ERR_INVALID_ARGUMENT;
+  a.groups = groups;
+  a.C = max_prefix_pages << lg;
+  const int shared = bd::cdiv(a.C, bd::DEC_KT), own = bd::cdiv(a.s.C, bd::DEC_KT) + bd::cdiv(S, bd::DEC_KT);
+  if (bd::shared_items(a) > (size_t)INT32_MAX / 2 / (size_t)bd::imax(shared, own)) return BD_ATTN_ERR_INVALID_ARGUMENT;
   return BD_ATTN_OK;
 }
 // Validation of a decode call with a list of pages for each KV head; fills the shape
@@ -1038,9 +1040,9 @@ int bd_attn_paged_decode_fwd(const void* Q, const void* K_pages, const void* V_p
 
 size_t bd_attn_paged_shared_decode_workspace_bytes(int B, int groups, int S, int Hq, int Hkv, int D, int page_size,
                                                    int max_prefix_pages, int max_pages, int dtype) {
-  bd::DecodeShape s;
+  bd::SharedShape s;
   if (validate_shared(B, groups, S, Hq, Hkv, D, page_size, max_prefix_pages, max_pages, 0.f, dtype, s) != BD_ATTN_OK) return 0;
-  return bd::shared_workspace_bytes(s, groups);
+  return bd::shared_workspace_bytes(s);
 }
 
 int bd_attn_paged_shared_decode_fwd(const void* Q, const void* K_pages, const void* V_pages, const int32_t* group_sizes,
@@ -1051,7 +1053,7 @@ int bd_attn_paged_shared_decode_fwd(const void* Q, const void* K_pages, const vo
                                     int64_t table_stride, int64_t page_stride, int64_t head_stride, int64_t row_stride,
                                     float scale, int dtype, void* O, float* LSE, void* ws, size_t ws_bytes,
                                     hipStream_t stream) {
-  bd::DecodeShape s;
+  bd::SharedShape s;
   int st = validate_shared(B, groups, S, Hq, Hkv, D, page_size, max_prefix_pages, max_pages, scale, dtype, s);
   if (st != BD_ATTN_OK) return st;
   if (prefix_stride < 0 || (groups > 1 && prefix_stride != 0 && prefix_stride < max_prefix_pages))
@@ -1063,10 +1065,9 @@ int bd_attn_paged_shared_decode_fwd(const void* Q, const void* K_pages, const vo
   const PagedCall c{Q,           K_pages,    V_pages, page_table, cache_lens, K_new, V_new, num_pages, page_size, max_pages, table_stride,
                     page_stride, head_stride, row_stride, O, LSE, ws, ws_bytes};
   bd::SharedArgs a{};
-  st = paged_arrays(c, s, s.B, Hkv, bd::shared_workspace_bytes(s, groups), more, 3, a.own);
+  st = paged_arrays(c, s.s, s.s.B, Hkv, bd::shared_workspace_bytes(s), more, 3, a.own);
   if (st != BD_ATTN_OK) return st;
   a.sizes = group_sizes;
-  a.groups = groups;
   a.table = prefix_table;
   a.width = max_prefix_pages;
   a.table_stride = prefix_stride;

@@ -364,12 +364,6 @@ __device__ inline float tree_max(const float* v) {
     return fmaxf(tree_max<N / 2>(v), tree_max<N - N / 2>(v + N / 2));
   }
 }
-// Sum of N values (a power of two) as a balanced tree.
-template <int N>
-__device__ inline float tree_add(const float* v) {
-  if constexpr (N == 1) return v[0];
-  else return tree_add<N / 2>(v) + tree_add<N / 2>(v + N / 2);
-}
 // Sum of the 16 K entries of K accumulators as a balanced tree.
 template <int K>
 __device__ inline float tree_sum(const f32x16* a) {

@@ -365,39 +365,53 @@ hipError_t launch_sparse_decode(const DecodeShape& s, const PagedArgs& a, int he
 struct SharedArgs {
   PagedArgs own;
   const int* sizes;  // [groups]
-  int groups;
   const int* table;  // [groups][width], rows table_stride apart
   int width;
   int64_t table_stride;
   const int* lens;  // [groups]
 };
-// The prefix's items: a KV head's G * S rows of all members, in row groups of 32
-// rows for each wave of a team; a team as large as the average group needs.
-inline int shared_waves(const DecodeShape& s, int groups) {
-  const long long rows = ((long long)s.B * (s.Hq / s.Hkv) * s.S + groups - 1) / groups;
-  return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+struct SharedShape {
+  DecodeShape s;
+  int groups, C;  // keys of a prefix at most
+};
+// The prefix's items: a KV head's G * S rows of all members, in row groups of 32 rows for each
+// wave of a team.  Teams of one or two waves (the paged kernel) take the sequences' own keys as
+// items of the same launch (joint).  Four waves have a kernel of their own, which is faster at
+// the matrix products, and leave the own keys to a second launch.  They pay from about 10 million
+// pairs of a query row and a key of its prefix on; us (D = 128, 8 KV heads of 4) joint, apart:
+//   8 sequences of 4 queries on one prefix of 4096 keys 23.6 28.9; of 16384 42.9 38.2; of 65536 117 80;
+//   four groups of those, prefixes of 1024 25.3 30.8; of 2048 32.1 35.1; of 4096 46.9 41.8;
+//   8 sequences of 32 queries on one of 512 keys 24.3 32.7; of 2048 44.9 41.2.
+// (The prefix's length is known on the device only: the table's width bounds it.)
+// One wave or two, us: 32 rows a KV head, prefixes of 4000, four groups 29.2 32.7; 80 rows, three groups 23.0 20.8.
+inline bool shared_joint(const SharedShape& a) {
+  const long long rows = (long long)a.s.B * (a.s.Hq / a.s.Hkv) * a.s.S;
+  return rows <= 64ll * a.groups || rows * a.s.Hkv * a.C <= 1ll << 23;
 }
-// Teams that work on the prefixes, at most (four waves: two a CU, eight: one).
-inline int shared_runs(int waves) { return waves >= 4 ? 2 * DEC_WAVES / waves : DEC_WAVES / waves; }
-inline size_t shared_items(const DecodeShape& s, int groups) {
-  const size_t rows = (size_t)s.B * (s.Hq / s.Hkv) * s.S;
-  return (size_t)s.Hkv * (rows / (DEC_QT * shared_waves(s, groups)) + (groups < s.B ? groups : s.B));
+inline int shared_waves(const SharedShape& a) {
+  return (long long)a.s.B * (a.s.Hq / a.s.Hkv) * a.s.S <= 32ll * a.groups ? 1 : shared_joint(a) ? 2 : 4;
 }
-// Workspace: the sequences' own (decode_workspace_bytes), then for the prefixes a
-// descriptor for each item and a reference for each sequence, and the partial
-// results of every (team, item) run.
-inline size_t shared_desc_bytes(const DecodeShape& s, int groups) {
-  return ((shared_items(s, groups) + s.B + 1) * 16 + 255) & ~(size_t)255;
+// Teams that work on the prefixes, at most.
+inline int shared_runs(int waves) { return waves == 4 ? 2 * DEC_WAVES / waves : DEC_WAVES / waves; }
+inline size_t shared_items(const SharedShape& a) {
+  const size_t B = a.s.B, rows = (size_t)(a.s.Hq / a.s.Hkv) * a.s.S, per = DEC_QT * shared_waves(a);
+  const size_t own = shared_joint(a) ? B * ((rows + per - 1) / per) : 0;
+  return a.s.Hkv * (B * rows / per + (a.groups < a.s.B ? a.groups : a.s.B) + own);
 }
-inline size_t shared_part_bytes(const DecodeShape& s, int groups) {
-  const int waves = shared_waves(s, groups);
-  return (shared_runs(waves) + shared_items(s, groups)) * DEC_QT * waves * decode_part_stride(s.D) * 4;
+// Workspace: the sequences' own (decode_workspace_bytes), if apart, then a descriptor for each
+// item, a reference for each sequence and their count, and the partial results of every (team, item) run.
+inline size_t shared_desc_bytes(const SharedShape& a) {
+  return ((shared_items(a) + a.s.B + 1) * 16 + 255) & ~(size_t)255;
+}
+inline size_t shared_part_bytes(const SharedShape& a) {
+  const int waves = shared_waves(a);
+  return (shared_runs(waves) + shared_items(a)) * DEC_QT * waves * decode_part_stride(a.s.D) * 4;
 }
 inline size_t shared_own_bytes(const DecodeShape& s) { return (decode_workspace_bytes(s) + 255) & ~(size_t)255; }
-inline size_t shared_workspace_bytes(const DecodeShape& s, int groups) {
-  return shared_own_bytes(s) + shared_desc_bytes(s, groups) + shared_part_bytes(s, groups);
+inline size_t shared_workspace_bytes(const SharedShape& a) {
+  return (shared_joint(a) ? 0 : shared_own_bytes(a.s)) + shared_desc_bytes(a) + shared_part_bytes(a);
 }
-hipError_t launch_shared_decode(const DecodeShape& s, const SharedArgs& a, void* ws, hipStream_t st);
+hipError_t launch_shared_decode(const SharedShape& s, const SharedArgs& a, void* ws, hipStream_t st);
 
 // Smallest and largest keys of the pages that hold positions from[b] to lens[b].
 struct SummaryArgs {

@@ -30,10 +30,10 @@ struct PagedTile {
 //           (DecodeShape with B * Hkv sequences, G query heads and one KV head);
 //   Own     as Plain, of sequences that also have a prefix: every item leaves a
 //           partial result, which a kernel of its own joins with the prefix's;
-//   Prefix  the keys that the sequences of a group share: the query rows of a KV head
-//           are those of all members, G * S each, in row groups of grows.  Items
-//           leave partial results.
-enum class PagedMode { Plain, Lists, Own, Prefix };
+//   Joint   the sequences' own keys; then, behind the sequences, the keys that those of
+//           each group share, the query rows of a KV head being those of all members,
+//           G * S each, in row groups of grows.  Items leave partial results.
+enum class PagedMode { Plain, Lists, Own, Joint };
 
 struct PagedParams {
   DecParams d;  // C: the table's room in keys
@@ -41,11 +41,18 @@ struct PagedParams {
   int Sn;  // the block's own keys (0: none)
   // Lists: KV heads of the pages
   int heads;
-  // Prefix: members of each group (d.B groups), sequences in all, and the results for the merge
+  // Prefixes (d.B, d.C, d.cache_lens and t's table are theirs): members of each group, sequences in all
   const int* sizes;
   int seqs;
-  SharedRef* refs;
-  int* members;
+  SharedRef* refs;  // [seqs], for the merge
+  int* members;     // the sequences that are in a group
+  // Joint: the sequences' own keys, in a table of own.width entries a row
+  struct {
+    uint64_t table;
+    int64_t table_stride;
+    int last, C;
+    const int* lens;
+  } own;
 };
 
 // Key tiles of an item of a sequence with cache length len.
@@ -100,37 +107,60 @@ __device__ inline int paged_run_start(int gw, int n, int T) {
 struct PagedPos {
   int b, len, nt, h, g, j;
 };
-// Prefix: also the group's row groups, first member and members, and the row groups of
-// the groups before it.
+// Prefixes: also the group's row groups, first member and members, the members of all
+// groups up to it, and the row groups before it; tiles of cached keys, the entry's row of its
+// table and the last entry of that.
 struct PrefixPos : PagedPos {
-  int ng, first, n, row;
+  int ng, first, n, upto, row, ntc, last;
+  uint64_t table;
 };
 
-// The tiles of all prefixes in order of (group, KV head, row group): how many there
-// are, where a run starts, and what follows a tile.  NW waves scan the groups.
-template <int KT, int TW, int NW, int TEAMS>
+// The tiles of all prefixes in order of (group, KV head, row group), JOINT: behind those of the
+// sequences' own keys: how many there are, where a run starts, and what follows a tile.
+// Entry b of the list is group b, JOINT: sequence b or, from seqs on, group b - seqs.  NW waves scan it.
+template <int KT, int TW, int NW, int TEAMS, bool JOINT>
 struct PrefixWork {
   struct Smem {
     int wmem[NW], wrow[NW], wsum[NW];  // per-wave sums: members, row groups, tiles of a KV head
-    int b[TEAMS], off[TEAMS], first[TEAMS], n[TEAMS], row[TEAMS];  // where each team's run starts
+    int b[TEAMS], off[TEAMS], first[TEAMS], n[TEAMS], upto[TEAMS], row[TEAMS];  // where each team's run starts
   };
   const PagedParams& p;
-  const int* __restrict__ lens;
-  int c0, c1, before_members, before_rows, before_tiles, tiles;  // this thread's groups, what lies before them, their tiles
+  int c0, c1, before_members, before_rows, before_tiles, tiles;  // this thread's entries, what lies before them, their tiles
 
-  // Members of group b, whose first is sequence `first` (sizes that pass the sequences end there).
-  __device__ int members(int b, int first) const { return imin(imax(p.sizes[b], 0), p.seqs - first); }
+  typedef const __attribute__((address_space(4))) int* Uniform;  // (scalar loads: nothing writes these arrays meanwhile)
+  __device__ int own() const { return JOINT ? p.seqs : 0; }      // entries ahead of the groups
+  __device__ int entries() const { return own() + p.d.B; }
   __device__ int row_groups(int n) const { return tiles_of<32 * TW>(n * p.d.G * p.d.S); }
-  __device__ int tiles_at(int b) const { return imax(tiles_of<KT>(dec_len(p.d, lens, b)), 1); }
+  // Members and first member of entry b, where the groups before it have `upto`, which it
+  // adds to (sizes that pass the sequences end there); its keys; its tiles of a KV head and row group.
+  template <class Ints>
+  __device__ void members(int b, int& first, int& n, int& upto) const {
+    if (JOINT && b < p.seqs) {
+      first = b;
+      n = 1;
+    } else {
+      first = upto;
+      n = imin(imax(((Ints)(uintptr_t)p.sizes)[b - own()], 0), p.seqs - upto);
+      upto += n;
+    }
+  }
+  template <class Ints>
+  __device__ int keys(int b) const {
+    if (JOINT && b < p.seqs) return imin(imax(((Ints)(uintptr_t)p.own.lens)[b], 0), p.own.C);
+    return imin(imax(((Ints)(uintptr_t)p.d.cache_lens)[b - own()], 0), p.d.C);
+  }
+  __device__ int tiles_at(int b, int len) const {
+    return imax(tiles_of<KT>(len) + (JOINT && b < p.seqs ? tiles_of<KT>(p.Sn) : 0), 1);
+  }
 
-  // Tiles of a KV head in all groups; the first workgroup notes the sequences that are in one.
+  // Tiles of a KV head in all entries; the first workgroup notes what the merge needs.
   __device__ int scan(Smem& sm, int tid) {
     const int lane = tid & 63, w = tid >> 6;
-    const int cpt = cdiv(p.d.B, 64 * NW);
-    c0 = imin(p.d.B, tid * cpt);
-    c1 = imin(p.d.B, c0 + cpt);
+    const int cpt = cdiv(entries(), 64 * NW);
+    c0 = imin(entries(), tid * cpt);
+    c1 = imin(entries(), c0 + cpt);
     int mem = 0;
-    for (int b = c0; b < c1; ++b) mem += members(b, mem);
+    for (int b = imax(c0, own()); b < c1; ++b) mem += imin(imax(p.sizes[b - own()], 0), p.seqs - mem);
     int imem = mem;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -149,11 +179,12 @@ struct PrefixWork {
     if (blockIdx.x == 0 && tid == 0) *p.members = all;
     int rows = 0;
     tiles = 0;
-    for (int b = c0, first = before_members; b < c1; ++b) {
-      const int n = members(b, first), r = row_groups(n);
-      first += n;
+    for (int b = c0, upto = before_members; b < c1; ++b) {
+      int first, n;
+      members<const int*>(b, first, n, upto);
+      const int r = row_groups(n);
       rows += r;
-      tiles += tiles_at(b) * r;
+      tiles += tiles_at(b, keys<const int*>(b)) * r;
     }
     int irow = rows, itile = tiles;
 #pragma unroll
@@ -183,21 +214,33 @@ struct PrefixWork {
   __device__ void find(Smem& sm, int v, int x0) const {
     const int I = p.d.Hkv;
     if (tiles == 0 || x0 < before_tiles * I || x0 >= (before_tiles + tiles) * I) return;
-    int pb = before_tiles, first = before_members, row = before_rows;
+    int pb = before_tiles, upto = before_members, row = before_rows;
     for (int b = c0; b < c1; ++b) {
-      const int n = members(b, first), r = row_groups(n), t = tiles_at(b) * r;
+      int first, n;
+      members<const int*>(b, first, n, upto);
+      const int r = row_groups(n), t = tiles_at(b, keys<const int*>(b)) * r;
       if (x0 < (pb + t) * I) {
         sm.b[v] = b;
         sm.off[v] = x0 - pb * I;
         sm.first[v] = first;
         sm.n[v] = n;
+        sm.upto[v] = upto;
         sm.row[v] = row;
         return;
       }
       pb += t;
-      first += n;
       row += r;
     }
+  }
+  // What q holds of its entry q.b, of q.n members.
+  __device__ void enter(PrefixPos& q) const {
+    const bool mine = JOINT && q.b < p.seqs;  // a sequence's own keys
+    q.len = keys<Uniform>(q.b);
+    q.nt = tiles_at(q.b, q.len);
+    q.ntc = mine ? tiles_of<KT>(q.len) : q.nt;
+    q.ng = row_groups(q.n);
+    q.last = mine ? p.own.last : p.t.last;
+    q.table = mine ? p.own.table + (int64_t)q.b * p.own.table_stride : p.t.table + (int64_t)(q.b - own()) * p.t.table_stride;
   }
   __device__ PrefixPos start(const Smem& sm, int v) const {
     PrefixPos q;
@@ -205,10 +248,9 @@ struct PrefixWork {
     const int off = __builtin_amdgcn_readfirstlane(sm.off[v]);
     q.first = __builtin_amdgcn_readfirstlane(sm.first[v]);
     q.n = __builtin_amdgcn_readfirstlane(sm.n[v]);
+    q.upto = __builtin_amdgcn_readfirstlane(sm.upto[v]);
     q.row = __builtin_amdgcn_readfirstlane(sm.row[v]);
-    q.len = __builtin_amdgcn_readfirstlane(dec_len(p.d, lens, q.b));
-    q.nt = imax(tiles_of<KT>(q.len), 1);
-    q.ng = row_groups(q.n);
+    enter(q);
     const int item = off / q.nt;
     q.j = off - item * q.nt;
     q.h = item / q.ng;
@@ -222,20 +264,15 @@ struct PrefixWork {
     q.g = 0;
     if (++q.h < p.d.Hkv) return;
     q.h = 0;
-    // (scalar loads: nothing writes these arrays while the kernel runs)
-    typedef const __attribute__((address_space(4))) int* Uniform;
-    const Uniform sizes = (Uniform)(uintptr_t)p.sizes, all = (Uniform)(uintptr_t)p.d.cache_lens;
     do {  // (to the next group that has members)
-      q.first += q.n;
       q.row += q.ng;
-      if (++q.b >= p.d.B) return;
-      q.n = imin(imax(sizes[q.b], 0), p.seqs - q.first);
+      if (++q.b >= entries()) return;
+      members<Uniform>(q.b, q.first, q.n, q.upto);
       q.ng = row_groups(q.n);
     } while (q.n == 0);
-    q.len = imin(imax(all[q.b], 0), p.d.C);
-    q.nt = imax(tiles_of<KT>(q.len), 1);
+    enter(q);
   }
-  // Query row R of the group's rows of a KV head (rows past the last: the last).
+  // Query row R of the entry's rows of a KV head (rows past the last: the last).
   __device__ __attribute__((always_inline)) size_t query_row(const DecParams& a, const PrefixPos& q, int R, bool& valid) const {
     const unsigned rows = (unsigned)(a.G * a.S);  // of a member
     valid = R < q.n * (int)rows;
@@ -252,19 +289,19 @@ struct PagedSmem {
   alignas(256) char buf[TEAMS][NST * 2 * TILE];  // per team: a ring of K and V tiles
   int wsum[NW];                                  // prologue: per-wave sums of the scan
   int start_b[TEAMS], start_off[TEAMS];          // where each team's run starts
-  using Work = PrefixWork<KT, TW, NW, TEAMS>;
+  using Work = PrefixWork<KT, TW, NW, TEAMS, true>;
   // (in here: with a second object the compiler tells their accesses apart in a way that has it wait for all copies in
   // flight before the next read of a tile)
-  std::conditional_t<MODE == PagedMode::Prefix, typename Work::Smem, Nothing> work;
+  std::conditional_t<MODE == PagedMode::Joint, typename Work::Smem, Nothing> work;
 };
 
 // `lens` is the parameters' array as a restrict kernel argument, read through the
 // scalar cache where the index is uniform.
 template <int D, int TW, int KT, int NST, PagedMode MODE>
 __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(PagedParams p, const int* __restrict__ lens) {
-  constexpr bool LISTS = MODE == PagedMode::Lists, PREFIX = MODE == PagedMode::Prefix;
-  constexpr bool PARTS = MODE == PagedMode::Own || PREFIX;  // every item leaves partial results
-  using Pos = std::conditional_t<PREFIX, PrefixPos, PagedPos>;
+  constexpr bool LISTS = MODE == PagedMode::Lists, JOINT = MODE == PagedMode::Joint;
+  constexpr bool PARTS = MODE == PagedMode::Own || JOINT;  // every item leaves partial results
+  using Pos = std::conditional_t<JOINT, PrefixPos, PagedPos>;
   constexpr int DS = D / 16, DB = D / 32, PST = D + 4, KB = KT / 32;
   using Smem = PagedSmem<D, TW, KT, NST, MODE>;
   constexpr int TEAMS = Smem::TEAMS, NW = Smem::NW, NT = 64 * NW;
@@ -276,15 +313,15 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, g2 = lane >> 5;
   const int tm = TW == 1 ? w : 0, tw = TW == 1 ? 0 : w;  // team of the workgroup, wave of the team
-  const int ng = TW < 4 || PREFIX ? 1 : p.d.ng;          // (decode_groups: smaller teams hold all rows of a KV head)
-  const int I = p.d.Hkv * ng;                            // items per sequence (Prefix: and row group)
-  typename Smem::Work work{p, lens};
+  const int ng = TW < 4 || JOINT ? 1 : p.d.ng;          // (decode_groups: smaller teams hold all rows of a KV head)
+  const int I = p.d.Hkv * ng;                            // items per sequence (Joint: and row group)
+  typename Smem::Work work{p};
   // ---- prologue: T, and the position of each team's first tile (as over a dense cache) ----
   const int cpt = cdiv(p.d.B, NT);
   const int c0 = imin(p.d.B, tid * cpt), c1 = imin(p.d.B, c0 + cpt);
   int csum = 0;
 #pragma unroll 4
-  for (int b = c0; b < c1; ++b) csum += PREFIX ? 0 : paged_tiles<KT>(p, dec_len(p.d, lens, b));
+  for (int b = c0; b < c1; ++b) csum += JOINT ? 0 : paged_tiles<KT>(p, dec_len(p.d, lens, b));
   int incl = csum;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -302,7 +339,7 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
   }
   const int excl = before + incl - csum;  // tiles per item of the sequences before c0
   total = __builtin_amdgcn_readfirstlane(total);
-  if constexpr (PREFIX) total = work.scan(sm.work, tid);
+  if constexpr (JOINT) total = work.scan(sm.work, tid);
   const int T = total * I;  // checked on the host to fit in 31 bits
   const int n = paged_runs<D, TW, PARTS>(T, p.d.B * I);
   const bool stream = total * p.d.Hkv > (int)(DEC_STREAM_BYTES / (2 * Smem::TILE));
@@ -310,7 +347,7 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
 #pragma unroll
   for (int v = 0; v < TEAMS; ++v) {
     const int x0 = run_of(v) < n ? paged_run_start(run_of(v), n, T) : T;
-    if constexpr (PREFIX) work.find(sm.work, v, x0);
+    if constexpr (JOINT) work.find(sm.work, v, x0);
     else if (csum > 0 && excl * I <= x0 && x0 < (excl + csum) * I) {
       int pb = excl;
       for (int b = c0; b < c1; ++b) {
@@ -331,7 +368,7 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
   if (gw >= n) return;
   const int x0 = paged_run_start(gw, n, T), x1 = paged_run_start(gw + 1, n, T);
   Pos pc;
-  if constexpr (PREFIX) {
+  if constexpr (JOINT) {
     pc = work.start(sm.work, tm);
   } else {
     pc.b = __builtin_amdgcn_readfirstlane(sm.start_b[tm]);
@@ -347,7 +384,7 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
   auto advance = [&](Pos q) __attribute__((always_inline)) {
     if (++q.j == q.nt) {
       q.j = 0;
-      if constexpr (PREFIX) {
+      if constexpr (JOINT) {
         work.next_item(q);
       } else if constexpr (LISTS) {
         if (++q.g == ng) {
@@ -371,6 +408,10 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
     }
     return q;
   };
+  auto cached_tiles = [&](const Pos& q) __attribute__((always_inline)) {
+    if constexpr (JOINT) return q.ntc;
+    else return tiles_of<KT>(q.len);
+  };
   // The kernel's arguments, read again (those needed once per item would take
   // scalar registers from the tile loop).
   auto arguments = [&]() __attribute__((always_inline)) -> DecParams {
@@ -391,7 +432,7 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
   // its column is computed like the others and never stored.
   auto query_row = [&](const DecParams& p, Pos q, bool& valid) __attribute__((always_inline)) -> size_t {
     const int rl = 32 * tw + l32, R = q.g * p.grows + rl;
-    if constexpr (PREFIX) {
+    if constexpr (JOINT) {
       return work.query_row(p, q, R, valid);
     } else {
       valid = R < p.G * p.S && (TW == 1 || rl < p.grows);
@@ -435,8 +476,17 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
   auto load_pages = [&](const PagedTile& t, Pos q) __attribute__((always_inline)) {
     Pages g;
     // (constant address space: scalar loads; nothing writes the table while the kernel runs)
-    auto* row = (const __attribute__((address_space(4))) int*)(t.table + (int64_t)imin(q.b, p.d.B - 1) * t.table_stride);
-    auto entry = [&](int piece) { return row[(uint32_t)imin((q.j * KT + 16 * piece) >> t.log_size, t.last)]; };
+    uint64_t at;
+    int last;
+    if constexpr (JOINT) {
+      at = q.table;
+      last = q.last;
+    } else {
+      at = t.table + (int64_t)imin(q.b, p.d.B - 1) * t.table_stride;
+      last = t.last;
+    }
+    auto* row = (const __attribute__((address_space(4))) int*)at;
+    auto entry = [&](int piece) { return row[(uint32_t)imin((q.j * KT + 16 * piece) >> t.log_size, last)]; };
     if ((1 << t.log_size) >= KT) {  // the tile lies in one page
       const int id = entry(0);
 #pragma unroll
@@ -455,8 +505,8 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
   // returns which pieces of the tile may hold keys (bit i: rows 16 i ...).
   auto issue = [&](const PagedTile& t, Pos q, const Pages& g, char* dst, auto streamed) __attribute__((always_inline)) {
     constexpr int POLICY = decltype(streamed)::value ? COPY_STREAM : 0;
-    const int ntc = tiles_of<KT>(q.len);
-    const bool cached = PREFIX || q.j < ntc;
+    const int ntc = cached_tiles(q);
+    const bool cached = q.j < ntc;
     const int row0 = (cached ? q.j : q.j - ntc) * KT, end = cached ? q.len : p.Sn;
     const uint32_t row_bytes = cached ? t.sr : D * 2;
     uint64_t base[PPW], kp, vp;
@@ -482,7 +532,9 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
     } else {
       kp = t.kn;
       vp = t.vn;
-      const uint32_t bh = LISTS ? (uint32_t)q.b : (uint32_t)q.b * (uint32_t)p.d.Hkv + (uint32_t)q.h;
+      uint32_t bh;
+      if constexpr (JOINT) bh = (uint32_t)q.first * (uint32_t)p.d.Hkv + (uint32_t)q.h;
+      else bh = LISTS ? (uint32_t)q.b : (uint32_t)q.b * (uint32_t)p.d.Hkv + (uint32_t)q.h;
       const uint64_t block = ((uint64_t)bh * (uint32_t)p.Sn + row0) * (D * 2);
 #pragma unroll
       for (int i = 0; i < PPW; ++i) base[i] = block + 16 * (tw + i * TW) * (D * 2);
@@ -547,11 +599,12 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
 
     // Write out the state of the current item's segment, which ends at tile pc.j
     // (tile x of all).
-    SharedRef* const refs = PREFIX ? p.refs : nullptr;
+    SharedRef* const refs = JOINT ? p.refs : nullptr;
+    const int seqs = JOINT ? p.seqs : 0;
     auto flush = [&](int x) __attribute__((always_inline)) {
       const DecParams p = arguments();
       int item;
-      if constexpr (PREFIX) item = pc.row * p.Hkv + pc.h * pc.ng + pc.g;
+      if constexpr (JOINT) item = pc.row * p.Hkv + pc.h * pc.ng + pc.g;
       else if constexpr (LISTS) item = pc.b * I + pc.g;
       else item = pc.b * I + pc.h * ng + pc.g;
       const int item_start = x - pc.j;  // flat index of the item's first tile
@@ -580,7 +633,7 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
         // Teams leave [D / 4][32] float4 for each wave's rows, a contiguous KiB a store (rows of D + 4 floats: 32
         // bytes of each row); one wave, with few rows, leaves rows, which the merge reads faster.
         size_t slot;
-        if constexpr (PREFIX) slot = (size_t)(gw + item) * p.grows;
+        if constexpr (JOINT) slot = (size_t)(gw + item) * p.grows;
         else if constexpr (LISTS) slot = dec_slot_row(p, gw, pc.b, pc.g);
         else slot = dec_slot_row(p, gw, (size_t)pc.b * p.Hkv + pc.h, pc.g);
         float* pr = p.part + (slot + 32 * tw + (TW == 1 ? l32 : 0)) * PST;
@@ -599,10 +652,10 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
         const int first = PARTS && item_start >= x0 ? gw : (int)((((long long)item_start + 1) * n - 1) / T);
         p.desc[item] = DecRuns{first, gw};
       }
-      if constexpr (PREFIX) {
+      if constexpr (JOINT) {
         // the first row of each member, once for all KV heads
         const int rows = p.G * p.S, R = pc.g * p.grows + 32 * tw + l32;
-        if (ends && pc.h == 0 && g2 == 0 && valid && R % rows == 0)
+        if (ends && pc.b >= seqs && pc.h == 0 && g2 == 0 && valid && R % rows == 0)
           refs[pc.first + R / rows] = SharedRef{pc.row * p.Hkv, pc.ng, R};
       }
     };
@@ -651,7 +704,7 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
       for (int i = 0; i < NP; ++i) asm volatile("" : "+s"(ga.id[i]));
 #pragma unroll
       for (int i = 0; i < PPW; ++i) asm volatile("" : "+s"(ga.own[i]));
-      const int ntc = tiles_of<KT>(pc.len);
+      const int ntc = cached_tiles(pc);
       const int nvalid = pc.j < ntc ? pc.len - pc.j * KT : p.Sn - (pc.j - ntc) * KT;  // keys before the end
       const uint32_t here = pieces & ((1u << NP) - 1);
       pieces >>= NP;
@@ -664,10 +717,24 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int e = 0; e < 16; ++e) sacc[kb][e] = 0.f;
+      if constexpr (JOINT) {
+        // (in the order of the text too: with this mode's scalars the scheduler falls back to that in one of the two copies)
+        constexpr int N = DS * KB, AHEAD = 4;
+        bf16x8 k[AHEAD];
 #pragma unroll
-      for (int s = 0; s < DS; ++s)
+        for (int i = 0; i < AHEAD; ++i) k[i] = lds_rows<D>(cur, ops.row_rel, i / KB, i % KB);
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) sacc[kb] = mfma32(lds_rows<D>(cur, ops.row_rel, s, kb), qreg.v[s], sacc[kb]);
+        for (int i = 0; i < N; ++i) {
+          const bf16x8 now = k[i % AHEAD];
+          if (i + AHEAD < N) k[i % AHEAD] = lds_rows<D>(cur, ops.row_rel, (i + AHEAD) / KB, (i + AHEAD) % KB);
+          sacc[i % KB] = mfma32(now, qreg.v[i / KB], sacc[i % KB]);
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < DS; ++s)
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb) sacc[kb] = mfma32(lds_rows<D>(cur, ops.row_rel, s, kb), qreg.v[s], sacc[kb]);
+      }
       pipeline_lds_reads<DS * KB, 4, 1>();  // operand reads four MFMAs ahead
       if (nvalid < KT || here != (1u << NP) - 1) {
 #pragma unroll
@@ -711,14 +778,28 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
       for (int c = 0; c < 2 * KB; ++c)
 #pragma unroll
         for (int e = 0; e < 8; ++e) pl[c][e] = (bf16)(sacc[c / 2][8 * (c & 1) + e] - (float)pb[c][e]);
+      if constexpr (JOINT) {
+        constexpr int N = 2 * KB * DB, AHEAD = 3;
+        bf16x8 v[AHEAD];
 #pragma unroll
-      for (int c = 0; c < 2 * KB; ++c)
+        for (int i = 0; i < AHEAD; ++i) v[i] = lds_tr<D>(cur + Smem::TILE, ops.tr_rel0, ops.tr_rel1, i / DB, i % DB);
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const bf16x8 v = lds_tr<D>(cur + Smem::TILE, ops.tr_rel0, ops.tr_rel1, c, db);
-          oacc[db] = mfma32(v, pb[c], oacc[db]);
-          oacc[db] = mfma32(v, pl[c], oacc[db]);
+        for (int i = 0; i < N; ++i) {
+          const bf16x8 now = v[i % AHEAD];
+          if (i + AHEAD < N) v[i % AHEAD] = lds_tr<D>(cur + Smem::TILE, ops.tr_rel0, ops.tr_rel1, (i + AHEAD) / DB, (i + AHEAD) % DB);
+          oacc[i % DB] = mfma32(now, pb[i / DB], oacc[i % DB]);
+          oacc[i % DB] = mfma32(now, pl[i / DB], oacc[i % DB]);
         }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 2 * KB; ++c)
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            const bf16x8 v = lds_tr<D>(cur + Smem::TILE, ops.tr_rel0, ops.tr_rel1, c, db);
+            oacc[db] = mfma32(v, pb[c], oacc[db]);
+            oacc[db] = mfma32(v, pl[c], oacc[db]);
+          }
+      }
       pipeline_lds_reads<4 * KB * DB, 6, 1>();
     };
 
@@ -790,7 +871,7 @@ template <int D, PagedMode MODE>
 hipError_t launch_paged_runs(const DecodeGroups& g, const PagedParams& p, hipStream_t st) {
   if (g.waves == 1) launch_paged_kernel<D, 1, 32, 2, MODE>(p, st);
   else if (g.waves == 2) launch_paged_kernel<D, 2, (D == 64 ? 64 : 32), 4, MODE>(p, st);
-  else if constexpr (MODE != PagedMode::Prefix) launch_paged_kernel<D, 4, 64, 512 / D, MODE>(p, st);
+  else if constexpr (MODE != PagedMode::Joint) launch_paged_kernel<D, 4, 64, 512 / D, MODE>(p, st);
   return hipGetLastError();
 }
 

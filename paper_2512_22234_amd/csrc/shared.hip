@@ -7,10 +7,10 @@
 // sum and unnormalised output over a part,
 //   M = max_i m_i,  O = sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i.
 // So the prefix is taken once for the n G S query rows that all members have for
-// a KV head, and its K and V are read once a group instead of once a sequence
-// (more than 32 TW rows: once for each TW waves, which run at about the same time).  One launch
-// does the prefixes, one the sequences' own keys, both by the paged kernel
-// (paged.hpp), and a third joins the partial results of both.
+// a KV head, in groups of rows that run at about the same time and read its K and V
+// from HBM once.  Few rows, or short prefixes (kernels.hpp): prefixes and own keys
+// are items of one launch of the paged kernel (paged.hpp, Joint).  Else one launch
+// does the prefixes, here, and one the own keys.  A last one joins the partial results.
 #include "paged.hpp"
 
 namespace bd {
@@ -18,24 +18,23 @@ namespace {
 
 // ---- prefixes with many query rows ----
 //
-// With more than 64 rows a row group the matrix products bound a prefix (512 bytes of K
-// and V a key for 4 D flops a row, at D = 128 256 rows for each byte per cycle and CU that HBM gives), so this kernel
-// differs from the paged one in what its tile loop spends beside them: a wave copies
-// one 16-row piece of K or of V a tile (TW = 8), page ids come one tile ahead of the
-// copies with the wait of the copies over them, and tiles without absent or missing
-// keys, nearly all, take no test a key.
-//   TW = 8: 256 rows, one workgroup a CU, two waves a SIMD.  Waves 4 to 7 (LAG) take the product with V
-//   of a tile after the scores of their partners' next one, so that the two waves of a SIMD are
-//   not at the same products and exponentials at the same time.
-//   TW = 4: 128 rows, two workgroups a CU.
-template <int D, int TW>
+// The matrix products bound a prefix with many rows: a key's 512 bytes of K and V (D = 128) go
+// with 6 D flops a row, P being two bfloat16 parts.  What the tile loop spends beside them is kept
+// small: a workgroup takes 128 rows, and a wave copies one 16-row piece of K and of V a tile;
+// page ids come a tile ahead of the copies, by scalar loads that are waited for under the softmax;
+// tiles without absent or missing keys, nearly all, take no test a key.  Two workgroups share
+// a CU, so that one is at its products while the other is at its exponentials.
+//   24 sequences of 32 rows and 4 query heads a KV head on prefixes of 8000 keys (D = 128): 167 us a call, 534 TFLOP/s
+//   of the two products as they are defined (800 executed).
+// Measured against it: 256 rows a workgroup of eight waves, half of them a product behind the
+// others, 167 us there and 5% to 2% either way elsewhere.
+constexpr int PREFIX_WAVES = 4, PREFIX_WORKGROUPS = 2;  // of a workgroup; a CU
+template <int D>
 struct PrefixShape {
   static constexpr int KT = 64, NP = KT / 16;
-  static constexpr bool PAIRS = TW == 8;                     // a wave copies a piece of K or of V, else of both
-  static constexpr int NST = PAIRS || D == 64 ? 4 : 2;       // tiles in the ring
-  static constexpr int AHEAD = PAIRS ? NST - 2 : NST - 1;    // copies run this many tiles ahead
+  static constexpr int NST = D == 64 ? 4 : 2;  // tiles in the ring
+  static constexpr int AHEAD = NST - 1;        // copies run this many tiles ahead
   static constexpr uint32_t TILE = KT * D * 2;
-  static constexpr int WORKGROUPS = 8 / TW;                  // a CU
 };
 // Scalars that stay in registers (and are not read again where they are needed).
 template <class A, class B>
@@ -52,23 +51,23 @@ __device__ inline void opaque(int& a) { asm volatile("" : "+v"(a)); }
 
 // (One object: with two, the compiler tells their accesses apart in a way that has it
 // wait for all copies in flight before the next read of a tile.)
-template <int D, int TW>
+template <int D>
 struct PrefixSmem {
-  using Shape = PrefixShape<D, TW>;
+  using Shape = PrefixShape<D>;
   alignas(256) char buf[Shape::NST * 2 * Shape::TILE];  // K and V tiles
-  typename PrefixWork<Shape::KT, TW, TW, 1>::Smem work;
+  typename PrefixWork<Shape::KT, PREFIX_WAVES, PREFIX_WAVES, 1, false>::Smem work;
 };
 
-template <int D, int TW>
-__global__ __launch_bounds__(64 * TW, 2) void prefix_kernel(PagedParams p, const int* __restrict__ lens) {
-  using Shape = PrefixShape<D, TW>;
-  constexpr int KT = Shape::KT, NP = Shape::NP, NST = Shape::NST, AHEAD = Shape::AHEAD, ROWS = 32 * TW;
+template <int D>
+__global__ __launch_bounds__(64 * PREFIX_WAVES, PREFIX_WORKGROUPS) void prefix_kernel(PagedParams p) {
+  using Shape = PrefixShape<D>;
+  constexpr int TW = PREFIX_WAVES, KT = Shape::KT, NP = Shape::NP, NST = Shape::NST, AHEAD = Shape::AHEAD, ROWS = 32 * TW;
   constexpr int DS = D / 16, DB = D / 32, PST = D + 4, KB = KT / 32;
   constexpr uint32_t TILE = Shape::TILE;
   constexpr int RPI = 512 / D, CPR = D / 8, UPP = 16 / RPI;  // rows of an instruction, 16-byte chunks of a row, instructions of a piece
-  constexpr int COPIES = Shape::PAIRS ? UPP : 2 * UPP;       // instructions of a wave and tile
-  using Work = PrefixWork<KT, TW, TW, 1>;
-  __shared__ PrefixSmem<D, TW> sm;
+  constexpr int COPIES = 2 * UPP;                            // instructions of a wave and tile
+  using Work = PrefixWork<KT, TW, TW, 1, false>;
+  __shared__ PrefixSmem<D> sm;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int tw = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -80,9 +79,9 @@ __global__ __launch_bounds__(64 * TW, 2) void prefix_kernel(PagedParams p, const
     asm volatile("" : "+s"(a));
     return *(const PagedParams*)a;
   };
-  Work work{p, lens};
+  Work work{p};
   const int T = work.scan(sm.work, tid) * p.d.Hkv;  // checked on the host to fit in 31 bits
-  const int n = imin(256 * Shape::WORKGROUPS, cdiv(T, 2));  // runs (two tiles at least, as dec_runs)
+  const int n = imin(256 * PREFIX_WORKGROUPS, cdiv(T, 2));  // runs (two tiles at least, as dec_runs)
   const int gw = blockIdx.x;
   if (gw >= n) return;
   const int x0 = paged_run_start(gw, n, T), x1 = paged_run_start(gw + 1, n, T);
@@ -92,7 +91,8 @@ __global__ __launch_bounds__(64 * TW, 2) void prefix_kernel(PagedParams p, const
   const LdsOperands<D> ops(lane);
 
   // ---- copies ----
-  const int piece = tw & (NP - 1);
+  static_assert(NP == TW, "a wave copies one 16-row piece of K and of V");
+  const int piece = tw;
   // What the tile loop needs of the arguments, in registers of its own.
   uint32_t sp = p.t.sp, sr = p.t.sr;
   int num = p.t.num, log_size = p.t.log_size, last_entry = p.t.last;
@@ -106,12 +106,12 @@ __global__ __launch_bounds__(64 * TW, 2) void prefix_kernel(PagedParams p, const
     const int row = u * RPI + lane / CPR;
     coff[u] = row * (int)sr + 16 * ((lane % CPR) ^ chunk_swizzle<D>(row));
   }
-  // Of the item at pa: the arrays at its KV head (PAIRS: the one this wave copies from), its row of the table.
+  // Of the item at pa: the arrays at its KV head, its row of the table.
   uint64_t k_head, v_head, table_row;
   auto copy_item = [&]() __attribute__((always_inline)) {
     const PagedParams a = arguments();
     const uint64_t head = (uint64_t)pa.h * (uint64_t)a.t.sh;
-    k_head = (Shape::PAIRS && tw >= NP ? a.t.vp : a.t.kp) + head;
+    k_head = a.t.kp + head;
     v_head = a.t.vp + head;
     table_row = a.t.table + (int64_t)imin(pa.b, a.d.B - 1) * a.t.table_stride;
   };
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(64 * TW, 2) void prefix_kernel(PagedParams p, const
   };
   auto next_item = [&](PrefixPos& q) __attribute__((always_inline)) {
     const PagedParams a = arguments();
-    Work{a, a.d.cache_lens}.next_item(q);
+    Work{a}.next_item(q);
   };
   int next = 0;           // ring slot of the next copy
   uint32_t present = 0;  // pieces of the tiles in flight that have a page, NP bits each, the next tile's lowest
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(64 * TW, 2) void prefix_kernel(PagedParams p, const
     // (products of 32 bits: the limits of the paged calls)
     const uint64_t off = (uint64_t)(ok ? (uint32_t)pages.own : 0u) * sp + r * sr;
     k_rows = uniform(k_head + off);
-    if constexpr (!Shape::PAIRS) v_rows = uniform(v_head + off);
+    v_rows = uniform(v_head + off);
     row_bytes = __builtin_amdgcn_readfirstlane((uint32_t)left * sr);
     next = next + 1 == NST ? 0 : next + 1;
     if (some && ++pa.j == pa.nt) {
@@ -170,9 +170,9 @@ __global__ __launch_bounds__(64 * TW, 2) void prefix_kernel(PagedParams p, const
   };
   // Instruction u of it, into the slot at dst.
   auto copy = [&](char* dst, int u) __attribute__((always_inline)) {
-    const bool value = Shape::PAIRS ? tw >= NP : u >= UPP;
+    const bool value = u >= UPP;
     const int i = u % UPP;
-    const __amdgpu_buffer_rsrc_t rs = make_buffer((const void*)(uintptr_t)(!Shape::PAIRS && u >= UPP ? v_rows : k_rows), row_bytes);
+    const __amdgpu_buffer_rsrc_t rs = make_buffer((const void*)(uintptr_t)(value ? v_rows : k_rows), row_bytes);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
         rs, (__attribute__((address_space(3))) void*)(dst + (value ? TILE : 0) + (piece * UPP + i) * 1024), 16, (int)(coff[i] + 0), 0, 0, 0);
   };
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(64 * TW, 2) void prefix_kernel(PagedParams p, const
   auto load_q = [&]() __attribute__((always_inline)) {
     const PagedParams a = arguments();
     bool valid;
-    const size_t row = Work{a, nullptr}.query_row(a.d, pc, pc.g * ROWS + 32 * tw + l32, valid);
+    const size_t row = Work{a}.query_row(a.d, pc, pc.g * ROWS + 32 * tw + l32, valid);
 #pragma unroll
     for (int s = 0; s < DS; ++s) qreg[s] = *reinterpret_cast<const bf16x8*>(a.d.Q + row * D + 16 * s + 8 * g2);
   };
@@ -298,79 +298,70 @@ __global__ __launch_bounds__(64 * TW, 2) void prefix_kernel(PagedParams p, const
     compute_fence();
     reset();
   };
-  PrefixPos last = pc;
-  // (restrict: tiles are read from cur and old, and copied to nxt.  Otherwise the compiler waits for every copy before
+  // (restrict: a tile is read from cur and one copied to nxt.  Otherwise the compiler waits for every copy before
   // it reads any.  It has to see these reads here, not in a lambda.)
-  auto step = [&](const char* __restrict__ cur, const char* __restrict__ values, char* __restrict__ nxt, int x,
-                  auto lag) __attribute__((always_inline)) {
-    constexpr bool LAG = decltype(lag)::value;
-    if (!LAG || x < x1) arrive();
+  auto step = [&](const char* __restrict__ cur, char* __restrict__ nxt, int x) __attribute__((always_inline)) {
+    arrive();
+    if (x > x0 && pc.j == 0) begin();
+    prepare(x + AHEAD < x1, AHEAD);
+    compute_fence();
+    // S^T[key][query] = sum_d K[key][d] Q[query][d]
+    f32x16 sacc[KB];
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
-      if (part == (LAG ? 0 : 1)) {
-        // O^T[d][query] += sum_key V^T[d][key] P^T[key][query]
-        if (some) {
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int c = 0; c < 2 * KB; ++c) {
-            const bf16x8 hi = __builtin_bit_cast(bf16x8, (u32x4{ph[4 * c], ph[4 * c + 1], ph[4 * c + 2], ph[4 * c + 3]}));
-            const bf16x8 lo = __builtin_bit_cast(bf16x8, (u32x4{pl[4 * c], pl[4 * c + 1], pl[4 * c + 2], pl[4 * c + 3]}));
+      for (int e = 0; e < 16; ++e) sacc[kb][e] = 0.f;
+    constexpr int K_AHEAD = 4;
+    bf16x8 k[K_AHEAD];
 #pragma unroll
-            for (int db = 0; db < DB; ++db) {
-              const bf16x8 v = lds_tr<D>(values + TILE, ops.tr_rel0, ops.tr_rel1, c, db);
-              oacc[db] = mfma32(v, hi, oacc[db]);
-              oacc[db] = mfma32(v, lo, oacc[db]);
-            }
-          }
-          pipeline_lds_reads<4 * KB * DB, 6, 1>();
-        }
-        if (LAG && x > x0 && (pc.j == 0 || x == x1)) {
-          flush(last, x - 1);
-          if (x < x1) begin();
-        }
-      } else if (!LAG || x < x1) {
-        if (!LAG && x > x0 && pc.j == 0) begin();
-        prepare(x + AHEAD < x1, AHEAD);
-        compute_fence();
-        // S^T[key][query] = sum_d K[key][d] Q[query][d]
-        f32x16 sacc[KB];
+    for (int i = 0; i < K_AHEAD; ++i) k[i] = lds_rows<D>(cur, ops.row_rel, i / KB, i % KB);
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
+    for (int i = 0; i < DS * KB; ++i) {
+      const bf16x8 now = k[i % K_AHEAD];
+      if (i + K_AHEAD < DS * KB) k[i % K_AHEAD] = lds_rows<D>(cur, ops.row_rel, (i + K_AHEAD) / KB, (i + K_AHEAD) % KB);
+      sacc[i % KB] = mfma32(now, qreg[i / KB], sacc[i % KB]);
+      if (i % (DS * KB / COPIES) == 0) copy(nxt, i / (DS * KB / COPIES));
+    }
+    pipeline_reads_and_copies<DS * KB, 4, 1, COPIES>();
+    compute_fence();
+    pages = pages_of();
+    softmax(sacc, pc.len - pc.j * KT, present & ((1u << NP) - 1));
+    landed(pages);
+    present >>= NP;
+    // O^T[d][query] += sum_key V^T[d][key] P^T[key][query]
+    if (some) {
+      // (the reads ahead are in the order of the text too: the scheduler, short of registers, may keep that)
+      constexpr int N = 2 * KB * DB, V_AHEAD = 3;
+      bf16x8 v[V_AHEAD];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) sacc[kb][e] = 0.f;
+      for (int i = 0; i < V_AHEAD; ++i) v[i] = lds_tr<D>(cur + TILE, ops.tr_rel0, ops.tr_rel1, i / DB, i % DB);
 #pragma unroll
-        for (int s = 0; s < DS; ++s)
-#pragma unroll
-          for (int kb = 0; kb < KB; ++kb) sacc[kb] = mfma32(lds_rows<D>(cur, ops.row_rel, s, kb), qreg[s], sacc[kb]);
-#pragma unroll
-        for (int u = 0; u < COPIES; ++u) copy(nxt, u);
-        pipeline_reads_and_copies<DS * KB, 4, 1, COPIES>();
-        compute_fence();
-        pages = pages_of();
-        softmax(sacc, pc.len - pc.j * KT, present & ((1u << NP) - 1));
-        landed(pages);
-        present >>= NP;
+      for (int i = 0; i < N; ++i) {
+        const int c = i / DB, db = i % DB;
+        const bf16x8 hi = __builtin_bit_cast(bf16x8, (u32x4{ph[4 * c], ph[4 * c + 1], ph[4 * c + 2], ph[4 * c + 3]}));
+        const bf16x8 lo = __builtin_bit_cast(bf16x8, (u32x4{pl[4 * c], pl[4 * c + 1], pl[4 * c + 2], pl[4 * c + 3]}));
+        const bf16x8 now = v[i % V_AHEAD];
+        if (i + V_AHEAD < N)
+          v[i % V_AHEAD] = lds_tr<D>(cur + TILE, ops.tr_rel0, ops.tr_rel1, (i + V_AHEAD) / DB, (i + V_AHEAD) % DB);
+        oacc[db] = mfma32(now, hi, oacc[db]);
+        oacc[db] = mfma32(now, lo, oacc[db]);
       }
+      pipeline_lds_reads<4 * KB * DB, 6, 1>();
     }
-    if (!LAG && (pc.j == pc.nt - 1 || x + 1 == x1)) flush(pc, x);
+    if (pc.j == pc.nt - 1 || x + 1 == x1) flush(pc, x);
   };
-  auto tiles = [&](auto lag) __attribute__((always_inline)) {
-    int slot = 0, before = 0;
-    for (int x = x0; x < (decltype(lag)::value ? x1 + 1 : x1); ++x) {
-      step(sm.buf + slot * (2 * TILE), sm.buf + (decltype(lag)::value ? before : slot) * (2 * TILE), sm.buf + next * (2 * TILE), x, lag);
-      before = slot;
-      slot = slot + 1 == NST ? 0 : slot + 1;
-      last = pc;
-      if (++pc.j == pc.nt) next_item(pc);
-    }
-  };
-  if (Shape::PAIRS && tw >= NP) tiles(Flag<true>());
-  else tiles(Flag<false>());
+  int slot = 0;
+  for (int x = x0; x < x1; ++x) {
+    step(sm.buf + slot * (2 * TILE), sm.buf + next * (2 * TILE), x);
+    slot = slot + 1 == NST ? 0 : slot + 1;
+    if (++pc.j == pc.nt) next_item(pc);
+  }
   wait_global_loads();
 }
 
-template <int D, int TW>
+template <int D>
 hipError_t launch_prefix(const PagedParams& p, hipStream_t st) {
-  hipLaunchKernelGGL((prefix_kernel<D, TW>), dim3(256 * PrefixShape<D, TW>::WORKGROUPS), dim3(64 * TW), 0, st, p, p.d.cache_lens);
+  hipLaunchKernelGGL((prefix_kernel<D>), dim3(256 * PREFIX_WORKGROUPS), dim3(64 * PREFIX_WAVES), 0, st, p);
   return hipGetLastError();
 }
 
@@ -414,7 +405,8 @@ __device__ inline void merge_part(MergeState& s, const float* part, size_t slot,
 // One thread per (query row, 4 features, part of the runs), as dec_combine_kernel:
 // P threads take every P-th run of the row's own item and of its prefix's and meet
 // in LDS in part order.
-template <int D, int P, bool OWN_COLS, bool PRE_COLS>
+// JOINT: both in the prefixes' arrays, the sequences' own items first.
+template <int D, int P, bool OWN_COLS, bool PRE_COLS, bool JOINT>
 __global__ __launch_bounds__((DEC_MERGE_THREADS<P, OWN_COLS || PRE_COLS>)) void shared_merge_kernel(MergeParams p) {
   constexpr bool COLS = OWN_COLS || PRE_COLS;  // consecutive threads take consecutive rows
   constexpr int NT = DEC_MERGE_THREADS<P, COLS>, TPR = D / 4, RPW = NT / (TPR * P);
@@ -432,11 +424,12 @@ __global__ __launch_bounds__((DEC_MERGE_THREADS<P, OWN_COLS || PRE_COLS>)) void 
     const int R = (int)(qrow % GS);
     const size_t bh = qrow / GS;
     const int g = R / p.own.grows, b = (int)(bh / p.own.Hkv), h = (int)(bh - (size_t)b * p.own.Hkv);
-    const DecRuns d = p.own.desc[bh * p.own.ng + g];
+    const int mine = (int)bh * p.own.ng + g;
+    const DecRuns d = p.own.desc[mine];
+    const SharedRef ref = p.refs[b];  // (of no meaning without a prefix)
     DecRuns e = {0, -1};
     int r2 = 0, item = 0;
     if (b < *p.members) {
-      const SharedRef ref = p.refs[b];
       const int G2 = (ref.row0 + R) / p.pre.grows;
       r2 = ref.row0 + R - G2 * p.pre.grows;
       item = ref.item0 + h * ref.ng + G2;
@@ -444,7 +437,8 @@ __global__ __launch_bounds__((DEC_MERGE_THREADS<P, OWN_COLS || PRE_COLS>)) void 
     }
 #pragma unroll 4
     for (int gw = d.first + part; gw <= d.last; gw += P)
-      merge_part<D, OWN_COLS>(s, p.own.part, dec_slot_row(p.own, gw, bh, g), R - g * p.own.grows, q4);
+      merge_part<D, OWN_COLS>(s, p.own.part,
+                              JOINT ? (size_t)(gw + mine) * p.own.grows : dec_slot_row(p.own, gw, bh, g), R - g * p.own.grows, q4);
 #pragma unroll 4
     for (int gw = e.first + part; gw <= e.last; gw += P)
       merge_part<D, PRE_COLS>(s, p.pre.part, (size_t)(gw + item) * p.pre.grows, r2, q4);
@@ -467,72 +461,73 @@ __global__ __launch_bounds__((DEC_MERGE_THREADS<P, OWN_COLS || PRE_COLS>)) void 
   if (q4 == 0) p.own.LSE[qrow] = none ? -INFINITY : (s.m + __log2f(s.l)) * LN2;
 }
 
-template <int D, bool OWN_COLS, bool PRE_COLS>
-void launch_merge_as(const MergeParams& p, bool many, hipStream_t st) {
+// Several threads a row's runs where the rows alone do not fill the card, us (D = 128, one thread, several):
+//   512 rows 25.5 21.9; 1024 rows 32.2 29.4 and 30.8 29.3; 2048 rows 34.2 32.6; 4096 rows 39.5 41.2 and 40.4 41.5.
+template <int D, bool OWN_COLS, bool PRE_COLS, bool JOINT = false>
+void launch_merge_as(const MergeParams& p, hipStream_t st) {
   constexpr bool COLS = OWN_COLS || PRE_COLS;
   const size_t rows = (size_t)p.own.B * p.own.Hq * p.own.S;
+  const bool many = rows * (D / 4) <= 65536;
   const auto merge = [&](auto parts) {
     constexpr int P = decltype(parts)::value, NT = DEC_MERGE_THREADS<P, COLS>, RPW = NT / (D / 4 * P);
-    hipLaunchKernelGGL((shared_merge_kernel<D, P, OWN_COLS, PRE_COLS>), dim3((unsigned)((rows + RPW - 1) / RPW)), dim3(NT), 0,
+    hipLaunchKernelGGL((shared_merge_kernel<D, P, OWN_COLS, PRE_COLS, JOINT>), dim3((unsigned)((rows + RPW - 1) / RPW)), dim3(NT), 0,
                        st, p);
   };
   if (many) merge(std::integral_constant<int, COLS ? 4 : 8>());
   else merge(std::integral_constant<int, 1>());
 }
 template <int D>
-void launch_merge(const MergeParams& p, bool own_cols, bool pre_cols, bool many, hipStream_t st) {
-  if (own_cols) {
-    if (pre_cols) launch_merge_as<D, true, true>(p, many, st);
-    else launch_merge_as<D, true, false>(p, many, st);
-  } else {
-    if (pre_cols) launch_merge_as<D, false, true>(p, many, st);
-    else launch_merge_as<D, false, false>(p, many, st);
-  }
-}
-
-template <int D>
-hipError_t launch_shared_d(const DecodeShape& s, const SharedArgs& a, void* ws, hipStream_t st) {
-  char* const pre_ws = static_cast<char*>(ws) + shared_own_bytes(s);
-  const DecodeGroups g = decode_groups(s);
-  const PagedParams own = paged_params(s, g, a.own, ws);
-
-  const int waves = shared_waves(s, a.groups);
+hipError_t launch_shared_d(const SharedShape& sh, const SharedArgs& a, void* ws, hipStream_t st) {
+  const DecodeShape& s = sh.s;
+  const int waves = shared_waves(sh);
+  const bool joint = shared_joint(sh);
+  char* const pre_ws = static_cast<char*>(ws) + (joint ? 0 : shared_own_bytes(s));
+  const size_t items = shared_items(sh);
   const DecodeGroups gp = {waves, 1, DEC_QT * waves, shared_runs(waves)};
   PagedArgs pa = a.own;
   pa.table = a.table;
   pa.width = a.width;
   pa.table_stride = a.table_stride;
   pa.cache_lens = a.lens;
-  pa.Kn = pa.Vn = nullptr;
   PagedParams pre = paged_params(s, gp, pa, ws);
-  const size_t items = shared_items(s, a.groups);
-  pre.d.B = a.groups;
-  pre.d.C = a.width << a.own.pages.log_size;
+  pre.d.B = sh.groups;
+  pre.d.C = sh.C;
   pre.d.desc = reinterpret_cast<DecRuns*>(pre_ws);
-  pre.d.part = reinterpret_cast<float*>(pre_ws + shared_desc_bytes(s, a.groups));
+  pre.d.part = reinterpret_cast<float*>(pre_ws + shared_desc_bytes(sh));
   pre.sizes = a.sizes;
   pre.seqs = s.B;
   pre.refs = reinterpret_cast<SharedRef*>(pre_ws) + items;
   pre.members = reinterpret_cast<int*>(pre.refs + s.B);
+  MergeParams m = {pre.d, pre.d, pre.refs, pre.members};
+  m.own.B = s.B;
 
-  hipError_t e = waves == 8   ? launch_prefix<D, 8>(pre, st)
-                 : waves == 4 ? launch_prefix<D, 4>(pre, st)
-                              : launch_paged_runs<D, PagedMode::Prefix>(gp, pre, st);
+  if (joint) {
+    pre.own = {(uint64_t)(uintptr_t)a.own.table, a.own.table_stride * 4, a.own.width - 1, s.C, a.own.cache_lens};
+    m.own.ng = (m.own.G * s.S + gp.rows - 1) / gp.rows;
+    const hipError_t e = launch_paged_runs<D, PagedMode::Joint>(gp, pre, st);
+    if (e != hipSuccess) return e;
+    if (waves == 1) launch_merge_as<D, false, false, true>(m, st);
+    else launch_merge_as<D, true, true, true>(m, st);
+    return hipGetLastError();
+  }
+
+  const DecodeGroups g = decode_groups(s);
+  const PagedParams own = paged_params(s, g, a.own, ws);
+  pre.Sn = 0;
+  hipError_t e = launch_prefix<D>(pre, st);
   if (e != hipSuccess) return e;
   e = launch_paged_runs<D, PagedMode::Own>(g, own, st);
   if (e != hipSuccess) return e;
-  const MergeParams m = {own.d, pre.d, pre.refs, pre.members};
-  // (as launch_dec_combine: eight runs or more an item)
-  const size_t prefixes = (size_t)s.Hkv * ((size_t)s.B * (s.Hq / s.Hkv) * s.S / gp.rows + 1);
-  const bool many = decode_items(s) * 8 <= (size_t)g.runs || prefixes * 8 <= (size_t)gp.runs;
-  launch_merge<D>(m, g.waves > 1, waves > 1, many, st);
+  m.own = own.d;
+  if (g.waves > 1) launch_merge_as<D, true, true>(m, st);
+  else launch_merge_as<D, false, true>(m, st);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_shared_decode(const DecodeShape& s, const SharedArgs& a, void* ws, hipStream_t st) {
-  return s.D == 128 ? launch_shared_d<128>(s, a, ws, st) : launch_shared_d<64>(s, a, ws, st);
+hipError_t launch_shared_decode(const SharedShape& s, const SharedArgs& a, void* ws, hipStream_t st) {
+  return s.s.D == 128 ? launch_shared_d<128>(s, a, ws, st) : launch_shared_d<64>(s, a, ws, st);
 }
 
 }  // namespace bd

@@ -102,9 +102,9 @@ SHARED = [
     ([2, 1], [129, 1000], [5, 70, 0, 20, 64], 4, 2, 64, 4, 64, "heads", True),     # two sequences behind the groups
     ([3], [700], [100, 3, 0], 12, 3, 128, 4, 16, "tokens", True),                  # 48 rows: two waves
     ([4], [500], [100, 3, 0, 65], 16, 4, 64, 4, 32, "heads", True),                # 64 rows
-    ([5], [500], [100, 3, 0, 65, 1], 16, 4, 128, 4, 32, "heads", True),            # 80 rows: four waves
+    ([5], [500], [100, 3, 0, 65, 1], 16, 4, 128, 4, 32, "heads", True),            # 80 rows
     ([8], [260], [0, 1, 2, 3, 60, 64, 65, 70], 16, 4, 128, 4, 16, "heads", True),  # 128 rows
-    ([9], [97], [0, 1, 2, 3, 60, 64, 65, 70, 9], 16, 4, 64, 4, 64, "tokens", True),  # 144 rows: two row groups
+    ([9], [97], [0, 1, 2, 3, 60, 64, 65, 70, 9], 16, 4, 64, 4, 64, "tokens", True),  # 144 rows
     ([3, 5], [400, 31], [0, 1, 100, 3, 60, 64, 65, 2], 8, 2, 128, 32, 32, "heads", True),   # 384 and 640 rows
     ([4, 1, 2], [90, 1030, 64], [10, 40, 0, 33, 1, 2, 3], 4, 1, 64, 40, 16, "heads", False),  # 160 rows a sequence
     ([1] * 70, [i % 50 for i in range(70)], [i % 37 for i in range(70)], 4, 2, 64, 1, 16, "tokens", True),
@@ -235,6 +235,94 @@ def test_shared_decode_replayed():
     """Lengths, group sizes and queries that change between replays."""
     a = _shared_inputs([3, 3, 2], [300, 44, 129], [20, 1, 40, 65, 33, 7, 70, 30], 16, 4, 128, 4, 16, "heads", True, 19)
     _replayed(lambda: bd.bd_attn_paged_shared_decode_fwd(*a), "shared", [
+        lambda: None, lambda: a[3].copy_(_ints([1, 5, 2])), lambda: a[5].copy_(_ints([10, 44, 100])),
+        lambda: a[7].copy_(_ints([2, 0, 40, 3, 33, 7, 64, 0])), lambda: a[0].mul_(-0.5), lambda: a[3].copy_(_ints([0, 0, 0]))])
+
+
+# Tables that are much wider than the prefixes in them: with more than 64 rows a group such a call takes its
+# prefixes and the sequences' own keys in launches of their own.
+
+def _widened(a):
+    b = list(a)
+    P, groups = a[1].shape[2], a[4].shape[0]
+    b[4] = torch.full((groups, (1 << 20) // P), (1 << 31) - 1, **I32)
+    b[4][:, :a[4].shape[1]] = a[4]
+    return b
+
+
+WIDE = [i for i, c in enumerate(SHARED) if len(c[2]) * c[3] // c[4] * c[6] > 64 * len(c[0])] + [-1, -2]
+SHARED_MORE = [  # at -1, -2
+    ([4, 1], [64 * 37 + 5, 3000], [500, 0, 33, 64, 1], 16, 2, 64, 16, 16, "sides", True),   # 512 and 128 rows
+    ([7, 9], [1500, 2049], list(range(0, 160, 10)), 16, 2, 128, 8, 64, "tokens", False),    # 448 and 576 rows
+]
+
+
+@pytest.mark.parametrize("case", WIDE)
+def test_shared_wide_tables_match_oracle(case):
+    c = SHARED[case] if case >= 0 else SHARED_MORE[-1 - case]
+    print(f"[sparse] wide {c}", flush=True)
+    a = _shared_inputs(*c, seed=130 + case)
+    _check_shared(a, bd.bd_attn_paged_shared_decode_fwd(*_widened(a)), f"wide {case}")
+
+
+@pytest.mark.parametrize("P,D", [(16, 128), (32, 64), (64, 128)])
+def test_shared_wide_tables_absent_pages_and_clamped_lengths(P, D):
+    a = _shared_inputs([2, 2], [200, 190], [50, 0, 130, 64], 8, 2, D, 32, P, "heads", True, 11)
+    a[4][0, 1] = -1
+    a[4][1, : -(-190 // P)] = 1 << 30      # a prefix that is in no page
+    a[6][2, 0] = a[1].shape[0]
+    a[7] = _ints([50, -9, 130, 64])
+    _check_shared(a, bd.bd_attn_paged_shared_decode_fwd(*_widened(a), scale=0.3), f"wide absent P{P}", 0.3)
+    a[5] = _ints([-1, 1 << 30])            # to the end of the table, which names no page there
+    got = bd.bd_attn_paged_shared_decode_fwd(*_widened(a))
+    a[5] = _ints([0, 0])
+    _check_shared(a, got, f"wide clamped P{P}")
+
+
+@pytest.mark.parametrize("P,order", [(16, "tokens"), (64, "heads"), (32, "sides")])
+def test_shared_wide_tables_read_nothing_else(P, order):
+    a = _shared_inputs([3, 2], [70, 131], [20, 1, 0, 65, 33], 8, 2, 128, 32, P, order, True, 13)
+    want = bd.bd_attn_paged_shared_decode_fwd(*_widened(a))
+    keep = torch.zeros(a[1].shape[0], P, dtype=torch.bool)
+    for t, lens in ((a[4], a[5].tolist()), (a[6], a[7].tolist())):
+        for b, n in enumerate(lens):
+            for j in range(n):
+                keep[int(t[b, j // P]), j % P] = True
+    for x in a[1:3]:
+        x.copy_(torch.where(keep.to(DEV)[:, None, :, None], x, float("nan")))
+    # ... and a workspace full of NaN, another stream, guards behind the results
+    w = _widened(a)
+    B, Hq, S, D = a[0].shape
+    n = bd.bd_attn_paged_shared_decode_workspace_bytes(B, 2, S, Hq, 2, D, P, w[4].shape[1], a[6].shape[1])
+    ws = torch.full((n + 64,), 255, dtype=torch.uint8, device=DEV)
+    o = torch.full((a[0].numel() + 64,), 7.0, dtype=BF, device=DEV)
+    lse = torch.full((B * Hq * S + 64,), 7.0, device=DEV)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = bd.bd_attn_paged_shared_decode_fwd(*w, out=o[:-64].view(a[0].shape), lse=lse[:-64].view(B, Hq, S), workspace=ws[:n],
+                                             stream=side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert (o[-64:] == 7).all() and (lse[-64:] == 7).all() and (ws[n:] == 255).all()
+
+
+def test_shared_wide_tables_offsets_past_32_bits():
+    Hq, Hkv, D, P, n, S = 32, 8, 128, 64, 66000, 16
+    kp = torch.empty((n, Hkv, P, D), dtype=BF, device=DEV)
+    vp = torch.empty_like(kp)
+    ids = [n - 1, 5, 32768, 40000, n - 2, 7]
+    for x in (kp, vp):
+        x[ids] = (torch.randn((6, Hkv, P, D), device=DEV) * 0.5).to(BF)
+    q = (torch.randn((2, Hq, S, D), device=DEV) * 0.5).to(BF)
+    rest = [_ints([2]), _ints([ids[:3]]), _ints([150]), _ints([[ids[3]], [ids[4]]]), _ints([64, 30]), None, None]
+    near = [_ints([2]), _ints([[0, 1, 2]]), _ints([150]), _ints([[3], [4]]), _ints([64, 30]), None, None]
+    got = bd.bd_attn_paged_shared_decode_fwd(*_widened([q, kp, vp, *rest]))
+    _check_shared([q, *(x[ids] for x in (kp, vp)), *near], got, "wide, far pages")
+
+
+def test_shared_wide_tables_replayed():
+    a = _widened(_shared_inputs([3, 3, 2], [300, 44, 129], [20, 1, 40, 65, 33, 7, 70, 30], 16, 4, 128, 16, 16, "heads", True, 19))
+    _replayed(lambda: bd.bd_attn_paged_shared_decode_fwd(*a), "shared, wide", [
         lambda: None, lambda: a[3].copy_(_ints([1, 5, 2])), lambda: a[5].copy_(_ints([10, 44, 100])),
         lambda: a[7].copy_(_ints([2, 0, 40, 3, 33, 7, 64, 0])), lambda: a[0].mul_(-0.5), lambda: a[3].copy_(_ints([0, 0, 0]))])
 
