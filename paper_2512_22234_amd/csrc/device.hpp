@@ -313,6 +313,17 @@ __device__ inline bf16x8 pack8(const f32x16& acc, int base) {
   return r;
 }
 
+// Inclusive sum of numbers >= 0 over the wave's lanes, in registers; sums that pass `most` are `most`.
+__device__ inline int wave_scan(int x, int most = INT32_MAX) {
+  x = imin(x + __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true), most);   // row_shr:1
+  x = imin(x + __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true), most);   // row_shr:2
+  x = imin(x + __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true), most);   // row_shr:4
+  x = imin(x + __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true), most);   // row_shr:8
+  x = imin(x + __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false), most);  // row_bcast:15, into rows 1 and 3
+  x = imin(x + __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false), most);  // row_bcast:31, into rows 2 and 3
+  return x;
+}
+
 // Two values as bf16 (round to nearest even), the first in the low half.
 __device__ inline uint32_t pack2(float a, float b) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

@@ -399,9 +399,10 @@ inline size_t shared_items(const SharedShape& a) {
   return a.s.Hkv * (B * rows / per + (a.groups < a.s.B ? a.groups : a.s.B) + own);
 }
 // Workspace: the sequences' own (decode_workspace_bytes), if apart, then a descriptor for each
-// item, a reference for each sequence and their count, and the partial results of every (team, item) run.
+// item, a reference for each sequence and KV head, the count of the sequences with a prefix, and
+// the partial results of every (team, item) run.
 inline size_t shared_desc_bytes(const SharedShape& a) {
-  return ((shared_items(a) + a.s.B + 1) * 16 + 255) & ~(size_t)255;
+  return ((shared_items(a) + (size_t)a.s.B * a.s.Hkv + 1) * 16 + 255) & ~(size_t)255;
 }
 inline size_t shared_part_bytes(const SharedShape& a) {
   const int waves = shared_waves(a);

@@ -8,11 +8,13 @@
 namespace bd {
 namespace {
 
-// Where the merge finds the prefix's part of a sequence: its items are item0 + h * ng
-// + (row0 + R) / grows for query row R of KV head h.
+// Where the merge finds the prefix's part of a sequence and KV head: its first query row
+// is row row0 of item `item`, which the runs first to last hold; rows past an item's grows
+// are in the items behind it.
 struct alignas(16) SharedRef {
-  int item0, ng, row0;
+  int item, row0, first, last;
 };
+static_assert(sizeof(SharedRef) == 16 && sizeof(DecRuns) == 16, "the workspace's layout (kernels.hpp)");
 
 // What the copies of a tile need, in bytes.
 struct PagedTile {
@@ -44,7 +46,7 @@ struct PagedParams {
   // Prefixes (d.B, d.C, d.cache_lens and t's table are theirs): members of each group, sequences in all
   const int* sizes;
   int seqs;
-  SharedRef* refs;  // [seqs], for the merge
+  SharedRef* refs;  // [seqs][Hkv], for the merge
   int* members;     // the sequences that are in a group
   // Joint: the sequences' own keys, in a table of own.width entries a row
   struct {
@@ -122,25 +124,30 @@ template <int KT, int TW, int NW, int TEAMS, bool JOINT>
 struct PrefixWork {
   struct Smem {
     int wmem[NW], wrow[NW], wsum[NW];  // per-wave sums: members, row groups, tiles of a KV head
-    int b[TEAMS], off[TEAMS], first[TEAMS], n[TEAMS], upto[TEAMS], row[TEAMS];  // where each team's run starts
+    int b[TEAMS], off[TEAMS], first[TEAMS], n[TEAMS], upto[TEAMS], row[TEAMS], len[TEAMS];  // where each team's run starts
   };
   const PagedParams& p;
   int c0, c1, before_members, before_rows, before_tiles, tiles;  // this thread's entries, what lies before them, their tiles
+  int size0, keys0;                                              // of its first entry: members that it names, keys
 
   typedef const __attribute__((address_space(4))) int* Uniform;  // (scalar loads: nothing writes these arrays meanwhile)
   __device__ int own() const { return JOINT ? p.seqs : 0; }      // entries ahead of the groups
   __device__ int entries() const { return own() + p.d.B; }
   __device__ int row_groups(int n) const { return tiles_of<32 * TW>(n * p.d.G * p.d.S); }
-  // Members and first member of entry b, where the groups before it have `upto`, which it
-  // adds to (sizes that pass the sequences end there); its keys; its tiles of a KV head and row group.
+  // Members that entry b names (a sequence's own keys: none).
   template <class Ints>
-  __device__ void members(int b, int& first, int& n, int& upto) const {
+  __device__ int size(int b) const {
+    return JOINT && b < p.seqs ? 0 : imax(((Ints)(uintptr_t)p.sizes)[b - own()], 0);
+  }
+  // Members and first member of entry b, which names `size`, where the groups before it have `upto`, which it
+  // adds to (sizes that pass the sequences end there); its keys; its tiles of a KV head and row group.
+  __device__ void members(int b, int size, int& first, int& n, int& upto) const {
     if (JOINT && b < p.seqs) {
       first = b;
       n = 1;
     } else {
       first = upto;
-      n = imin(imax(((Ints)(uintptr_t)p.sizes)[b - own()], 0), p.seqs - upto);
+      n = imin(size, p.seqs - upto);
       upto += n;
     }
   }
@@ -153,20 +160,22 @@ struct PrefixWork {
     return imax(tiles_of<KT>(len) + (JOINT && b < p.seqs ? tiles_of<KT>(p.Sn) : 0), 1);
   }
 
+  // Of an entry of this thread.
+  __device__ int my_size(int b) const { return b == c0 ? size0 : size<const int*>(b); }
+  __device__ int my_keys(int b) const { return b == c0 ? keys0 : keys<const int*>(b); }
+
   // Tiles of a KV head in all entries; the first workgroup notes what the merge needs.
+  // (All that a thread with one entry reads, it reads at once, ahead of the sums.)
   __device__ int scan(Smem& sm, int tid) {
     const int lane = tid & 63, w = tid >> 6;
     const int cpt = cdiv(entries(), 64 * NW);
     c0 = imin(entries(), tid * cpt);
     c1 = imin(entries(), c0 + cpt);
+    size0 = c0 < c1 ? size<const int*>(c0) : 0;
+    keys0 = c0 < c1 ? keys<const int*>(c0) : 0;
     int mem = 0;
-    for (int b = imax(c0, own()); b < c1; ++b) mem += imin(imax(p.sizes[b - own()], 0), p.seqs - mem);
-    int imem = mem;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int u = __shfl_up(imem, o, 64);
-      if (lane >= o) imem = imin(imem + u, p.seqs);
-    }
+    for (int b = c0; b < c1; ++b) mem += imin(my_size(b), p.seqs - mem);
+    const int imem = wave_scan(mem, p.seqs);
     if (lane == 63) sm.wmem[w] = imem;
     __syncthreads();
     const int last = __shfl_up(imem, 1, 64);
@@ -181,20 +190,12 @@ struct PrefixWork {
     tiles = 0;
     for (int b = c0, upto = before_members; b < c1; ++b) {
       int first, n;
-      members<const int*>(b, first, n, upto);
+      members(b, my_size(b), first, n, upto);
       const int r = row_groups(n);
       rows += r;
-      tiles += tiles_at(b, keys<const int*>(b)) * r;
+      tiles += tiles_at(b, my_keys(b)) * r;
     }
-    int irow = rows, itile = tiles;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int u = __shfl_up(irow, o, 64), t = __shfl_up(itile, o, 64);
-      if (lane >= o) {
-        irow += u;
-        itile += t;
-      }
-    }
+    const int irow = wave_scan(rows), itile = wave_scan(tiles);
     if (lane == 63) {
       sm.wrow[w] = irow;
       sm.wsum[w] = itile;
@@ -217,8 +218,8 @@ struct PrefixWork {
     int pb = before_tiles, upto = before_members, row = before_rows;
     for (int b = c0; b < c1; ++b) {
       int first, n;
-      members<const int*>(b, first, n, upto);
-      const int r = row_groups(n), t = tiles_at(b, keys<const int*>(b)) * r;
+      members(b, my_size(b), first, n, upto);
+      const int len = my_keys(b), r = row_groups(n), t = tiles_at(b, len) * r;
       if (x0 < (pb + t) * I) {
         sm.b[v] = b;
         sm.off[v] = x0 - pb * I;
@@ -226,16 +227,16 @@ struct PrefixWork {
         sm.n[v] = n;
         sm.upto[v] = upto;
         sm.row[v] = row;
+        sm.len[v] = len;
         return;
       }
       pb += t;
       row += r;
     }
   }
-  // What q holds of its entry q.b, of q.n members.
+  // What q holds of its entry q.b, of q.n members and q.len keys.
   __device__ void enter(PrefixPos& q) const {
     const bool mine = JOINT && q.b < p.seqs;  // a sequence's own keys
-    q.len = keys<Uniform>(q.b);
     q.nt = tiles_at(q.b, q.len);
     q.ntc = mine ? tiles_of<KT>(q.len) : q.nt;
     q.ng = row_groups(q.n);
@@ -250,6 +251,7 @@ struct PrefixWork {
     q.n = __builtin_amdgcn_readfirstlane(sm.n[v]);
     q.upto = __builtin_amdgcn_readfirstlane(sm.upto[v]);
     q.row = __builtin_amdgcn_readfirstlane(sm.row[v]);
+    q.len = __builtin_amdgcn_readfirstlane(sm.len[v]);
     enter(q);
     const int item = off / q.nt;
     q.j = off - item * q.nt;
@@ -267,9 +269,10 @@ struct PrefixWork {
     do {  // (to the next group that has members)
       q.row += q.ng;
       if (++q.b >= entries()) return;
-      members<Uniform>(q.b, q.first, q.n, q.upto);
+      members(q.b, size<Uniform>(q.b), q.first, q.n, q.upto);
       q.ng = row_groups(q.n);
     } while (q.n == 0);
+    q.len = keys<Uniform>(q.b);
     enter(q);
   }
   // Query row R of the entry's rows of a KV head (rows past the last: the last).
@@ -319,27 +322,25 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
   // ---- prologue: T, and the position of each team's first tile (as over a dense cache) ----
   const int cpt = cdiv(p.d.B, NT);
   const int c0 = imin(p.d.B, tid * cpt), c1 = imin(p.d.B, c0 + cpt);
-  int csum = 0;
+  int csum = 0, excl = 0, total = 0;  // excl: tiles per item of the sequences before c0
+  if constexpr (JOINT) {
+    total = work.scan(sm.work, tid);
+  } else {
 #pragma unroll 4
-  for (int b = c0; b < c1; ++b) csum += JOINT ? 0 : paged_tiles<KT>(p, dec_len(p.d, lens, b));
-  int incl = csum;
+    for (int b = c0; b < c1; ++b) csum += paged_tiles<KT>(p, dec_len(p.d, lens, b));
+    const int incl = wave_scan(csum);
+    if (lane == 63) sm.wsum[w] = incl;
+    __syncthreads();
+    int before = 0;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int u = __shfl_up(incl, o, 64);
-    if (lane >= o) incl += u;
+    for (int v = 0; v < NW; ++v) {
+      const int s = sm.wsum[v];
+      before += v < w ? s : 0;
+      total += s;
+    }
+    excl = before + incl - csum;
+    total = __builtin_amdgcn_readfirstlane(total);
   }
-  if (lane == 63) sm.wsum[w] = incl;
-  __syncthreads();
-  int before = 0, total = 0;
-#pragma unroll
-  for (int v = 0; v < NW; ++v) {
-    const int s = sm.wsum[v];
-    before += v < w ? s : 0;
-    total += s;
-  }
-  const int excl = before + incl - csum;  // tiles per item of the sequences before c0
-  total = __builtin_amdgcn_readfirstlane(total);
-  if constexpr (JOINT) total = work.scan(sm.work, tid);
   const int T = total * I;  // checked on the host to fit in 31 bits
   const int n = paged_runs<D, TW, PARTS>(T, p.d.B * I);
   const bool stream = total * p.d.Hkv > (int)(DEC_STREAM_BYTES / (2 * Smem::TILE));
@@ -599,7 +600,7 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
 
     // Write out the state of the current item's segment, which ends at tile pc.j
     // (tile x of all).
-    SharedRef* const refs = JOINT ? p.refs : nullptr;
+    SharedRef* const refs = JOINT ? p.refs : nullptr;  // (`arguments` gives the first part alone)
     const int seqs = JOINT ? p.seqs : 0;
     auto flush = [&](int x) __attribute__((always_inline)) {
       const DecParams p = arguments();
@@ -647,16 +648,16 @@ __global__ __launch_bounds__(TW == 1 ? 192 : 64 * TW, 1) void paged_kernel(Paged
           }
         if (g2 == 0) *reinterpret_cast<float2*>(pr + (TW == 1 ? D : 32 * D + 2 * l32)) = float2{m, Lrow};
       }
-      if (ends && lane == 0 && tw == 0) {
+      if (ends && (JOINT || (lane == 0 && tw == 0))) {
         // the runs holding this item: from the one holding its first tile to this one
-        const int first = PARTS && item_start >= x0 ? gw : (int)((((long long)item_start + 1) * n - 1) / T);
-        p.desc[item] = DecRuns{first, gw};
-      }
-      if constexpr (JOINT) {
-        // the first row of each member, once for all KV heads
-        const int rows = p.G * p.S, R = pc.g * p.grows + 32 * tw + l32;
-        if (ends && pc.b >= seqs && pc.h == 0 && g2 == 0 && valid && R % rows == 0)
-          refs[pc.first + R / rows] = SharedRef{pc.row * p.Hkv, pc.ng, R};
+        const DecRuns runs = {PARTS && item_start >= x0 ? gw : (int)((((long long)item_start + 1) * n - 1) / T), gw};
+        if (!JOINT || (lane == 0 && tw == 0)) p.desc[item] = runs;
+        if constexpr (JOINT) {
+          // the first row of each member
+          const int rows = p.G * p.S, rl = 32 * tw + l32, R = pc.g * p.grows + rl;
+          if (pc.b >= seqs && g2 == 0 && valid && R % rows == 0)
+            refs[(pc.first + R / rows) * p.Hkv + pc.h] = SharedRef{item, rl, runs.first, runs.last};
+        }
       }
     };
 

@@ -262,10 +262,13 @@ __global__ __launch_bounds__(64 * PREFIX_WAVES, PREFIX_WORKGROUPS) void prefix_k
           *reinterpret_cast<f32x4*>(pr + 4 * lane + (4 * db + i) * 256) = v;
         }
       if (g2 == 0) *reinterpret_cast<float2*>(pr + 32 * D + 2 * l32) = float2{m, Lrow};
-      if (ends && q.h == 0 && g2 == 0 && R % per == 0) p.refs[q.first + R / per] = SharedRef{q.row * p.d.Hkv, q.ng, R};
     }
-    if (ends && lane == 0 && tw == 0)
-      p.d.desc[item] = DecRuns{x - q.j >= x0 ? gw : (int)((((long long)(x - q.j) + 1) * n - 1) / T), gw};
+    if (ends) {
+      const DecRuns runs = {x - q.j >= x0 ? gw : (int)((((long long)(x - q.j) + 1) * n - 1) / T), gw};
+      if (lane == 0 && tw == 0) p.d.desc[item] = runs;
+      if (valid && g2 == 0 && R % per == 0)  // the first row of each member
+        p.refs[(q.first + R / per) * p.d.Hkv + q.h] = SharedRef{item, 32 * tw + l32, runs.first, runs.last};
+    }
   };
 
   // ---- the run ----
@@ -423,17 +426,17 @@ __global__ __launch_bounds__((DEC_MERGE_THREADS<P, OWN_COLS || PRE_COLS>)) void 
   if (live) {
     const int R = (int)(qrow % GS);
     const size_t bh = qrow / GS;
-    const int g = R / p.own.grows, b = (int)(bh / p.own.Hkv), h = (int)(bh - (size_t)b * p.own.Hkv);
+    const int g = R / p.own.grows, b = (int)(bh / p.own.Hkv);
     const int mine = (int)bh * p.own.ng + g;
     const DecRuns d = p.own.desc[mine];
-    const SharedRef ref = p.refs[b];  // (of no meaning without a prefix)
+    const SharedRef ref = p.refs[bh];  // (of no meaning without a prefix)
     DecRuns e = {0, -1};
     int r2 = 0, item = 0;
     if (b < *p.members) {
-      const int G2 = (ref.row0 + R) / p.pre.grows;
+      const int G2 = (ref.row0 + R) / p.pre.grows;  // items behind that of the member's first row
       r2 = ref.row0 + R - G2 * p.pre.grows;
-      item = ref.item0 + h * ref.ng + G2;
-      e = p.pre.desc[item];
+      item = ref.item + G2;
+      e = G2 == 0 ? DecRuns{ref.first, ref.last} : p.pre.desc[item];
     }
 #pragma unroll 4
     for (int gw = d.first + part; gw <= d.last; gw += P)
@@ -497,7 +500,7 @@ hipError_t launch_shared_d(const SharedShape& sh, const SharedArgs& a, void* ws,
   pre.sizes = a.sizes;
   pre.seqs = s.B;
   pre.refs = reinterpret_cast<SharedRef*>(pre_ws) + items;
-  pre.members = reinterpret_cast<int*>(pre.refs + s.B);
+  pre.members = reinterpret_cast<int*>(pre.refs + (size_t)s.B * s.Hkv);
   MergeParams m = {pre.d, pre.d, pre.refs, pre.members};
   m.own.B = s.B;
 

@@ -219,17 +219,6 @@ constexpr int CHOOSE_NT = 512, SCORE_NT = 512, SELECT_NT = 1024;  // threads of 
 constexpr int SELECT_KEYS = 4096;   // of a sequence and KV head, in LDS
 constexpr int SCORE_PAGES = 256;    // of a workgroup, where several share a sequence and KV head
 
-// Inclusive sum over the wave's lanes, in registers.
-__device__ inline int wave_scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);   // row_shr:1
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);   // row_shr:2
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);   // row_shr:4
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);   // row_shr:8
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast:15, into rows 1 and 3
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31, into rows 2 and 3
-  return x;
-}
-
 template <int NT>
 struct SelectSmem {
   int bins[2][256];
