@@ -82,8 +82,9 @@ __global__ __launch_bounds__(64 * PREFIX_WAVES, PREFIX_WORKGROUPS) void prefix_k
   Work work{p};
   const int T = work.scan(sm.work, tid) * p.d.Hkv;  // checked on the host to fit in 31 bits
   const int n = imin(256 * PREFIX_WORKGROUPS, cdiv(T, 2));  // runs (two tiles at least, as dec_runs)
-  const int gw = blockIdx.x;
-  if (gw >= n) return;
+  // (consecutive runs on one die)
+  const int per = cdiv(n, 8), gw = (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
+  if ((int)(blockIdx.x / 8) >= per || gw >= n) return;
   const int x0 = paged_run_start(gw, n, T), x1 = paged_run_start(gw + 1, n, T);
   work.find(sm.work, 0, x0);
   __syncthreads();
