@@ -230,7 +230,7 @@ __device__ inline void score_pages(const SelectArgs& a, ScoreSmem<D, NW>& sm, in
 
 constexpr int CHOOSE_NT = 512, SCORE_NT = 512, SELECT_NT = 1024;  // threads of the kernels below
 constexpr int SELECT_KEYS = 4096;   // of a sequence and KV head, in LDS
-constexpr int SCORE_PAGES = 256;    // of a workgroup, where several share a sequence and KV head
+constexpr int SCORE_PAGES = 256;    // of a workgroup at most, where several share a sequence and KV head
 
 template <int NT>
 struct SelectSmem {
@@ -360,19 +360,19 @@ __global__ __launch_bounds__(CHOOSE_NT, 4) void choose_kernel(SelectArgs a) {
   }
 }
 
-// Several workgroups a sequence and KV head: keys of SCORE_PAGES pages each, in the workspace ...
+// Several workgroups a sequence and KV head: keys of a.chunk pages each, in the workspace ...
 template <int D>
 __global__ __launch_bounds__(SCORE_NT) void score_kernel(SelectArgs a) {
   __shared__ struct {
     ScoreSmem<D, SCORE_NT / 64> score;
     int ids[SCORE_PAGES];
   } sm;
-  const int chunks = cdiv(a.width, SCORE_PAGES);
+  const int chunks = cdiv(a.width, a.chunk);
   const int c = blockIdx.x % chunks, bh = blockIdx.x / chunks, h = bh % a.Hkv, b = bh / a.Hkv;
   const SelectSeq seq = select_seq(a, b);
-  if (c * SCORE_PAGES >= seq.used) return;
+  if (c * a.chunk >= seq.used) return;
   uint64_t* keys = a.keys + (int64_t)bh * a.width;
-  score_pages<D, SCORE_NT / 64>(a, sm.score, sm.ids, b, h, seq.used, c * SCORE_PAGES, imin(seq.used, (c + 1) * SCORE_PAGES),
+  score_pages<D, SCORE_NT / 64>(a, sm.score, sm.ids, b, h, seq.used, c * a.chunk, imin(seq.used, (c + 1) * a.chunk),
                     [&](int j, uint64_t key) { keys[j] = key; });
 }
 // ... and the choice among them.
@@ -396,7 +396,7 @@ __global__ __launch_bounds__(SELECT_NT) void select_kernel(SelectArgs a) {
 }
 
 // Whether one workgroup takes a sequence and KV head on its own.  us a call (D = 128, 8 KV heads, G S = 16), one workgroup
-// and several: one sequence of 250, 500, 625, 1000 pages 12.7 12.9 15.6 20.5 and 15.4 15.4 14.9 15.3; 2000 pages of
+// and several: one sequence of 250, 500, 625, 1000 pages 12.7 12.9 15.6 20.5 and (with 256 pages a workgroup) 15.4 15.4 14.9 15.3; 2000 pages of
 // 8, 16, 32, 64 sequences 37 40 58 99 and 24 40 67 127; 4062 pages of 16, 32 74 108 and 72 124.
 bool select_fused(const SelectArgs& a) {
   return a.width <= SELECT_KEYS && (a.width <= 512 || a.B * a.Hkv >= 256);
@@ -417,7 +417,8 @@ hipError_t launch_summarize(const SummaryArgs& in, int D, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_select(const SelectArgs& a, int D, hipStream_t st) {
+hipError_t launch_select(const SelectArgs& in, int D, hipStream_t st) {
+  SelectArgs a = in;
   const unsigned items = (unsigned)a.B * a.Hkv;
   if (select_fused(a)) {
     const bool few = a.width <= 1024;
@@ -427,7 +428,11 @@ hipError_t launch_select(const SelectArgs& a, int D, hipStream_t st) {
     else hipLaunchKernelGGL((choose_kernel<64, SELECT_KEYS>), dim3(items), dim3(CHOOSE_NT), 0, st, a);
     return hipGetLastError();
   }
-  const dim3 grid(items * cdiv(a.width, SCORE_PAGES));
+  // 128 pages a workgroup, or 256 where a launch would not hold the threads.  us a call
+  // (D = 128, 8 KV heads), 128 and 256: one sequence of 1000 pages 11.1 12.7, of 2048 14.1 15.8, of 8192 with 128 query rows
+  // 38.3 39.8; two of 2000, 128 rows 18.0 18.6; four of 4096 32.2 32.6.
+  a.chunk = (int64_t)items * cdiv(a.width, 128) <= 1 << 22 ? 128 : SCORE_PAGES;
+  const dim3 grid(items * cdiv(a.width, a.chunk));
   if (D == 128) hipLaunchKernelGGL(score_kernel<128>, grid, dim3(SCORE_NT), 0, st, a);
   else hipLaunchKernelGGL(score_kernel<64>, grid, dim3(SCORE_NT), 0, st, a);
   const hipError_t e = hipGetLastError();

@@ -336,6 +336,7 @@ def test_shared_wide_tables_replayed():
     (5, 2, 64, 1024, "tokens", [0, 0, 5, 1023, 2000], [0, 1, 6, 1025, 2049]), (2, 1, 128, 1 << 15, "heads", [0, 40000], [40000, 33000]),
     (300, 4, 128, 32, "heads", [i % 60 for i in range(300)], [i % 90 for i in range(300)]),
     (2, 2, 64, 16, "heads", [-5, 3], [1 << 30, -1]),
+    (4200, 5, 64, 16, "tokens", [i % 40 for i in range(4200)], [i % 70 for i in range(4200)]),
 ])
 def test_summaries_match_oracle(B, Hkv, D, P, order, before, after):
     """Equal to the oracle's, and those of other pages as they were; NaN in rows past the lengths."""
