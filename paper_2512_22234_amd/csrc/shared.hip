@@ -24,10 +24,11 @@ namespace {
 // page ids come a tile ahead of the copies, by scalar loads that are waited for under the softmax;
 // tiles without absent or missing keys, nearly all, take no test a key.  Two workgroups share
 // a CU, so that one is at its products while the other is at its exponentials.
-//   24 sequences of 32 rows and 4 query heads a KV head on prefixes of 8000 keys (D = 128): 167 us a call, 534 TFLOP/s
-//   of the two products as they are defined (800 executed).
+//   One group of 24 sequences of 32 queries, 4 query heads a KV head, 8 KV heads, D = 128: on a prefix of 8000 keys 176 us
+//   a call, 573 TFLOP/s of the two products as they are defined (860 executed); on one of 64,000 1167 us, 690 TFLOP/s.
+// MFMA busy 0.41: a wave's products and its exponentials take about as long and overlap with the other workgroup's only.
 // Measured against it: 256 rows a workgroup of eight waves, half of them a product behind the
-// others, 167 us there and 5% to 2% either way elsewhere.
+// others, the same there and 5% to 2% either way elsewhere.
 constexpr int PREFIX_WAVES = 4, PREFIX_WORKGROUPS = 2;  // of a workgroup; a CU
 template <int D>
 struct PrefixShape {
@@ -82,7 +83,9 @@ __global__ __launch_bounds__(64 * PREFIX_WAVES, PREFIX_WORKGROUPS) void prefix_k
   Work work{p};
   const int T = work.scan(sm.work, tid) * p.d.Hkv;  // checked on the host to fit in 31 bits
   const int n = imin(256 * PREFIX_WORKGROUPS, cdiv(T, 2));  // runs (two tiles at least, as dec_runs)
-  // (consecutive runs on one die)
+  // Consecutive runs on one die, whose L2 then holds more of the prefix for the row groups of a KV head: three groups
+  // of 8, blocks of 32, prefixes of 4096 to 8192, 526 -> 304 MB fetched, 141.7 -> 139.1 us; the 8000 keys above 179 -> 175,
+  // the 64,000 1152 -> 1168.
   const int per = cdiv(n, 8), gw = (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
   if ((int)(blockIdx.x / 8) >= per || gw >= n) return;
   const int x0 = paged_run_start(gw, n, T), x1 = paged_run_start(gw + 1, n, T);
@@ -465,6 +468,8 @@ __global__ __launch_bounds__((DEC_MERGE_THREADS<P, OWN_COLS || PRE_COLS>)) void 
   if (q4 == 0) p.own.LSE[qrow] = none ? -INFINITY : (s.m + __log2f(s.l)) * LN2;
 }
 
+// What bounds it: reading the partial results, 528 bytes a row and run (D = 128; 21,504 rows, 6.2 runs each, 71 MB: 14 us,
+// 5.5 TB/s with what it writes), and below 20 MB the latency of two dependent loads.
 // Several threads a row's runs where the rows alone do not fill the card, us (D = 128, one thread, several):
 //   512 rows 25.5 21.9; 1024 rows 32.2 29.4 and 30.8 29.3; 2048 rows 34.2 32.6; 4096 rows 39.5 41.2 and 40.4 41.5.
 template <int D, bool OWN_COLS, bool PRE_COLS, bool JOINT = false>

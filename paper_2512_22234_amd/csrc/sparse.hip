@@ -337,7 +337,9 @@ __device__ inline void select_pages(const SelectArgs& a, SelectSmem<NT>& sm, int
   if (tid == (used > 0 ? (used - 1) % NT : 0)) a.rows_out[bh] = tail >= 0 ? tail : count << a.log_size;
 }
 
-// One workgroup a sequence and KV head, its pages and keys in LDS.
+// One workgroup a sequence and KV head, its pages and keys in LDS.  64 sequences of 512 to 8192 tokens in pages of 16 (61 MB
+// of summaries, D = 128, 8 KV heads, 16 query rows) 21 us: 12 for the reading, as fast as HBM gives it, and 7, all that one
+// sequence of 94 pages takes, for the chain of query rows, first pages, and the digits of the choice.
 // (four waves a SIMD: two workgroups a CU)
 template <int D, int KEYS>
 __global__ __launch_bounds__(CHOOSE_NT, 4) void choose_kernel(SelectArgs a) {
@@ -360,7 +362,8 @@ __global__ __launch_bounds__(CHOOSE_NT, 4) void choose_kernel(SelectArgs a) {
   }
 }
 
-// Several workgroups a sequence and KV head: keys of a.chunk pages each, in the workspace ...
+// Several workgroups a sequence and KV head: keys of a.chunk pages each, in the workspace ...  Two sequences of 120,000
+// tokens in pages of 64 with 128 query rows (16 MB): 9.9 us, then 8.7 for the choice, a chain of loads and barriers each.
 template <int D>
 __global__ __launch_bounds__(SCORE_NT) void score_kernel(SelectArgs a) {
   __shared__ struct {
