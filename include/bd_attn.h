@@ -504,6 +504,8 @@ size_t bd_attn_paged_decode_workspace_bytes(int B, int S, int Hq, int Hkv, int D
  *   prefix, as for bd_attn_paged_decode_fwd (max_pages >= 1; cache_lens may be 0).
  * A prefix takes whole pages of its own: the last one need not be full.  Pages
  * may be shared freely, nothing is written to them.
+ * How the work is laid out goes by B / groups and max_prefix_pages * page_size, so
+ * a list with many empty groups, or a table far wider than the prefixes, is right but slower.
  * groups from 1 to 2^16, max_prefix_pages >= 1 and max_prefix_pages * page_size
  * <= 2^22; all else as for bd_attn_paged_decode_fwd.
  */

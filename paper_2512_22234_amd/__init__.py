@@ -1031,7 +1031,8 @@ def bd_attn_paged_shared_decode_fwd(q, k_pages, v_pages, group_sizes, prefix_tab
     behind the last group have no prefix); prefix_table int32 [groups,
     max_prefix_pages] (rows may be strided) and prefix_lens int32 [groups]: the
     pages and keys of the prefixes; page_table, cache_lens and all else: the
-    sequences' own keys, behind the prefix, as for bd_attn_paged_decode_fwd."""
+    sequences' own keys, behind the prefix, as for bd_attn_paged_decode_fwd.
+    (Empty groups and a prefix_table far wider than the prefixes cost time.)"""
     B, Hq, S, Hkv, D, pages, kn, vn = _paged_inputs("bd_attn_paged_shared_decode_fwd", q, k_pages, v_pages, k_new, v_new)
     n, P, sp, sh, sr = pages
     dev = q.device

@@ -131,6 +131,17 @@ def test_shared_many_groups():
     _check_shared(a, bd.bd_attn_paged_shared_decode_fwd(*a), "many groups")
 
 
+@pytest.mark.parametrize("B", [7, 9])
+@pytest.mark.parametrize("wide", [False, True])
+def test_shared_lists_that_end_in_empty_groups(B, wide):
+    """Members all gone before the list ends, or sequences behind it; an overlong group and empty ones between."""
+    sizes = [0, 3, 0, 0, 4] + [0] * 40 + ([5] if B == 7 else [])
+    a = _shared_inputs(sizes, [10, 300, 7, 0, 170] + [33] * (len(sizes) - 5), list(range(5, 5 + B)), 32, 2, 128, 32, 16, "heads", True, 17)
+    if wide:
+        a = _widened(a)
+    _check_shared(a, bd.bd_attn_paged_shared_decode_fwd(*a), f"empty end B{B} wide {wide}")
+
+
 @pytest.mark.parametrize("S,Hq,D,P", [(1, 8, 128, 16), (4, 16, 64, 64), (32, 8, 128, 32)])
 def test_shared_absent_pages_clamped_lengths_and_scale(S, Hq, D, P):
     a = _shared_inputs([2, 2], [200, 190], [50, 0, 130, 64], Hq, 2, D, S, P, "heads", S > 1, 11)
