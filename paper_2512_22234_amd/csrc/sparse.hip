@@ -400,8 +400,8 @@ __global__ __launch_bounds__(SELECT_NT) void select_kernel(SelectArgs a) {
 
 // Whether one workgroup takes a sequence and KV head on its own.  Device us a call (D = 128, 8 KV heads, one query), one
 // workgroup and several: one sequence of 250, 380, 510 pages 9.2 11.1 12.6 and 10.1 10.5 10.3; four of 250, 380, 510 9.4 11.4
-// 12.9 and 10.4 11.0 11.2; 16 of 140, 510 8.3 14.5 and 12.2 16.3.  us a call with 256 pages a workgroup: one of 1000 20.5 and 15.3; 2000 pages of
-// 8, 16, 32, 64 37 40 58 99 and 24 40 67 127; 4062 pages of 16, 32 74 108 and 72 124.
+// 12.9 and 10.4 11.0 11.2; 16 of 140, 510 8.3 14.5 and 12.2 16.3.  us a call, several with 256 pages each: one of 1000 pages
+// 20.5 and 15.3; 2000 pages of 8, 16, 32, 64 37 40 58 99 and 24 40 67 127; 4062 pages of 16, 32 74 108 and 72 124.
 bool select_fused(const SelectArgs& a) {
   const int items = a.B * a.Hkv;
   return a.width <= SELECT_KEYS && (a.width <= (items <= 32 ? 320 : 512) || items >= 256);
