@@ -1151,7 +1151,7 @@ int bd_paged_select(const void* Q, const void* summaries, const int32_t* page_ta
   }
   const bd::SelectArgs a{static_cast<const __bf16*>(Q), static_cast<const __bf16*>(summaries), page_table, B, Hkv, Hq / Hkv * S,
                          max_pages, table_stride, cache_lens, num_pages, lg, budget, first, last, lists, list_lens,
-                         static_cast<uint64_t*>(ws), 0};
+                         static_cast<uint64_t*>(ws)};
   (void)hipGetLastError();
   return bd::launch_select(a, D, stream) == hipSuccess ? BD_ATTN_OK : BD_ATTN_ERR_HIP;
 }

@@ -439,7 +439,6 @@ struct SelectArgs {
   int* lists;      // [B][Hkv][budget]
   int* rows_out;   // [B][Hkv]
   uint64_t* keys;  // workspace: [B][Hkv][width]
-  int chunk;       // pages of a workgroup (set by the launcher)
 };
 inline size_t select_workspace_bytes(int B, int Hkv, int width) { return (size_t)B * Hkv * width * 8; }
 hipError_t launch_select(const SelectArgs& a, int D, hipStream_t st);

@@ -229,8 +229,9 @@ __device__ inline void score_pages(const SelectArgs& a, ScoreSmem<D, NW>& sm, in
 // ---- the choice ----
 
 constexpr int CHOOSE_NT = 512, SCORE_NT = 512, SELECT_NT = 1024;  // threads of the kernels below
+constexpr int SCORE_WORKGROUPS = 4096;  // at most
 constexpr int SELECT_KEYS = 4096;   // of a sequence and KV head, in LDS
-constexpr int SCORE_PAGES = 256;    // of a workgroup at most, where several share a sequence and KV head
+constexpr int SCORE_PAGES = 128;    // of a workgroup at a time, where several share a sequence and KV head
 
 template <int NT>
 struct SelectSmem {
@@ -337,7 +338,7 @@ __device__ inline void select_pages(const SelectArgs& a, SelectSmem<NT>& sm, int
   if (tid == (used > 0 ? (used - 1) % NT : 0)) a.rows_out[bh] = tail >= 0 ? tail : count << a.log_size;
 }
 
-// One workgroup a sequence and KV head, its pages and keys in LDS.  64 sequences of 512 to 8192 tokens in pages of 16 (61 MB
+// One workgroup a sequence and KV head, its pages and keys in LDS (past KEYS pages, keys in the workspace).  64 sequences of 512 to 8192 tokens in pages of 16 (61 MB
 // of summaries, D = 128, 8 KV heads, 16 query rows) 21 us: 12 for the reading, as fast as HBM gives it, and 7, all that one
 // sequence of 94 pages takes, for the chain of query rows, first pages, and the digits of the choice.
 // (four waves a SIMD: two workgroups a CU)
@@ -351,18 +352,26 @@ __global__ __launch_bounds__(CHOOSE_NT, 4) void choose_kernel(SelectArgs a) {
   } sm;
   const int bh = blockIdx.x, h = bh % a.Hkv, b = bh / a.Hkv;
   const SelectSeq seq = select_seq(a, b);
-  if (seq.used > a.budget) {
+  const int* row = a.table + (int64_t)b * a.table_stride;
+  if (seq.used > a.budget && seq.used <= KEYS) {
     score_pages<D, CHOOSE_NT / 64>(a, sm.score, sm.ids, b, h, seq.used, 0, seq.used, [&](int j, uint64_t key) { sm.keys[j] = key; });
     __syncthreads();
     select_pages(a, sm.select, bh, seq, [&](int j) { return sm.keys[j]; }, [&](int j) { return sm.ids[j]; });
+  } else if (seq.used > a.budget) {  // more than LDS holds: keys in the workspace
+    uint64_t* keys = a.keys + (int64_t)bh * a.width;
+    for (int j0 = 0; j0 < seq.used; j0 += KEYS) {
+      score_pages<D, CHOOSE_NT / 64>(a, sm.score, sm.ids, b, h, seq.used, j0, imin(seq.used, j0 + KEYS),
+                                     [&](int j, uint64_t key) { keys[j] = key; });
+      __syncthreads();
+    }
+    select_pages(a, sm.select, bh, seq, [&](int j) { return keys[j]; }, [&](int j) { return row[j]; });
   } else {  // every page that there is
-    const int* row = a.table + (int64_t)b * a.table_stride;
     select_pages(a, sm.select, bh, seq, [&](int j) -> uint64_t { return (unsigned)row[j] < (unsigned)a.num_pages; },
                  [&](int j) { return row[j]; });
   }
 }
 
-// Several workgroups a sequence and KV head: keys of a.chunk pages each, in the workspace ...  Two sequences of 120,000
+// Several workgroups a sequence and KV head: keys of SCORE_PAGES pages each, in the workspace ...  Two sequences of 120,000
 // tokens in pages of 64 with 128 query rows (16 MB): 9.9 us, then 8.7 for the choice, a chain of loads and barriers each.
 template <int D>
 __global__ __launch_bounds__(SCORE_NT) void score_kernel(SelectArgs a) {
@@ -370,13 +379,18 @@ __global__ __launch_bounds__(SCORE_NT) void score_kernel(SelectArgs a) {
     ScoreSmem<D, SCORE_NT / 64> score;
     int ids[SCORE_PAGES];
   } sm;
-  const int chunks = cdiv(a.width, a.chunk);
-  const int c = blockIdx.x % chunks, bh = blockIdx.x / chunks, h = bh % a.Hkv, b = bh / a.Hkv;
-  const SelectSeq seq = select_seq(a, b);
-  if (c * a.chunk >= seq.used) return;
-  uint64_t* keys = a.keys + (int64_t)bh * a.width;
-  score_pages<D, SCORE_NT / 64>(a, sm.score, sm.ids, b, h, seq.used, c * a.chunk, imin(seq.used, (c + 1) * a.chunk),
-                    [&](int j, uint64_t key) { keys[j] = key; });
+  // (the first pages of all lists, then the next ones, ...: sequences far shorter than the table leave the last ones empty)
+  const int chunks = cdiv(a.width, SCORE_PAGES), items = a.B * a.Hkv;
+  const int64_t total = (int64_t)items * chunks;  // checked on the host
+  for (int64_t t = blockIdx.x; t < total; t += gridDim.x) {
+    const int c = (int)(t / items), bh = (int)(t - (int64_t)c * items), h = bh % a.Hkv, b = bh / a.Hkv;
+    const SelectSeq seq = select_seq(a, b);
+    if (c * SCORE_PAGES >= seq.used) continue;
+    uint64_t* keys = a.keys + (int64_t)bh * a.width;
+    score_pages<D, SCORE_NT / 64>(a, sm.score, sm.ids, b, h, seq.used, c * SCORE_PAGES, imin(seq.used, (c + 1) * SCORE_PAGES),
+                                  [&](int j, uint64_t key) { keys[j] = key; });
+    __syncthreads();
+  }
 }
 // ... and the choice among them.
 __global__ __launch_bounds__(SELECT_NT) void select_kernel(SelectArgs a) {
@@ -402,9 +416,11 @@ __global__ __launch_bounds__(SELECT_NT) void select_kernel(SelectArgs a) {
 // workgroup and several: one sequence of 250, 380, 510 pages 9.2 11.1 12.6 and 10.1 10.5 10.3; four of 250, 380, 510 9.4 11.4
 // 12.9 and 10.4 11.0 11.2; 16 of 140, 510 8.3 14.5 and 12.2 16.3.  us a call, several with 256 pages each: one of 1000 pages
 // 20.5 and 15.3; 2000 pages of 8, 16, 32, 64 37 40 58 99 and 24 40 67 127; 4062 pages of 16, 32 74 108 and 72 124.
+// In a table of 8193 pages, which bounds them for the host: 16 sequences of 125, 2000, 8192 pages 8.8 40 200 and 22 59 196;
+// 32 of 125, 8192 9.0 279 and 29 353; 64 of 500 29 and 79.
 bool select_fused(const SelectArgs& a) {
   const int items = a.B * a.Hkv;
-  return a.width <= SELECT_KEYS && (a.width <= (items <= 32 ? 320 : 512) || items >= 256);
+  return a.width <= (items <= 32 ? 320 : 512) || items >= 128;
 }
 
 }  // namespace
@@ -422,8 +438,7 @@ hipError_t launch_summarize(const SummaryArgs& in, int D, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_select(const SelectArgs& in, int D, hipStream_t st) {
-  SelectArgs a = in;
+hipError_t launch_select(const SelectArgs& a, int D, hipStream_t st) {
   const unsigned items = (unsigned)a.B * a.Hkv;
   if (select_fused(a)) {
     const bool few = a.width <= 1024;
@@ -433,11 +448,10 @@ hipError_t launch_select(const SelectArgs& in, int D, hipStream_t st) {
     else hipLaunchKernelGGL((choose_kernel<64, SELECT_KEYS>), dim3(items), dim3(CHOOSE_NT), 0, st, a);
     return hipGetLastError();
   }
-  // 128 pages a workgroup, or 256 where a launch would not hold the threads.  us a call
-  // (D = 128, 8 KV heads), 128 and 256: one sequence of 1000 pages 11.1 12.7, of 2048 14.1 15.8, of 8192 with 128 query rows
-  // 38.3 39.8; two of 2000, 128 rows 18.0 18.6; four of 4096 32.2 32.6.
-  a.chunk = (int64_t)items * cdiv(a.width, 128) <= 1 << 22 ? 128 : SCORE_PAGES;
-  const dim3 grid(items * cdiv(a.width, a.chunk));
+  // 128 pages a workgroup at a time; us a call (D = 128, 8 KV heads), 128 and 256: one sequence of 1000 pages 11.1 12.7, of
+  // 2048 14.1 15.8, of 8192 with 128 query rows 38.3 39.8; two of 2000, 128 rows 18.0 18.6; four of 4096 32.2 32.6.
+  const int64_t tasks = (int64_t)items * cdiv(a.width, SCORE_PAGES);
+  const dim3 grid((unsigned)(tasks < SCORE_WORKGROUPS ? tasks : SCORE_WORKGROUPS));
   if (D == 128) hipLaunchKernelGGL(score_kernel<128>, grid, dim3(SCORE_NT), 0, st, a);
   else hipLaunchKernelGGL(score_kernel<64>, grid, dim3(SCORE_NT), 0, st, a);
   const hipError_t e = hipGetLastError();

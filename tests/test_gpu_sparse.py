@@ -398,6 +398,10 @@ def _select_inputs(B, Hq, Hkv, D, S, P, width, lens, seed):
     (2, 4, 4, 128, 32, 16, 100, [1600, 1599], 16, 2, 0), (2, 12, 3, 64, 3, 32, 300, [9600, 4000], 299, 1, 1),
     (2, 4, 1, 128, 40, 16, 700, [11200, 8209], 33, 0, 33), (1, 8, 8, 64, 1, 16, 2100, [33600], 7, 3, 4),
     (2, 16, 8, 128, 2, 16, 321, [5136, 2049], 40, 1, 2), (33, 2, 1, 64, 1, 16, 321, [i * 155 for i in range(33)], 40, 1, 2),
+    # tables far wider than the sequences, and sequences of more pages than LDS holds
+    (130, 2, 1, 64, 1, 16, 4100, [65600, 65537, 65536, 0, 1] + [i * 9 for i in range(125)], 40, 1, 2),
+    (16, 8, 8, 128, 2, 16, 9000, [140000, 70000, 131073] + [i * 90 for i in range(13)], 50, 1, 2),
+    (65, 2, 1, 64, 1, 16, 9000, [140000, 0, 33000] + [i * 50 for i in range(62)], 50, 1, 2),
     (1, 2, 1, 128, 1, 16, 12000, [191999], 2048, 1, 1), (70, 4, 2, 64, 1, 16, 9, [i * 2 for i in range(70)], 5, 1, 1),
     (2, 65, 1, 64, 5, 128, 20, [2560, 100], 20, 0, 0), (3, 4, 2, 64, 1, 16, 10, [-4, 1 << 30, 160], 5, 1, 1),
 ])
