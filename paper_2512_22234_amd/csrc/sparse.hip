@@ -116,10 +116,10 @@ template <int D, int NW>
 struct ScoreSmem {
   double part[NW][2 * D], sum[2 * D];  // at e * CPP + (lane of a page): feature e of eight (no two lanes in one bank)
 };
-template <int D, int NW, class Put>
+template <int D, int NW, int U = 8, class Put>
 __device__ inline void score_pages(const SelectArgs& a, ScoreSmem<D, NW>& sm, int* ids, int b, int h, int used, int j0, int j1,
                                    Put put) {
-  constexpr int CPP = D / 4, PPI = 64 / CPP, U = 8, UQ = 4;
+  constexpr int CPP = D / 4, PPI = 64 / CPP, UQ = 4;
   static_assert(2 * D <= 64 * NW, "a thread a sum");
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int in_page = lane % CPP, side = in_page / (CPP / 2), d0 = in_page % (CPP / 2) * 8;
@@ -338,11 +338,13 @@ __device__ inline void select_pages(const SelectArgs& a, SelectSmem<NT>& sm, int
   if (tid == (used > 0 ? (used - 1) % NT : 0)) a.rows_out[bh] = tail >= 0 ? tail : count << a.log_size;
 }
 
-// One workgroup a sequence and KV head, its pages and keys in LDS (past KEYS pages, keys in the workspace).  64 sequences of 512 to 8192 tokens in pages of 16 (61 MB
-// of summaries, D = 128, 8 KV heads, 16 query rows) 21 us: 12 for the reading, as fast as HBM gives it, and 7, all that one
+// One workgroup a sequence and KV head, its pages and keys in LDS (past KEYS pages, keys in the workspace).  64 sequences of
+// 512 to 8192 tokens in pages of 16 (61 MB of summaries, D = 128, 8 KV heads, 16 query rows) 21 us: 12 for the reading, as fast as HBM gives it, and 7, all that one
 // sequence of 94 pages takes, for the chain of query rows, first pages, and the digits of the choice.
 // (four waves a SIMD: two workgroups a CU)
-template <int D, int KEYS>
+// LONG: tables of more than KEYS pages.  (Four loads in flight a wave: with eight, and the longer lists' loop, a wave's
+// registers would not do.)
+template <int D, int KEYS, bool LONG>
 __global__ __launch_bounds__(CHOOSE_NT, 4) void choose_kernel(SelectArgs a) {
   __shared__ struct {
     uint64_t keys[KEYS];
@@ -353,18 +355,21 @@ __global__ __launch_bounds__(CHOOSE_NT, 4) void choose_kernel(SelectArgs a) {
   const int bh = blockIdx.x, h = bh % a.Hkv, b = bh / a.Hkv;
   const SelectSeq seq = select_seq(a, b);
   const int* row = a.table + (int64_t)b * a.table_stride;
-  if (seq.used > a.budget && seq.used <= KEYS) {
-    score_pages<D, CHOOSE_NT / 64>(a, sm.score, sm.ids, b, h, seq.used, 0, seq.used, [&](int j, uint64_t key) { sm.keys[j] = key; });
-    __syncthreads();
-    select_pages(a, sm.select, bh, seq, [&](int j) { return sm.keys[j]; }, [&](int j) { return sm.ids[j]; });
-  } else if (seq.used > a.budget) {  // more than LDS holds: keys in the workspace
+  if (seq.used > a.budget) {
+    const bool held = !LONG || seq.used <= KEYS;
     uint64_t* keys = a.keys + (int64_t)bh * a.width;
-    for (int j0 = 0; j0 < seq.used; j0 += KEYS) {
-      score_pages<D, CHOOSE_NT / 64>(a, sm.score, sm.ids, b, h, seq.used, j0, imin(seq.used, j0 + KEYS),
-                                     [&](int j, uint64_t key) { keys[j] = key; });
+    int j0 = 0;
+    do {
+      score_pages<D, CHOOSE_NT / 64, LONG ? 4 : 8>(a, sm.score, sm.ids, b, h, seq.used, j0, LONG ? imin(seq.used, j0 + KEYS) : seq.used,
+                                                   [&](int j, uint64_t key) {
+                                                     if (held) sm.keys[j] = key;
+                                                     else keys[j] = key;
+                                                   });
       __syncthreads();
-    }
-    select_pages(a, sm.select, bh, seq, [&](int j) { return keys[j]; }, [&](int j) { return row[j]; });
+      j0 += KEYS;
+    } while (LONG && j0 < seq.used);
+    select_pages(a, sm.select, bh, seq, [&](int j) { return held ? sm.keys[j] : keys[j]; },
+                 [&](int j) { return held ? sm.ids[j] : row[j]; });
   } else {  // every page that there is
     select_pages(a, sm.select, bh, seq, [&](int j) -> uint64_t { return (unsigned)row[j] < (unsigned)a.num_pages; },
                  [&](int j) { return row[j]; });
@@ -416,11 +421,18 @@ __global__ __launch_bounds__(SELECT_NT) void select_kernel(SelectArgs a) {
 // workgroup and several: one sequence of 250, 380, 510 pages 9.2 11.1 12.6 and 10.1 10.5 10.3; four of 250, 380, 510 9.4 11.4
 // 12.9 and 10.4 11.0 11.2; 16 of 140, 510 8.3 14.5 and 12.2 16.3.  us a call, several with 256 pages each: one of 1000 pages
 // 20.5 and 15.3; 2000 pages of 8, 16, 32, 64 37 40 58 99 and 24 40 67 127; 4062 pages of 16, 32 74 108 and 72 124.
-// In a table of 8193 pages, which bounds them for the host: 16 sequences of 125, 2000, 8192 pages 8.8 40 200 and 22 59 196;
-// 32 of 125, 8192 9.0 279 and 29 353; 64 of 500 29 and 79.
+// In a table of 8193 pages, which bounds them for the host: 16 sequences of 125, 2000, 8192 pages 8.9 43 215 and 22 59 196;
+// 32 of 125, 8192 9.0 276 and 29 353; 64 of 500 29 and 79.
 bool select_fused(const SelectArgs& a) {
   const int items = a.B * a.Hkv;
   return a.width <= (items <= 32 ? 320 : 512) || items >= 128;
+}
+
+template <int D>
+void launch_choose(const SelectArgs& a, unsigned items, hipStream_t st) {
+  if (a.width <= 1024) hipLaunchKernelGGL((choose_kernel<D, 1024, false>), dim3(items), dim3(CHOOSE_NT), 0, st, a);
+  else if (a.width <= SELECT_KEYS) hipLaunchKernelGGL((choose_kernel<D, SELECT_KEYS, false>), dim3(items), dim3(CHOOSE_NT), 0, st, a);
+  else hipLaunchKernelGGL((choose_kernel<D, SELECT_KEYS, true>), dim3(items), dim3(CHOOSE_NT), 0, st, a);
 }
 
 }  // namespace
@@ -441,11 +453,8 @@ hipError_t launch_summarize(const SummaryArgs& in, int D, hipStream_t st) {
 hipError_t launch_select(const SelectArgs& a, int D, hipStream_t st) {
   const unsigned items = (unsigned)a.B * a.Hkv;
   if (select_fused(a)) {
-    const bool few = a.width <= 1024;
-    if (D == 128 && few) hipLaunchKernelGGL((choose_kernel<128, 1024>), dim3(items), dim3(CHOOSE_NT), 0, st, a);
-    else if (D == 128) hipLaunchKernelGGL((choose_kernel<128, SELECT_KEYS>), dim3(items), dim3(CHOOSE_NT), 0, st, a);
-    else if (few) hipLaunchKernelGGL((choose_kernel<64, 1024>), dim3(items), dim3(CHOOSE_NT), 0, st, a);
-    else hipLaunchKernelGGL((choose_kernel<64, SELECT_KEYS>), dim3(items), dim3(CHOOSE_NT), 0, st, a);
+    if (D == 128) launch_choose<128>(a, items, st);
+    else launch_choose<64>(a, items, st);
     return hipGetLastError();
   }
   // 128 pages a workgroup at a time; us a call (D = 128, 8 KV heads), 128 and 256: one sequence of 1000 pages 11.1 12.7, of
