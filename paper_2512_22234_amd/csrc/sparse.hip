@@ -339,8 +339,9 @@ __device__ inline void select_pages(const SelectArgs& a, SelectSmem<NT>& sm, int
 }
 
 // One workgroup a sequence and KV head, its pages and keys in LDS (past KEYS pages, keys in the workspace).  64 sequences of
-// 512 to 8192 tokens in pages of 16 (61 MB of summaries, D = 128, 8 KV heads, 16 query rows) 21 us: 12 for the reading, as fast as HBM gives it, and 7, all that one
-// sequence of 94 pages takes, for the chain of query rows, first pages, and the digits of the choice.
+// 512 to 8192 tokens in pages of 16 (61 MB of summaries, D = 128, 8 KV heads, 16 query rows) 21 us: 12 for the reading, as
+// fast as HBM gives it, and 7, all that one sequence of 94 pages takes, for the chain of query rows, first pages, and the
+// digits of the choice.
 // (four waves a SIMD: two workgroups a CU)
 // LONG: tables of more than KEYS pages.  (Four loads in flight a wave: with eight, and the longer lists' loop, a wave's
 // registers would not do.)
@@ -360,11 +361,11 @@ __global__ __launch_bounds__(CHOOSE_NT, 4) void choose_kernel(SelectArgs a) {
     uint64_t* keys = a.keys + (int64_t)bh * a.width;
     int j0 = 0;
     do {
-      score_pages<D, CHOOSE_NT / 64, LONG ? 4 : 8>(a, sm.score, sm.ids, b, h, seq.used, j0, LONG ? imin(seq.used, j0 + KEYS) : seq.used,
-                                                   [&](int j, uint64_t key) {
-                                                     if (held) sm.keys[j] = key;
-                                                     else keys[j] = key;
-                                                   });
+      const int j1 = LONG ? imin(seq.used, j0 + KEYS) : seq.used;
+      score_pages<D, CHOOSE_NT / 64, LONG ? 4 : 8>(a, sm.score, sm.ids, b, h, seq.used, j0, j1, [&](int j, uint64_t key) {
+        if (held) sm.keys[j] = key;
+        else keys[j] = key;
+      });
       __syncthreads();
       j0 += KEYS;
     } while (LONG && j0 < seq.used);
