@@ -531,7 +531,9 @@ size_t bd_attn_paged_shared_decode_workspace_bytes(int B, int groups, int S, int
  * cache_lens[b]) are written, each over the page's positions below
  * cache_lens[b]; the other summaries are left as they are.  So with from_lens
  * the lengths before some tokens were added and cache_lens those after, the
- * summaries follow the cache.  A table entry outside [0, num_pages) is passed over.
+ * summaries follow the cache.  A sequence whose from_lens[b] is not below its
+ * cache_lens[b] (one that waits, is done or was cut short) writes none.  A table entry
+ * outside [0, num_pages) is passed over.
  *
  * K_pages and page_table as for bd_attn_paged_decode_fwd (no bound on
  * row_stride); summaries: bfloat16 [num_pages, Hkv, 2, D].  B * Hkv at most

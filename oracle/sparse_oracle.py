@@ -58,7 +58,9 @@ def summarize(Kp, table, before, lens, summaries):
     pages, _, P, _ = Kp.shape
     for b in range(len(lens)):
         n = min(max(int(lens[b]), 0), len(table[b]) * P)
-        for j in range(min(max(int(before[b]), 0), n) // P, -(-n // P)):
+        if before[b] >= n:  # no new position
+            continue
+        for j in range(max(int(before[b]), 0) // P, -(-n // P)):
             if 0 <= table[b][j] < pages:
                 k = Kp[table[b][j], :, :min(P, n - j * P)]
                 out[table[b][j]] = np.stack([k.min(axis=1), k.max(axis=1)], axis=1)

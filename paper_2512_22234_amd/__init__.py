@@ -1070,7 +1070,8 @@ def bd_paged_summarize(k_pages, page_table, from_lens, cache_lens, summaries, st
 
     k_pages [pages,Hkv,page_size,D] (any strides as for the other paged calls),
     page_table int32 [B,max_pages]; summaries [pages,Hkv,2,D] bfloat16, updated
-    in place (the other pages' are left as they are) and returned."""
+    in place (the other pages' are left as they are, all of a sequence's where
+    from_lens[b] >= cache_lens[b]) and returned."""
     if k_pages.dim() != 4:
         raise ValueError("k_pages [pages,Hkv,page_size,D] expected")
     Hkv, D, dev = k_pages.shape[1], k_pages.shape[3], k_pages.device

@@ -29,7 +29,8 @@ __global__ __launch_bounds__(256) void summarize_kernel(SummaryArgs a) {
   const int z = blockIdx.x / a.B, b = blockIdx.x % a.B;  // (few pages of each sequence: their workgroups on all dies)
   const int P = 1 << a.pages.log_size, room = a.width << a.pages.log_size;
   const int len = imin(imax(a.lens[b], 0), room), from = imin(imax(a.from[b], 0), len);
-  const int j1 = (len + P - 1) >> a.pages.log_size;
+  // (no new position, no page: the last one of a sequence that waits or is done may have another owner)
+  const int j1 = from < len ? (len + P - 1) >> a.pages.log_size : 0;
   const int row = lane / CPR, chunk = lane % CPR;
   const int* table = a.table + (int64_t)b * a.table_stride;
   const int i0 = 4 * z + w, dj = 4 * a.split / a.Hkv, dh = 4 * a.split % a.Hkv;

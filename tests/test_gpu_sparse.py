@@ -371,6 +371,60 @@ def test_summaries_match_oracle(B, Hkv, D, P, order, before, after):
     np.testing.assert_array_equal(_np(s), want)
 
 
+# Sequences without a new position: in the middle of a page, at its edge, truncated ones, lengths past the table.
+IDLE = [(20, 20), (16, 16), (32, 20), (21, 20), (128, 128), (1 << 30, 200), (1 << 30, 1 << 30), (0, 0), (5, -1), (9, 3)]
+
+
+@pytest.mark.parametrize("Hkv,D,P,order", [(1, 64, 16, "heads"), (3, 128, 16, "tokens"), (8, 128, 64, "heads"), (2, 64, 128, "sides")])
+def test_summaries_of_idle_sequences_stay(Hkv, D, P, order):
+    """Equal lengths before and after: no summary is written; a sequence with one new token between them has its own."""
+    print(f"[sparse] idle H{Hkv} D{D} P{P} {order}", flush=True)
+    g = torch.Generator().manual_seed(P + D)
+    width = 128 // P
+    n = (len(IDLE) + 1) * width
+    kp, _ = _cache(n, Hkv, P, D, order, g)
+    table = torch.arange(n, dtype=torch.int32).view(-1, width).to(DEV)
+    before, after = [a for a, _ in IDLE] + [17], [b for _, b in IDLE] + [18]
+    s = torch.full((n, Hkv, 2, D), 3.0, dtype=BF, device=DEV)
+    bd.bd_paged_summarize(kp, table, *_ints(before, after), s)
+    page = len(IDLE) * width + 17 // P
+    rows = kp[page, :, : 18 - 17 // P * P]
+    assert torch.equal(s[page], torch.stack([rows.amin(1), rows.amax(1)], 1))
+    s[page] = 3.0
+    assert (s == 3.0).all()
+
+
+def test_summaries_of_pages_that_an_idle_sequence_gave_away():
+    """A finished sequence's last page now belongs to another, which adds to it: the summary is over the owner's keys,
+    also in a captured call whose lengths go on."""
+    Hkv, D, P, width = 2, 128, 16, 4
+    g = torch.Generator().manual_seed(41)
+    kp, _ = _cache(40, Hkv, P, D, "heads", g)
+    # 64 finished sequences of 20 keys around one that owns their last page, and a fork of it that waits at its first key
+    table = torch.tensor([[i % 30, 35, -1, -1] for i in range(64)], **I32)
+    table = torch.cat([table[:32], _ints([[34, 35, 36, -1]]), _ints([[33, 35, -1, -1]]), table[32:]])
+    lens = [20] * 32 + [31, 17] + [20] * 32
+    before, after = _ints(lens, lens)
+    before[32] = 30
+    s = torch.full((40, Hkv, 2, D), 3.0, dtype=BF, device=DEV)
+
+    def want():
+        return torch.tensor(oracle.summarize(_np(kp), table.tolist(), before.tolist(), after.tolist(), np.full(s.shape, 3.0)))
+
+    bd.bd_paged_summarize(kp, table, before, after, s)
+    assert (s.double().cpu() == want()).all() and (s[35] != 3.0).all() and (s[:30] == 3.0).all()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bd.bd_paged_summarize(kp, table, before, after, s)
+    for n in (32, 33, 34):
+        before[32], after[32] = n - 1, n
+        s.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (s.double().cpu() == want()).all(), n
+
+
 # ---------------------------------------------------------------------------
 # the choice
 

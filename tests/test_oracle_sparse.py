@@ -68,6 +68,18 @@ def test_summaries_follow_the_cache():
     np.testing.assert_array_equal(at_once[5, 0, 1], kp[5, 0, :8].max(axis=0))
 
 
+def test_no_new_position_no_summary():
+    """[from, len) names no position: nothing is written, inside a page as at its edge, and where from is past len."""
+    rng = np.random.default_rng(8)
+    kp, table = rng.normal(size=(4, 1, 16, 8)), np.array([[2, 0, 3]])
+    mark = np.full((4, 1, 2, 8), 7.0)
+    for before, after in ((20, 20), (16, 16), (32, 20), (21, 20), (48, 48), (99, 50), (0, 0), (3, -1), (1 << 30, 1 << 30)):
+        assert (oracle.summarize(kp, table, [before], [after], mark) == mark).all(), (before, after)
+    one = oracle.summarize(kp, table, [20], [21], mark)
+    np.testing.assert_array_equal(one[0, 0], [kp[0, 0, :5].min(axis=0), kp[0, 0, :5].max(axis=0)])
+    assert (one[1:] == mark[1:]).all()
+
+
 def test_choice_of_pages():
     """By hand: the first and the last page, then the highest scores, the earlier of equal ones; keys of the last page."""
     D = 64
