@@ -865,6 +865,9 @@ def _page_layout(k_shape, k_strides, v_shape, v_strides, Hkv, D):
 
 def _pages(k_pages, v_pages, Hkv, D, device):
     lay = _page_layout(k_pages.shape, k_pages.stride(), v_pages.shape, v_pages.stride(), Hkv, D)
+    bf16 = torch.bfloat16
+    if k_pages.dtype is bf16 and v_pages.dtype is bf16 and k_pages.device == device and v_pages.device == device:
+        return lay
     for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
         if t.dtype is not torch.bfloat16:
             raise TypeError(f"{name}: expected {torch.bfloat16}, got {t.dtype}")
@@ -959,15 +962,16 @@ def bd_attn_paged_decode_workspace_bytes(B, S, Hq, Hkv, D, page_size, max_pages,
 
 
 def _paged_inputs(call, q, k_pages, v_pages, k_new, v_new):
-    """Checks the arrays that the decode calls over pages share: (B, Hq, S, Hkv, D, page arguments, addresses
-    of the block's keys and values)."""
+    """Checks the arrays that the decode calls over pages share: (shape of q, KV heads, device, page arguments,
+    addresses of the block's keys and values)."""
     if q.dim() != 4 or k_pages.dim() != 4:
         raise ValueError("q [B,Hq,S,D] and k_pages/v_pages [pages,Hkv,page_size,D] expected")
     B, Hq, S, D = shape = q.shape
     Hkv, dev, bf16 = k_pages.shape[1], q.device, torch.bfloat16
     if q.dtype is not bf16:
         raise TypeError(f"{call} supports bfloat16 tensors, got {q.dtype}")
-    _check("q", q, shape, bf16, dev)
+    if not q.is_contiguous():
+        raise ValueError("q: must be contiguous")
     pages = _pages(k_pages, v_pages, Hkv, D, dev)
     if (k_new is None) != (v_new is None):
         raise ValueError("k_new and v_new: both or neither expected")
@@ -976,16 +980,14 @@ def _paged_inputs(call, q, k_pages, v_pages, k_new, v_new):
         _check("k_new", k_new, (B, Hkv, S, D), bf16, dev)
         _check("v_new", v_new, (B, Hkv, S, D), bf16, dev)
         kn, vn = _ptr(k_new), _ptr(v_new)
-    return B, Hq, S, Hkv, D, pages, kn, vn
+    return shape, Hkv, dev, pages, kn, vn
 
 
-def _paged_outputs(q, out, lse):
-    o = _result("out", out, q, q.shape)
-    shape = q.shape[:3]
+def _paged_lse(lse, B, Hq, S, device):
     if lse is None:
-        return o, torch.empty(shape, dtype=torch.float32, device=q.device)
-    _check("lse", lse, shape, torch.float32, q.device)
-    return o, lse
+        return torch.empty((B, Hq, S), dtype=torch.float32, device=device)
+    _check("lse", lse, (B, Hq, S), torch.float32, device)
+    return lse
 
 
 def bd_attn_paged_decode_fwd(q, k_pages, v_pages, page_table, cache_lens, k_new=None, v_new=None, scale=None, out=None,
@@ -997,14 +999,13 @@ def bd_attn_paged_decode_fwd(q, k_pages, v_pages, page_table, cache_lens, k_new=
     strided); cache_lens int32 [B], clamped to [0, max_pages * page_size];
     k_new, v_new [B,Hkv,S,D]: the block's own keys, or None where the queries
     see the cache alone.  Rows that see no key: O = 0, LSE = -inf."""
-    B, Hq, S, Hkv, D, pages, kn, vn = _paged_inputs("bd_attn_paged_decode_fwd", q, k_pages, v_pages, k_new, v_new)
-    n, P, sp, sh, sr = pages
-    dev = q.device
+    shape, Hkv, dev, (n, P, sp, sh, sr), kn, vn = _paged_inputs("bd_attn_paged_decode_fwd", q, k_pages, v_pages, k_new, v_new)
+    B, Hq, S, D = shape
     table_stride = _table_stride(page_table, B, dev)
     width = page_table.shape[1]
     _check("cache_lens", cache_lens, (B,), torch.int32, dev)
     with _launch_context(dev, stream):
-        o, l_ = _paged_outputs(q, out, lse)
+        o, l_ = _result("out", out, q, shape), _paged_lse(lse, B, Hq, S, dev)
         nbytes = _known_size("bd_attn_paged_decode_workspace_bytes", B, S, Hq, Hkv, D, P, width, BD_ATTN_BF16)
         ws, wp, wn = _workspace(nbytes, dev, workspace)
         st = lib().bd_attn_paged_decode_fwd(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(cache_lens), kn,
@@ -1033,9 +1034,8 @@ def bd_attn_paged_shared_decode_fwd(q, k_pages, v_pages, group_sizes, prefix_tab
     pages and keys of the prefixes; page_table, cache_lens and all else: the
     sequences' own keys, behind the prefix, as for bd_attn_paged_decode_fwd.
     (Empty groups and a prefix_table far wider than the prefixes cost time.)"""
-    B, Hq, S, Hkv, D, pages, kn, vn = _paged_inputs("bd_attn_paged_shared_decode_fwd", q, k_pages, v_pages, k_new, v_new)
-    n, P, sp, sh, sr = pages
-    dev = q.device
+    shape, Hkv, dev, (n, P, sp, sh, sr), kn, vn = _paged_inputs("bd_attn_paged_shared_decode_fwd", q, k_pages, v_pages, k_new, v_new)
+    B, Hq, S, D = shape
     if group_sizes.dim() != 1:
         raise ValueError("group_sizes: 1-D expected")
     groups = group_sizes.shape[0]
@@ -1047,7 +1047,7 @@ def bd_attn_paged_shared_decode_fwd(q, k_pages, v_pages, group_sizes, prefix_tab
     prefix_width, width = prefix_table.shape[1], page_table.shape[1]
     _check("cache_lens", cache_lens, (B,), torch.int32, dev)
     with _launch_context(dev, stream):
-        o, l_ = _paged_outputs(q, out, lse)
+        o, l_ = _result("out", out, q, shape), _paged_lse(lse, B, Hq, S, dev)
         nbytes = _known_size("bd_attn_paged_shared_decode_workspace_bytes", B, groups, S, Hq, Hkv, D, P, prefix_width, width,
                              BD_ATTN_BF16)
         ws, wp, wn = _workspace(nbytes, dev, workspace)
@@ -1145,9 +1145,8 @@ def bd_attn_paged_sparse_decode_fwd(q, k_pages, v_pages, lists, list_lens, k_new
                                     lse=None, workspace=None, stream=None):
     """bd_attn_paged_decode_fwd with pages of its own for each KV head: lists int32 [B,Hkv,max_pages]
     (contiguous), of which the first list_lens int32 [B,Hkv] keys are seen (bd_paged_select)."""
-    B, Hq, S, Hkv, D, pages, kn, vn = _paged_inputs("bd_attn_paged_sparse_decode_fwd", q, k_pages, v_pages, k_new, v_new)
-    n, P, sp, sh, sr = pages
-    dev = q.device
+    shape, Hkv, dev, (n, P, sp, sh, sr), kn, vn = _paged_inputs("bd_attn_paged_sparse_decode_fwd", q, k_pages, v_pages, k_new, v_new)
+    B, Hq, S, D = shape
     if lists.dim() != 3:
         raise ValueError("lists [B,Hkv,max_pages] expected")
     width = lists.shape[2]
@@ -1155,7 +1154,7 @@ def bd_attn_paged_sparse_decode_fwd(q, k_pages, v_pages, lists, list_lens, k_new
     _check("lists", lists, (B, Hkv, width), torch.int32, dev)
     _check("list_lens", list_lens, (B, Hkv), torch.int32, dev)
     with _launch_context(dev, stream):
-        o, l_ = _paged_outputs(q, out, lse)
+        o, l_ = _result("out", out, q, shape), _paged_lse(lse, B, Hq, S, dev)
         nbytes = _known_size("bd_attn_paged_sparse_decode_workspace_bytes", B, S, Hq, Hkv, D, P, width, BD_ATTN_BF16)
         ws, wp, wn = _workspace(nbytes, dev, workspace)
         st = lib().bd_attn_paged_sparse_decode_fwd(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(lists), _ptr(list_lens), kn,
