@@ -338,6 +338,36 @@ def test_shared_wide_tables_replayed():
         lambda: a[7].copy_(_ints([2, 0, 40, 3, 33, 7, 64, 0])), lambda: a[0].mul_(-0.5), lambda: a[3].copy_(_ints([0, 0, 0]))])
 
 
+def test_shared_wide_tables_many_groups():
+    """More groups than a workgroup has threads, empty ones and wild sizes between, 80 rows a member."""
+    g = np.random.default_rng(16)
+    sizes = [int(n) for n in g.choice([0, 1, 1, 2, 3, -3], 600)]
+    B = sum(max(n, 0) for n in sizes) + 5
+    assert B * 80 > 64 * len(sizes)
+    prefix = [int(n) for n in g.integers(0, 150, 600)]
+    a = _shared_inputs(sizes, prefix, [int(n) for n in g.integers(0, 40, B)], 2, 1, 64, 40, 64, "heads", False, 7)
+    _check_shared(a, bd.bd_attn_paged_shared_decode_fwd(*_widened(a)), "wide, many groups")
+
+
+# Groups that all have the same prefix and queries, with as many key tiles as make the runs' cuts pass 32 bits (2^22), in
+# one launch (four rows a group and KV head) and in launches of their own (128 rows).
+@pytest.mark.parametrize("groups,n,S,G,P", [(3900, 4, 1, 1, 32), (4000, 4, 1, 1, 32), (8350, 1, 32, 4, 64)])
+def test_shared_many_tiles(groups, n, S, G, P):
+    Hkv, D, prefix, own = 8, 64, 4000, [1, 64, 33, 40][:n]
+    print(f"[sparse] many tiles, {groups} groups of {n}, S{S}", flush=True)
+    a = _shared_inputs([n], [prefix], own, Hkv * G, Hkv, D, S, P, "heads", False, 43)
+    want, size = _shared_oracle(a), _shared_oracle(a, True)[0]
+    for i in (0, 3, 4, 5, 6, 7):
+        a[i] = a[i].repeat(groups, *[1] * (a[i].dim() - 1))
+    got = bd.bd_attn_paged_shared_decode_fwd(*a)
+    _check([x[:n] for x in got], want, size, f"many tiles, {groups} groups")
+    # the other groups: off by the same bound, against a result that is off by it
+    tol = torch.tensor(2 * (2.0 ** -8 * np.abs(want[0]) + SUMS * size), device=DEV, dtype=torch.float32)
+    for o, lse in zip(got[0].split(n * 500), got[1].split(n * 500)):
+        assert ((o.view(-1, *tol.shape).float() - got[0][:n].float()).abs() <= tol).all()
+        assert ((lse.view(-1, *tol.shape[:3]) - got[1][:n]).abs() <= 2 * SUMS).all()
+
+
 # ---------------------------------------------------------------------------
 # summaries
 
