@@ -510,6 +510,79 @@ def test_choice_among_equal_scores(budget):
     _select_check(q, s, table, lens, P, budget, 0, 0, f"zeros budget{budget}")
 
 
+# Each form of the choice: one workgroup a list with up to 1024, up to 4096 and more pages in the table (the last with lists
+# that it holds in LDS and lists that it does not), and several workgroups a list, whose keys the second launch holds in LDS or not.
+FORMS = [  # B, Hkv, D, width, lengths in pages
+    (3, 2, 64, 40, [40, 39, 17]), (64, 2, 128, 1024, [1024, 1023, 513, 40]), (64, 2, 64, 1025, [1025, 1024, 1000, 513, 41]),
+    (16, 8, 128, 2000, [2000, 1999, 1025, 9, 40]), (130, 1, 64, 4096, [4096, 4095, 2049, 40, 8]),
+    (32, 4, 128, 4096, [4096, 4095, 0, 41]), (64, 2, 64, 4097, [4097, 4096, 600, 1]), (16, 8, 128, 9000, [9000, 4097, 4096]),
+    (3, 2, 64, 700, [700, 699, 513]), (2, 4, 128, 5000, [5000, 4096]), (1, 8, 64, 4097, [4097]),
+]
+
+
+def _form(B, Hkv, D, width, pages, S=1, G=1, seed=5):
+    """Inputs of the first lists as given (the odd ones end inside a page), and of short ones behind them."""
+    lens = [16 * p - 5 * (i % 2) if p else 0 for i, p in enumerate(pages)] + [(37 * i) % 900 for i in range(B - len(pages))]
+    return _select_inputs(B, G * Hkv, Hkv, D, S, 16, width, lens, seed + width)
+
+
+@pytest.mark.parametrize("form", range(len(FORMS)))
+def test_choice_in_each_form(form):
+    a = _form(*FORMS[form], S=3, G=2)
+    for budget, first, last in ((1, 0, 0), (40, 1, 2), (min(2000, FORMS[form][3]), 2, 5)):
+        _select_check(*a, 16, budget, first, last, f"form {FORMS[form]} budget{budget}")
+
+
+@pytest.mark.parametrize("form", range(len(FORMS)))
+def test_choice_among_equal_scores_in_each_form(form):
+    q, s, table, lens = _form(*FORMS[form])
+    kinds = s[:4].clone()
+    for i in range(4):
+        s[i::4] = kinds[i * 3 % 4]
+    for budget in (1, 37, 600, 1100):
+        _select_check(q, s, table, lens, 16, budget, 0, 1 if budget > 1 else 0, f"ties, form {FORMS[form]} budget{budget}")
+    s.copy_(kinds[0].expand_as(s))
+    _select_check(q, s, table, lens, 16, 515, 1, 0, f"all equal, form {FORMS[form]}")
+    s.zero_()
+    s[::3] = -0.0
+    _select_check(q, s, table, lens, 16, 100, 0, 0, f"zeros, form {FORMS[form]}")
+
+
+@pytest.mark.parametrize("form", range(len(FORMS)))
+def test_choice_with_absent_pages_in_each_form(form):
+    """A third of the pages outside the pool, and a list of which fewer than the budget are inside."""
+    q, s, table, lens = _form(*FORMS[form])
+    g = torch.Generator().manual_seed(form)
+    for value in (-1, s.shape[0], -(1 << 31), (1 << 31) - 1):
+        table[(torch.rand(table.shape, generator=g) < 0.1).to(DEV)] = value
+    table[0, 7 : table.shape[1] - 3] = -1
+    for budget, first, last in ((30, 1, 2), (600, 0, 0)):
+        _select_check(q, s, table, lens, 16, budget, first, last, f"absent, form {FORMS[form]} budget{budget}")
+
+
+@pytest.mark.parametrize("form", range(len(FORMS)))
+def test_choice_in_each_form_workspace_streams_and_replays(form):
+    """A workspace full of ones with guards behind it and behind the results, another stream, and replays of a captured call
+    with other lengths, queries and summaries: the same lists."""
+    B, Hkv, D, width, _ = FORMS[form]
+    a = _form(*FORMS[form])
+    budget = 45
+    want = bd.bd_paged_select(*a, 16, budget)
+    n = bd.bd_paged_select_workspace_bytes(B, 1, Hkv, Hkv, D, 16, width, budget)
+    ws = torch.full((n + 64,), 255, dtype=torch.uint8, device=DEV)
+    lists, lens = torch.full((B * Hkv * budget + 16,), 7, **I32), torch.full((B * Hkv + 16,), 7, **I32)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = bd.bd_paged_select(*a, 16, budget, lists=lists[:-16].view(B, Hkv, budget), lens=lens[:-16].view(B, Hkv), workspace=ws[:n],
+                             stream=side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert (ws[n:] == 255).all() and (lists[-16:] == 7).all() and (lens[-16:] == 7).all()
+    _replayed(lambda: bd.bd_paged_select(*a, 16, budget, workspace=ws[:n]), f"select, form {form}", [
+        lambda: None, lambda: a[3].mul_(2).clamp_(max=400), lambda: a[3].copy_(a[3].flip(0)), lambda: a[0].mul_(-1),
+        lambda: a[1].add_(0.25), lambda: ws.fill_(255)])
+
+
 def test_choice_with_absent_pages():
     """Pages outside the pool are not chosen, whatever their place: all, the first and last ones, or all but fewer than the budget."""
     P, width = 16, 50
