@@ -53,3 +53,17 @@ def test_tile_loops(assembly, src):
             drained = sum("v_mfma" in y and "lgkmcnt(0)" in x for x, y in zip(block, block[1:]))
             assert drained <= 2, (name, drained)
         assert seen >= 2, name
+
+
+@pytest.mark.parametrize("D,products,copies", [(64, 8, 4), (128, 16, 8)])
+def test_prefix_tile_loops(assembly, D, products, copies):
+    """The prefixes' kernel: the scores' products with the copies of a tile among them, then the output's, without a wait
+    for copies, a scalar load or a repeated wait for all reads in between."""
+    blocks = [b for b in _blocks(assembly["shared.hip"], f"prefix_kernelILi{D}E") if sum("v_mfma" in x for x in b) >= 8]
+    assert [sum("v_mfma" in x for x in b) for b in blocks] == [products, 2 * products]
+    for block, n in zip(blocks, (copies, 0)):
+        at = [i for i, x in enumerate(block) if "v_mfma" in x]
+        inner = block[at[0]:at[-1]]
+        assert not any("vmcnt" in x or x.startswith("s_load") for x in inner), (D, block[0])
+        assert sum("v_mfma" in y and "lgkmcnt(0)" in x for x, y in zip(block, block[1:])) <= 2, (D, block[0])
+        assert sum("buffer_load" in x for x in block) == n == sum("buffer_load" in x and "lds" in x for x in block), (D, block[0])
