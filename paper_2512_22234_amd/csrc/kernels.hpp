@@ -423,7 +423,7 @@ struct SummaryArgs {
   int64_t table_stride;
   const int *from, *lens;
   __bf16* summaries;  // [pages][Hkv][2][D]
-  int split;          // workgroups a sequence and KV head (set by the launcher)
+  int split;          // workgroups a sequence (set by the launcher)
 };
 hipError_t launch_summarize(const SummaryArgs& a, int D, hipStream_t st);
 

@@ -8,7 +8,10 @@
 //   score = sum_d (Q+_d hi_d + Q-_d lo_d),  Q+ = sum_r max(q_r, 0), Q- = sum_r min(q_r, 0),
 // so it costs 2 D multiply-adds a page however many rows there are, and reading
 // the summaries, 4 D bytes a page and KV head, bounds the choice.  Scores are
-// float64: which pages are chosen must not depend on the order of a sum.
+// float64, summed in an order that is the same for every page and form of the choice,
+// so that equal summaries score equally and results repeat.  In another order of the
+// 2 D terms a score differs by up to about 2^-45 of their absolute sum: only pages nearer
+// to each other than that could be chosen differently there.
 #include "paged.hpp"
 
 namespace bd {
@@ -419,12 +422,19 @@ __global__ __launch_bounds__(SELECT_NT) void select_kernel(SelectArgs a) {
   }
 }
 
-// Whether one workgroup takes a sequence and KV head on its own.  Device us a call (D = 128, 8 KV heads, one query), one
-// workgroup and several: one sequence of 250, 380, 510 pages 9.2 11.1 12.6 and 10.1 10.5 10.3; four of 250, 380, 510 9.4 11.4
-// 12.9 and 10.4 11.0 11.2; 16 of 140, 510 8.3 14.5 and 12.2 16.3.  us a call, several with 256 pages each: one of 1000 pages
-// 20.5 and 15.3; 2000 pages of 8, 16, 32, 64 37 40 58 99 and 24 40 67 127; 4062 pages of 16, 32 74 108 and 72 124.
-// In a table of 8193 pages, which bounds them for the host: 16 sequences of 125, 2000, 8192 pages 8.9 43 215 and 22 59 196;
-// 32 of 125, 8192 9.0 276 and 29 353; 64 of 500 29 and 79.
+// Whether one workgroup takes a sequence and KV head on its own.  Device us a call (8 KV heads, one query), one workgroup and
+// several of SCORE_PAGES, by sequences and their pages:
+//   D = 128   one      1 of 250 380 510 1000   9.2 10.8 12.8 20.2    4 of 250 380 510 2000   9.4 11.1 12.8 36.2
+//             several                         10.4 10.0 10.6 10.8                           10.5 10.7 10.8 18.2
+//             one      8 of 510 1000 2000     13.0 21.4 36.8        12 of 510 2000          13.1 37.3
+//             several                         11.0 16.1 31.2                                14.6 41.0
+//             one     16 of 140 510 1000 2000 4062  8.1 13.9 22.2 37.3 67.6   32 of 510 1000 2000 4062  17.3 28.2 49.9 114
+//             several                              10.5 16.0 28.9 50.4 94.2                             28.9 48.2 89.5 184
+//   D = 64    one      1 of 250 380 510 1000   7.8  8.2  9.3 13.9    4 of 510 2000  9.7 22.7    16 of 510 2000  10.1 24.9
+//             several                         10.0  9.7  9.8 10.6                  10.1 15.6                    13.9 40.4
+// In a table of 8193 pages, which is all that the host knows of them (D = 128): 16 of 125, 2000, 8192 pages 8.1 41.6 213 and
+// 21.2 57.4 195; 32 of 125, 8192 8.6 277 and 28.8 355; 64 of 500 27.2 and 77.7.
+// (The sides meet between 64 and 96 lists; at the rule's own borders the worse side is up to a fifth slower.)
 bool select_fused(const SelectArgs& a) {
   const int items = a.B * a.Hkv;
   return a.width <= (items <= 32 ? 320 : 512) || items >= 128;
